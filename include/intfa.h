@@ -256,6 +256,45 @@ int int_flash_attn_fwd_half_rect(const signed char *Q_i8, const signed char *K_i
                                  const float *s_Q, const float *s_K,
                                  int B, int H, int Nq, int Nk, int d, int causal, void *O, int o_dtype, void *hip_stream);
 
+/*
+ * ---- A quantized cache in long use -----------------------------------------------------------------------------------
+ * The calls below read (or cut down) the cache of a batch: own keys K_i8 [B, Hkv, Nk, d] with s_K [B, Hkv, Nk], V [B, Hkv, Nk, d]
+ * either fp16 (s_V null) or INT8 with s_V [B, Hkv].  Nk is the size of the buffers; sequence b has L_b = lens[b] keys (device
+ * memory, int32 [B]; null: Nk; values outside [0, Nk] count as the nearer end).  What lies at or beyond L_b is not looked at.
+ *   Queries: Q_i8 [B, H, Nq, d], s_Q [B, H, Nq], H = G Hkv: query head h reads key head h / G.  The Nq queries of sequence b are its LAST
+ * positions: query i stands at p = L_b - Nq + i and sees own keys j <= p.  A query at p < 0 (padding in front, an empty
+ * sequence) sees no own key; one that sees no key at all gives zeros.
+ *   The weights are those of the half-INT8 variant, whatever V is: P~ = fp16(exp(S - m)), l the sum of the rounded weights, O = P~ V / l
+ * (times s_V) with fp32 accumulation.  Unlike Algorithm 1's INT8 P they do not lie on the grid of a running maximum, so the result depends
+ * on how the keys are shared out over the chip only by the rounding of a weight (2^-11 of it) and the order of fp32 additions.
+ * Supported: d in {64, 128}; H a multiple of Hkv; 2 Nk d and 2 Np d <= 0x7ff00000; B H <= 2^23, B H Nq <= 2^26.
+ *   Workspaces: device memory, 256-byte aligned, owned by the caller, contents undefined before and after, not to be shared by calls
+ * that may overlap (two streams, two captured graphs that may replay at once).  The ..._workspace_bytes functions return the bytes needed (0: none, the pointer may be null), -1 for
+ * sizes that the call refuses.
+ */
+
+/*
+ * Attention in which query p sees the last `window` keys up to its own, j > p - window, and the first `sinks` keys of the sequence,
+ * j < sinks: a prompt (Nq = Nk), a chunk, a decode step (Nq = 1).  window >= 1 (Nk and more: every key j <= p), sinks >= 0.  No key that
+ * no query of a tile of rows sees is read.  O [B, H, Nq, d] of o_dtype.
+ */
+long ifa_window_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks);
+
+int int_flash_attn_fwd_window(const signed char *Q_i8, const signed char *K_i8, const void *V, const float *s_Q, const float *s_K,
+                              const float *s_V, const int *lens, int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks,
+                              void *O, int o_dtype, void *workspace, long workspace_bytes, void *hip_stream);
+
+/*
+ * Attention for a batch whose sequences begin with the same Np >= 1 keys: shared keys Kp_i8, Vp [Hkv, Np, d], s_Kp [Hkv, Np], s_Vp [Hkv] (null
+ * exactly where s_V is), held once, and own keys as above behind them.  Every query sees all shared keys and its own keys j <= p.
+ */
+long ifa_prefix_workspace_bytes(int B, int H, int Hkv, int Nq, int Np, int Nk, int d);
+
+int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8, const void *Vp, const signed char *K_i8, const void *V,
+                              const float *s_Q, const float *s_Kp, const float *s_K, const float *s_Vp, const float *s_V, const int *lens,
+                              int B, int H, int Hkv, int Nq, int Np, int Nk, int d, void *O, int o_dtype,
+                              void *workspace, long workspace_bytes, void *hip_stream);
+
 /* Key-block size of the half-INT8 kernel for (d, causal); 0 if that pair is unsupported. */
 int ifa_block_cols_half(int d, int causal);
 

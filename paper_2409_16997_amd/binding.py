@@ -37,6 +37,10 @@ SIGNATURES = {
     "ifa_block_cols": (_i, [_i, _i]),
     "int_flash_attn_fwd_half": (_i, [_vp] * 5 + [_i] * 5 + [_vp, _i, _vp]),
     "int_flash_attn_fwd_half_rect": (_i, [_vp] * 5 + [_i] * 6 + [_vp, _i, _vp]),
+    "ifa_window_workspace_bytes": (_l, [_i] * 8),
+    "int_flash_attn_fwd_window": (_i, [_vp] * 7 + [_i] * 8 + [_vp, _i, _vp, _l, _vp]),
+    "ifa_prefix_workspace_bytes": (_l, [_i] * 7),
+    "int_flash_attn_fwd_prefix": (_i, [_vp] * 11 + [_i] * 7 + [_vp, _i, _vp, _l, _vp]),
     "ifa_block_cols_half": (_i, [_i, _i]),
     "ifa_debug_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
@@ -360,6 +364,111 @@ def int_flash_attn_fwd_half(Q_i8, K_i8, V_f16, s_Q, s_K, causal=False, out_dtype
 
 def block_cols_half(d: int, causal: bool) -> int:
     return lib().ifa_block_cols_half(int(d), int(bool(causal)))
+
+
+# ---- a quantized cache in long use
+
+def _operand(t, what, dtypes, shape, device):
+    """Address of a contiguous tensor of one of the dtypes and exactly this shape, on the device of the call."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise IntfaError(f"{what}: expected a contiguous tensor in GPU memory")
+    if t.dtype not in dtypes:
+        raise IntfaError(f"{what}: expected dtype {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise IntfaError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device.index != device:
+        raise IntfaError(f"{what} is on {t.device}, the current device is cuda:{device}")
+    return t.data_ptr()
+
+
+def _cache_sizes(Q_i8, K_i8):
+    if getattr(Q_i8, "dim", int)() != 4 or getattr(K_i8, "dim", int)() != 4:
+        raise IntfaError("Q [B, H, Nq, d] and K [B, Hkv, Nk, d] are 4-dimensional")
+    B, H, Nq, d = Q_i8.shape
+    Hkv, Nk = K_i8.shape[1:3]
+    if min(B, H, Nq, d, Hkv, Nk) == 0 or K_i8.shape[0] != B or K_i8.shape[3] != d or H % Hkv:
+        raise IntfaError(f"Q {tuple(Q_i8.shape)} and K {tuple(K_i8.shape)} do not agree (H is a multiple of Hkv, nothing is empty)")
+    return B, H, Hkv, Nq, Nk, d
+
+
+def _cache_operands(Q_i8, K_i8, V, s_Q, s_K, s_V, lens, out, out_dtype):
+    """(sizes, device, addresses of Q, K, V, s_Q, s_K, s_V and lens, out) of a call on a cache."""
+    import torch
+    sizes = B, H, Hkv, Nq, Nk, d = _cache_sizes(Q_i8, K_i8)
+    dev = torch.cuda.current_device()
+    i8, f32 = (torch.int8,), (torch.float32,)
+    at = [_operand(Q_i8, "Q_i8", i8, (B, H, Nq, d), dev), _operand(K_i8, "K_i8", i8, (B, Hkv, Nk, d), dev),
+          _operand(V, "V", (torch.float16,) if s_V is None else i8, (B, Hkv, Nk, d), dev),
+          _operand(s_Q, "s_Q", f32, (B, H, Nq), dev), _operand(s_K, "s_K", f32, (B, Hkv, Nk), dev),
+          None if s_V is None else _operand(s_V, "s_V", f32, (B, Hkv), dev),
+          None if lens is None else _operand(lens, "lens", (torch.int32,), (B,), dev)]
+    if out is None:
+        out = torch.empty_like(Q_i8, dtype=out_dtype or torch.float16)
+    else:
+        _operand(out, "out", (torch.float16, torch.bfloat16, torch.float32) if out_dtype is None else (out_dtype,), (B, H, Nq, d), dev)
+    return sizes, dev, at, out
+
+
+def _workspace(workspace, need, device):
+    """(address, bytes) of the caller's workspace or of one allocated here; the caller keeps the third value until the call is enqueued."""
+    import torch
+    if need < 0:
+        raise IntfaError("these sizes are not supported (d in {64, 128}; see include/intfa.h)")
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", device))
+    elif not isinstance(workspace, torch.Tensor) or workspace.device.index != device:
+        raise IntfaError("workspace: a uint8 tensor on the current device")
+    return _dev(workspace, torch.uint8), workspace.numel(), workspace
+
+
+def window_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: int, window: int, sinks: int = 0) -> int:
+    """Bytes of workspace int_flash_attn_fwd_window needs for this shape (0: none; -1: sizes that it refuses)."""
+    return int(lib().ifa_window_workspace_bytes(int(B), int(H), int(Hkv), int(Nq), int(Nk), int(d), min(int(window), 0x7fffffff), min(int(sinks), 0x7fffffff)))
+
+
+def int_flash_attn_fwd_window(Q_i8, K_i8, V, s_Q, s_K, window, sinks=0, s_V=None, lens=None, out_dtype=None, out=None, workspace=None):
+    """Attention with a sliding window over a quantized cache: int8 Q [B, H, Nq, d], K [B, Hkv, Nk, d] (H a multiple of Hkv) with
+    token-level scales, V [B, Hkv, Nk, d] fp16, or int8 with s_V [B, Hkv].  Sequence b has lens[b] keys (int32 [B]; None: Nk); its queries
+    are its last Nq positions, and the query at position p sees keys j <= p with j > p - window or j < sinks.  A query that sees nothing
+    gives zeros.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).  `workspace`: a uint8 device tensor of
+    window_workspace_bytes(...) bytes (allocated here if not given)."""
+    (B, H, Hkv, Nq, Nk, d), dev, at, out = _cache_operands(Q_i8, K_i8, V, s_Q, s_K, s_V, lens, out, out_dtype)
+    window, sinks = min(int(window), 0x7fffffff), min(int(sinks), 0x7fffffff)
+    if window < 1 or sinks < 0:
+        raise IntfaError("window is at least 1, sinks at least 0")
+    ws, n, _keep = _workspace(workspace, window_workspace_bytes(B, H, Hkv, Nq, Nk, d, window, sinks), dev)
+    _check(lib().int_flash_attn_fwd_window(*at, B, H, Hkv, Nq, Nk, d, window, sinks, out.data_ptr(), _dtype_enum(out), ws, n, _stream()),
+           "int_flash_attn_fwd_window")
+    return out
+
+
+def prefix_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Np: int, Nk: int, d: int) -> int:
+    """Bytes of workspace int_flash_attn_fwd_prefix needs for this shape (0: none; -1: sizes that it refuses)."""
+    return int(lib().ifa_prefix_workspace_bytes(int(B), int(H), int(Hkv), int(Nq), int(Np), int(Nk), int(d)))
+
+
+def int_flash_attn_fwd_prefix(Q_i8, Kp_i8, Vp, K_i8, V, s_Q, s_Kp, s_K, s_Vp=None, s_V=None, lens=None, out_dtype=None, out=None, workspace=None):
+    """Attention of a batch whose sequences begin with the same keys: shared Kp, Vp [Hkv, Np, d] with s_Kp [Hkv, Np], held once, in front of
+    own K, V [B, Hkv, Nk, d] (lens[b] of them).  V and Vp are fp16, or int8 with s_V [B, Hkv] and s_Vp [Hkv].  Queries as in
+    int_flash_attn_fwd_window, without the window: each sees all shared keys and its own keys j <= lens[b] - Nq + i."""
+    import torch
+    (B, H, Hkv, Nq, Nk, d), dev, at, out = _cache_operands(Q_i8, K_i8, V, s_Q, s_K, s_V, lens, out, out_dtype)
+    if getattr(Kp_i8, "dim", int)() != 3 or Kp_i8.shape[1] == 0:
+        raise IntfaError("Kp is [Hkv, Np, d] with at least one key")
+    if (s_Vp is None) != (s_V is None):
+        raise IntfaError("s_V and s_Vp: both (int8 V) or neither (fp16 V)")
+    Np = Kp_i8.shape[1]
+    kp, vp = _operand(Kp_i8, "Kp_i8", (torch.int8,), (Hkv, Np, d), dev), _operand(Vp, "Vp", (V.dtype,), (Hkv, Np, d), dev)
+    skp = _operand(s_Kp, "s_Kp", (torch.float32,), (Hkv, Np), dev)
+    svp = None if s_Vp is None else _operand(s_Vp, "s_Vp", (torch.float32,), (Hkv,), dev)
+    ws, n, _keep = _workspace(workspace, prefix_workspace_bytes(B, H, Hkv, Nq, Np, Nk, d), dev)
+    q, k, v, sq, sk, sv, ln = at
+    _check(lib().int_flash_attn_fwd_prefix(q, kp, vp, k, v, sq, skp, sk, svp, sv, ln, B, H, Hkv, Nq, Np, Nk, d, out.data_ptr(), _dtype_enum(out), ws, n, _stream()),
+           "int_flash_attn_fwd_prefix")
+    return out
 
 
 def debug_fwd(Q_i8, K_i8, V_i8, s_Q, s_K, s_V, causal=False, P_in=None, fill=-1):

@@ -1,0 +1,416 @@
+// Attention over a quantized cache for gfx950: with a sliding window and sinks, and over keys that a batch shares.
+//
+//     S = s_Q s_K (Q K^T)        v_mfma_i32_32x32x32_i8, exact in int32, fp32 scales
+//     P~ = fp16(exp(S - m))      m the running maximum; l = the sum of the rounded weights in fp32
+//     O = P~ V / l               v_mfma_f32_32x32x16_f16, fp32 accumulation; INT8 V enters as fp16 (exactly) and its scale meets O
+//
+// The weights are those of the half-INT8 variant, for INT8 V too: rounded relative to themselves (2^-11) rather than on the grid of a running maximum,
+// they do not depend on where a sequence is cut, so its keys may be shared out over workgroups and the parts joined with e^{m_part - m}.
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_bf16.h>
+#include <stdint.h>
+
+#include "intfa.h"
+#include "intfa_internal.h"
+#include "intfa_device.h"
+#include "intfa_cache.h"
+
+namespace {
+
+using namespace ifa_cache;
+
+// Four outputs of a row, to fp32, fp16 or bf16
+__device__ __forceinline__ void store4(void *O, int o_dtype, long at, float a, float b, float c, float d) {
+    if (o_dtype == IFA_F32) *reinterpret_cast<float4 *>(static_cast<float *>(O) + at) = float4{a, b, c, d};
+    else if (o_dtype == IFA_F16) *reinterpret_cast<uint2 *>(static_cast<__half *>(O) + at) = Pack4<__half>::pack(a, b, c, d);
+    else *reinterpret_cast<uint2 *>(static_cast<__hip_bfloat16 *>(O) + at) = Pack4<__hip_bfloat16>::pack(a, b, c, d);
+}
+
+// Row `row` of unit `unit` in Q and O (in rows)
+__device__ __forceinline__ long row_of(const Call &c, bool all, int unit, int row) {
+    const int per = c.Nq * c.G, b = all ? row / per : unit / c.Hkv, hk = all ? unit : unit % c.Hkv;
+    const int in = all ? row % per : row, i = in / c.G, g = in % c.G;
+    return (static_cast<long>(b * c.Hkv + hk) * c.G + g) * c.Nq + i;
+}
+
+// ---- 32 rows against many keys: every wavefront for itself -------------------------------------------------------
+// The four wavefronts of a workgroup hold the same 32 rows and take every fourth tile of 32 keys each, with an online softmax of their own; they meet
+// once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
+// asks for the one that goes into its place before it computes.
+constexpr int FEW_WAVES = 4;
+template <int D, bool VI8> struct SmemFew {
+    static constexpr int ST = 3, KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
+    union {
+        struct {
+            alignas(4096) int8_t k[FEW_WAVES][ST][KB];
+            alignas(4096) int8_t v[FEW_WAVES][ST][VB];
+            alignas(128) float sk[FEW_WAVES][ST][32];
+        };
+        float o[FEW_WAVES][32][D];                               // when the loop is over
+    };
+    float2 ml[FEW_WAVES][32];
+};
+static_assert(sizeof(SmemFew<128, false>) <= 160 * 1024, "LDS budget");
+
+// ALL: unit = key head, rows of the whole batch, the shared keys alone.  Otherwise unit = (sequence, key head), shared keys (if any) and its own.
+template <int D, bool VI8, bool ALL>
+__global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Call c, int units, int row_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemFew<D, VI8> sm;
+    constexpr int KS = D / 32, DT = D / 32, ST = SmemFew<D, VI8>::ST, KB = SmemFew<D, VI8>::KB, VB = SmemFew<D, VI8>::VB;
+    constexpr int PER_TILE = K_PIECES<D> + V_PIECES<D, VI8> + 1;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // the row tiles of one share of the keys run 8 apart: on one XCD
+    const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), rt = in8 >> 3;
+    const int unit = share / c.splits, split = share % c.splits;
+    if (unit >= units) return;
+    const int b = ALL ? 0 : unit / c.Hkv, hk = ALL ? unit : unit % c.Hkv;
+    const int row0 = 32 * rt, last_row = imin(row0 + 31, c.rows - 1), row = imin(row0 + r, c.rows - 1);
+    const bool shared = ALL || c.Kp != nullptr;
+    const int L = ALL ? 0 : keys_of(c.lens, b, c.Nk);
+    // positions of the first and the last row, and of this lane's
+    const int p0 = ALL ? -1 : L - c.Nq + row0 / c.G, p1 = ALL ? -1 : L - c.Nq + last_row / c.G, p = ALL ? -1 : L - c.Nq + row / c.G;
+    const Runs runs(shared, c.Np, c.window, c.sinks, p0, p1);
+    const int tilesA = (runs.lenA + 31) / 32, tiles = tilesA + (runs.lenB + 31) / 32;
+    const int per = (tiles + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(tiles, t0 + per);
+
+    const long kA = shared ? static_cast<long>(hk) * c.Np : static_cast<long>(unit) * c.Nk, kB = static_cast<long>(unit) * c.Nk + runs.lo;
+    const int8_t *vA = static_cast<const int8_t *>(shared ? c.Vp : c.V), *vB = static_cast<const int8_t *>(c.V);
+    const BufRsrc rKA = make_rsrc((shared ? c.Kp : c.K) + kA * D, runs.lenA * D), rVA = make_rsrc(vA + kA * V_ROW<D, VI8>, runs.lenA * V_ROW<D, VI8>),
+                  rSA = make_rsrc((shared ? c.sKp : c.sK) + kA, runs.lenA * 4);
+    const BufRsrc rKB = ALL ? rKA : make_rsrc(c.K + kB * D, runs.lenB * D), rVB = ALL ? rVA : make_rsrc(vB + kB * V_ROW<D, VI8>, runs.lenB * V_ROW<D, VI8>),
+                  rSB = ALL ? rSA : make_rsrc(c.sK + kB, runs.lenB * 4);
+    const float unitA = VI8 ? (shared ? c.sVp[hk] : c.sV[unit]) : 1.0f, unitB = VI8 && !ALL ? c.sV[unit] : unitA;
+
+    const Lane<D, VI8> lo(lane);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]);
+    auto stage = [&](int t, int slot) {                          // (a tile past the last costs as many copies, of nothing)
+        const bool inA = t < tilesA;
+        const int j0 = 32 * (inA ? t : t - tilesA);
+        const bool real = t < t1;
+        copy_pieces<K_PIECES<D>>(pick(inA, rKA, rKB), kbuf + slot * KB, lo.gk, lo.gk, real ? j0 * D : NOTHING);
+        copy_pieces<V_PIECES<D, VI8>>(pick(inA, rVA, rVB), vbuf + slot * VB, lo.gv[0], lo.gv[1], real ? j0 * V_ROW<D, VI8> : NOTHING);
+        if (g == 0) lds_copy4(pick(inA, rSA, rSB), skbuf + slot * 128, 4 * r, real ? j0 * 4 : NOTHING);
+    };
+    const int first = t0 + wave;
+#pragma unroll
+    for (int s = 0; s < ST; ++s) stage(first + s * FEW_WAVES, s);
+
+    const long qrow = row_of(c, ALL, unit, row);
+    v4i qf[KS];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
+    const float sq2 = c.sQ[qrow] * LOG2E;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));    // landed before the loop
+    v16i bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
+    asm volatile("" : "+v"(bias));
+
+    float m2 = -INFINITY, l = 0.0f, unit_of_o = first < tilesA ? unitA : unitB;
+    v16f o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[dt][v] = 0.0f;
+    const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+
+    int slot = 0;
+    for (int t = first; t < t1; t += FEW_WAVES) {
+        wait_vmcnt<PER_TILE *(ST - 1)>();                        // this tile has landed
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        v4i kop[KS];
+        v4f skv[4];
+        h8 vop[DT][2];
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) kop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(kbuf + slot * KB, 32 * kk, lo.k0));
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) skv[vq] = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 128 + 16 * g + 32 * vq);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) vop[dt][s] = v_operand<D, VI8>(vbuf + slot * VB, lo.v0, dt, 16 * s);
+        wait_lds();
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        stage(t + ST * FEW_WAVES, slot);                         // into the place this tile has left
+        __builtin_amdgcn_sched_barrier(0);
+        slot = slot == ST - 1 ? 0 : slot + 1;
+
+        v16i acc = bias;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc, 0, 0, 0);
+        const bool inA = t < tilesA;
+        const int j0 = 32 * (inA ? t : t - tilesA);
+        float a[16], tmax = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) a[v] = (__int_as_float(acc[v]) - ACC_BIAS_F) * skv[v >> 2][v & 3];
+        // whether all 32 rows see all 32 keys (wave-uniform)
+        const bool clear = inA ? j0 + 32 <= runs.lenA && (shared || p0 >= 0)
+                               : p0 >= 0 && j0 + 31 <= p0 - runs.lo && (j0 > p1 - runs.lo - c.window || j0 + 31 < c.sinks - runs.lo);
+        if (!clear) {
+            const int hi = inA ? (shared || p >= 0 ? runs.lenA - 1 : -1) - j0 : p - runs.lo - j0;
+            const int from = inA ? 0 : p - runs.lo - c.window + 1 - j0, sink = inA ? 0 : c.sinks - runs.lo - j0;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int k = 8 * (v >> 2) + 4 * g + (v & 3);
+                if (k > hi || (k < from && k >= sink)) a[v] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) tmax = fmaxf(tmax, a[v]);
+        tmax = pair_max(tmax);
+        const float m_new = fmaxf(m2, tmax * sq2);
+        const float m_at = m_new == -INFINITY ? 0.0f : m_new;    // a row that has seen nothing yet: weights of 0, no NaN
+        float alpha = __builtin_amdgcn_exp2f(m2 - m_at);         // exp2(-inf) = 0
+        m2 = m_new;
+        h2 ph[8];
+        float psum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ph[e] = h2{(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[2 * e], sq2, -m_at)),
+                       (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[2 * e + 1], sq2, -m_at))};
+            psum = __builtin_amdgcn_fdot2(ph[e], ones, psum, false);
+        }
+        l = __builtin_fmaf(l, alpha, psum);
+        if (VI8 && !inA && t - FEW_WAVES < tilesA) {             // from the shared keys' scale of V to the own ones', once
+            alpha *= unit_of_o / unitB;
+            unit_of_o = unitB;
+        }
+        if (__any(alpha != 1.0f)) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const h8 pb = {ph[4 * s][0], ph[4 * s][1], ph[4 * s + 1][0], ph[4 * s + 1][1], ph[4 * s + 2][0], ph[4 * s + 2][1], ph[4 * s + 3][0], ph[4 * s + 3][1]};
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vop[dt][s], pb, o[dt], 0, 0, 0);
+        }
+    }
+    wait_all_memory();                                           // requests past the last tile
+    __syncthreads();                                             // every wavefront is done with its buffers: o may lie there
+
+    // ---- the four meet
+    l += swap32(l);
+    if (g == 0) sm.ml[wave][r] = float2{m2, l};
+    __syncthreads();
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) m_all = fmaxf(m_all, sm.ml[w][r].x);
+    const float f = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_all) * unit_of_o;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) {
+            // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
+            const int chunk = (8 * dt + 2 * vq + g) ^ (r & 7);
+            *reinterpret_cast<v4f *>(&sm.o[wave][r][4 * chunk]) = v4f{o[dt][4 * vq] * f, o[dt][4 * vq + 1] * f, o[dt][4 * vq + 2] * f, o[dt][4 * vq + 3] * f};
+        }
+    __syncthreads();
+    constexpr int TPR = D / 4;                                   // threads to a row
+    const int valid = last_row - row0 + 1;
+    for (int at = tid; at < valid * TPR; at += 64 * FEW_WAVES) {
+        const int rr = at / TPR, cc = at % TPR;
+        float m = -INFINITY, ls = 0.0f;
+        v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, sm.ml[w][rr].x);
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) {
+            const float2 x = sm.ml[w][rr];
+            ls += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - m);
+            s += *reinterpret_cast<const v4f *>(&sm.o[w][rr][4 * (cc ^ (rr & 7))]);
+        }
+        if (c.part_o) {
+            const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows + row0 + rr;
+            *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = s;
+            if (cc == 0) c.part_ml[pr] = float2{m, ls};
+        } else {
+            const float q = ls > 0.0f ? 1.0f / ls : 0.0f;        // a row that sees nothing: zeros
+            store4(c.O, c.o_dtype, row_of(c, ALL, unit, row0 + rr) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
+        }
+    }
+#endif
+}
+
+// ---- the parts of a row joined -----------------------------------------------------------------------------------
+// One row to D / 4 threads.  `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.
+struct Parts {
+    const float *o_shared, *o_own;
+    const float2 *ml_shared, *ml_own;
+    int shared, own;
+};
+template <int D>
+__global__ __launch_bounds__(256) void cache_attention_join_kernel(Call c, Parts parts, long all_rows) {
+    constexpr int TPR = D / 4;
+    const long idx = blockIdx.x * (256L / TPR) + threadIdx.x / TPR;
+    const int cc = threadIdx.x % TPR;
+    if (idx >= all_rows) return;
+    const int per = c.Nq * c.G, unit = static_cast<int>(idx / per), in = static_cast<int>(idx % per), b = unit / c.Hkv, hk = unit % c.Hkv;
+    const long s0 = static_cast<long>(hk) * parts.shared * c.B * per + static_cast<long>(b) * per + in, s_step = static_cast<long>(c.B) * per;
+    const long o0 = static_cast<long>(unit) * parts.own * per + in;
+    float m = -INFINITY;
+    for (int i = 0; i < parts.shared; ++i) m = fmaxf(m, parts.ml_shared[s0 + i * s_step].x);
+    for (int i = 0; i < parts.own; ++i) m = fmaxf(m, parts.ml_own[o0 + static_cast<long>(i) * per].x);
+    float l = 0.0f;
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](const float *po, const float2 *pml, long at) {
+        const float2 x = pml[at];
+        const float f = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);
+        const v4f y = *reinterpret_cast<const v4f *>(po + at * D + 4 * cc);
+        l += x.y * f;
+        s += y * f;
+    };
+    for (int i = 0; i < parts.shared; ++i) add(parts.o_shared, parts.ml_shared, s0 + i * s_step);
+    for (int i = 0; i < parts.own; ++i) add(parts.o_own, parts.ml_own, o0 + static_cast<long>(i) * per);
+    const float q = l > 0.0f ? 1.0f / l : 0.0f;
+    store4(c.O, c.o_dtype, row_of(c, false, unit, in) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+// How a call is carried out: in how many parts the shared keys and the own keys of a unit are taken, each part leaving 4 (d + 2) bytes a row.
+struct Plan {
+    int shared, own;                       // parts of the shared keys taken for the whole batch (0: every sequence reads them), and of the own keys
+    long rows_shared, rows_own;            // rows of parts: all units x parts x rows
+    bool join() const { return shared > 0 || own > 1; }
+    long bytes(int d) const { return join() ? (rows_shared + rows_own) * (4L * d + 8) + 512 : 0; }
+};
+constexpr int MOST_PARTS = 64;
+
+// parts so that about two workgroups a CU have work, of at least 256 keys each
+int parts_for(long groups, long keys) {
+    long parts = (512 + groups - 1) / groups;
+    if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
+    return static_cast<int>(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
+}
+
+Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sinks) {
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = (rows + 31) / 32;
+    Plan p = {};
+    const long span = static_cast<long>(window) + imin(Nq, 32) + sinks, keys = Nk < span ? Nk : span;
+    p.own = parts_for(units * tiles, keys);
+    if (Np > 0) {
+        const long all = rows * B, all_tiles = (all + 31) / 32;
+        p.shared = parts_for(Hkv * all_tiles, Np);
+        p.rows_shared = Hkv * all * p.shared;
+    }
+    p.rows_own = units * rows * p.own;
+    return p;
+}
+
+template <int D, bool VI8>
+int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
+    const int units = c.B * c.Hkv;
+    const int8_t *const Kp = c.Kp;
+    Parts parts = {};
+    float *o = nullptr;
+    float2 *ml = nullptr;
+    if (plan.join()) {
+        o = static_cast<float *>(workspace);
+        ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
+        parts = {o, o + plan.rows_shared * D, ml, ml + plan.rows_shared, plan.shared, plan.own};
+    }
+    auto few = [&](auto all, Call k, int n_units) {
+        const int row_tiles = (k.rows + 31) / 32;
+        const long grid = (static_cast<long>(n_units) * k.splits + 7) / 8 * 8 * row_tiles;
+        hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, n_units, row_tiles);
+    };
+    if (plan.shared > 0) {
+        Call k = c;
+        k.rows = c.rows * c.B;
+        k.splits = plan.shared;
+        k.part_o = o, k.part_ml = ml;
+        few(std::true_type{}, k, c.Hkv);
+        c.Kp = nullptr, c.Np = 0;                                // (the own keys alone from here on)
+    }
+    c.splits = plan.own;
+    if (plan.join()) c.part_o = o + plan.rows_shared * D, c.part_ml = ml + plan.rows_shared;
+    few(std::false_type{}, c, units);
+    if (plan.join()) {
+        c.Kp = Kp;
+        const long all_rows = static_cast<long>(units) * c.rows;
+        hipLaunchKernelGGL((cache_attention_join_kernel<D>), dim3(static_cast<unsigned>((all_rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, c, parts, all_rows);
+    }
+    return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
+}
+
+// The argument rules that both entry points share
+int refuse(const Call &c, int d, const void *workspace, long workspace_bytes, const Plan &plan) {
+    const bool prefix = c.Np > 0;
+    if (!c.Q || !c.K || !c.V || !c.sQ || !c.sK || !c.O || (prefix && (!c.Kp || !c.Vp || !c.sKp || !c.sVp != !c.sV))) return IFA_ERR_NULL;
+    if (c.o_dtype < IFA_F32 || c.o_dtype > IFA_BF16) return IFA_ERR_DTYPE;
+    for (const void *p : {static_cast<const void *>(c.Q), static_cast<const void *>(c.K), c.V, static_cast<const void *>(c.O), static_cast<const void *>(c.Kp), c.Vp})
+        if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(c.sQ), static_cast<const void *>(c.sK), static_cast<const void *>(c.sV), static_cast<const void *>(c.sKp), static_cast<const void *>(c.sVp), static_cast<const void *>(c.lens)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
+    if (plan.join()) {
+        if (!workspace) return IFA_ERR_NULL;
+        if (reinterpret_cast<uintptr_t>(workspace) & 255) return IFA_ERR_UNSUPPORTED;
+        if (workspace_bytes < plan.bytes(d)) return IFA_ERR_WORKSPACE;
+    }
+    return IFA_OK;
+}
+
+// Sizes alone: what a call or a workspace query takes
+int refuse_sizes(int B, int H, int Hkv, int Nq, int Np, int Nk, int d) {
+    if (B <= 0 || H <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || Np < 0 || d <= 0 || H % Hkv) return IFA_ERR_SHAPE;
+    const long heads = static_cast<long>(B) * H, N = Nq > Nk ? Nq : Nk;
+    if (heads > (1L << 40) / N / d) return IFA_ERR_SHAPE;
+    if (d != 64 && d != 128) return IFA_ERR_UNSUPPORTED;
+    if (static_cast<long>(Nk) * d * 2 > 0x7ff00000L || static_cast<long>(Np) * d * 2 > 0x7ff00000L) return IFA_ERR_UNSUPPORTED;
+    if (heads * Nq > 1L << 26 || heads > 1L << 23) return IFA_ERR_UNSUPPORTED;      // a launch has less than 2^32 threads: 256 to 32 rows or to a unit, d / 4 to a joined row
+    return IFA_OK;
+}
+
+int entry(const Call &c, int d, void *workspace, long workspace_bytes, void *hip_stream) {
+    const Plan plan = plan_of(c.B, c.Hkv, c.G, c.Nq, c.Np, c.Nk, c.window, c.sinks);
+    if (const int rc = refuse(c, d, workspace, workspace_bytes, plan)) return rc;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const bool i8 = c.sV != nullptr;
+    if (d == 128) return i8 ? launch<128, true>(c, plan, workspace, st) : launch<128, false>(c, plan, workspace, st);
+    return i8 ? launch<64, true>(c, plan, workspace, st) : launch<64, false>(c, plan, workspace, st);
+}
+
+}  // namespace
+
+extern "C" long ifa_window_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks) {
+    if (refuse_sizes(B, H, Hkv, Nq, 0, Nk, d) || window <= 0 || sinks < 0) return -1;
+    return plan_of(B, Hkv, H / Hkv, Nq, 0, Nk, imin(window, Nk), imin(sinks, Nk)).bytes(d);
+}
+
+extern "C" int int_flash_attn_fwd_window(const signed char *Q_i8, const signed char *K_i8, const void *V, const float *s_Q, const float *s_K,
+                                         const float *s_V, const int *lens, int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks,
+                                         void *O, int o_dtype, void *workspace, long workspace_bytes, void *hip_stream) {
+    if (window <= 0 || sinks < 0) return IFA_ERR_SHAPE;
+    if (const int rc = refuse_sizes(B, H, Hkv, Nq, 0, Nk, d)) return rc;
+    Call c = {};
+    c.Q = Q_i8, c.K = K_i8, c.V = V, c.sQ = s_Q, c.sK = s_K, c.sV = s_V, c.lens = lens;
+    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.window = imin(window, Nk), c.sinks = imin(sinks, Nk);
+    c.rows = c.G * Nq, c.O = O, c.o_dtype = o_dtype;
+    return entry(c, d, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" long ifa_prefix_workspace_bytes(int B, int H, int Hkv, int Nq, int Np, int Nk, int d) {
+    if (refuse_sizes(B, H, Hkv, Nq, Np, Nk, d) || Np <= 0) return -1;
+    return plan_of(B, Hkv, H / Hkv, Nq, Np, Nk, Nk, 0).bytes(d);
+}
+
+extern "C" int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8, const void *Vp, const signed char *K_i8, const void *V,
+                                         const float *s_Q, const float *s_Kp, const float *s_K, const float *s_Vp, const float *s_V, const int *lens,
+                                         int B, int H, int Hkv, int Nq, int Np, int Nk, int d, void *O, int o_dtype,
+                                         void *workspace, long workspace_bytes, void *hip_stream) {
+    if (Np <= 0) return IFA_ERR_SHAPE;
+    if (const int rc = refuse_sizes(B, H, Hkv, Nq, Np, Nk, d)) return rc;
+    Call c = {};
+    c.Q = Q_i8, c.K = K_i8, c.V = V, c.sQ = s_Q, c.sK = s_K, c.sV = s_V, c.Kp = Kp_i8, c.Vp = Vp, c.sKp = s_Kp, c.sVp = s_Vp, c.lens = lens;
+    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Np = Np, c.Nk = Nk, c.window = Nk, c.sinks = 0;
+    c.rows = c.G * Nq, c.O = O, c.o_dtype = o_dtype;
+    return entry(c, d, workspace, workspace_bytes, hip_stream);
+}

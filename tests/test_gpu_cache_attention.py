@@ -1,0 +1,161 @@
+"""Attention over a quantized cache (sliding window with sinks, shared prefix) against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import cache_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ifa():
+    import paper_2409_16997_amd as ifa
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return ifa
+
+
+def dev_lens(lens):
+    return None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+def window(ifa, s, w, sinks, lens=None, **kw):
+    t = ref.on_gpu(s)
+    return ifa.int_flash_attn_fwd_window(t["q8"], t["k8"], t["v"], t["sq"], t["sk"], w, sinks, s_V=t["sv"], lens=dev_lens(lens), **kw)
+
+
+def prefix(ifa, s, lens=None, **kw):
+    t = ref.on_gpu(s)
+    return ifa.int_flash_attn_fwd_prefix(t["q8"], t["kp8"], t["vp"], t["k8"], t["v"], t["sq"], t["skp"], t["sk"], s_Vp=t["svp"], s_V=t["sv"], lens=dev_lens(lens), **kw)
+
+
+def check(got, want, tol):
+    got = got.cpu().double()
+    off = (got - want).abs()
+    assert bool((off <= tol).all()), f"off by up to {(off / tol.clamp_min(1e-300)).max().item():.3f} of the tolerance"
+
+
+# B, Hkv, G, Nq, Nk, d, window, sinks, lens
+WINDOWS = [
+    (1, 1, 1, 1, 1, 64, 1, 0, None),                     # one key
+    (2, 3, 1, 1, 33, 128, 5, 0, None),
+    (2, 2, 4, 1, 300, 128, 64, 4, (300, 257)),           # a decode step, grouped heads
+    (1, 1, 8, 1, 5000, 128, 4096, 4, None),              # shared out over workgroups
+    (3, 2, 2, 1, 2500, 64, 2000, 100, (2500, 0, 1)),     # an empty sequence, one of one key
+    (1, 2, 3, 5, 700, 128, 100, 7, (650,)),              # draft tokens, an odd group
+    (1, 1, 7, 9, 1200, 64, 1000, 64, (1199,)),
+    (2, 1, 1, 40, 40, 128, 3, 2, (40, 17)),              # a prompt, padded in front
+    (1, 2, 1, 129, 129, 64, 1, 0, None),                 # every query sees itself alone
+    (1, 1, 2, 130, 257, 128, 64, 64, None),              # a chunk; sinks as many as the window
+    (1, 1, 4, 200, 200, 64, 500, 3, None),               # a window beyond the sequence: causal attention
+    (2, 1, 1, 31, 95, 128, 32, 300, (95, 20)),           # more sinks than keys: causal attention
+    (1, 3, 1, 300, 300, 128, 129, 1, (290,)),
+    (4, 1, 1, 2, 4, 64, 2, 1, (4, 3, 2, 1)),
+    (1, 1, 1, 700, 700, 128, 256, 4, None),
+    (9, 1, 5, 3, 64, 64, 7, 1, (64, 0, 1, 2, 3, 4, 31, 32, 33)),
+]
+
+
+@pytest.mark.parametrize("v,out", [("fp16", torch.float32), ("int8", torch.float16), ("fp16", torch.bfloat16)])
+@pytest.mark.parametrize("case", WINDOWS, ids=[f"{i}" for i in range(len(WINDOWS))])
+def test_window(ifa, case, v, out):
+    B, Hkv, G, Nq, Nk, d, w, sinks, lens = case
+    s = ref.problem(7, B, Hkv, G, Nq, Nk, d, v=v)
+    want, tol = ref.attention(s, out, lens, w, sinks)
+    check(window(ifa, s, w, sinks, lens, out_dtype=out), want, tol)
+
+
+# B, Hkv, G, Nq, Np, Nk, d, lens
+PREFIXES = [
+    (1, 1, 1, 1, 1, 1, 64, None),
+    (2, 2, 1, 1, 300, 40, 64, None),
+    (3, 1, 4, 1, 33, 65, 128, (65, 0, 1)),               # nothing of its own, one key of its own
+    (5, 2, 3, 2, 700, 100, 128, (100, 1, 99, 33, 0)),    # an odd group; a query in front of its own keys
+    (40, 1, 4, 1, 2000, 200, 64, None),                  # more rows than a tile
+    (1, 1, 8, 1, 5000, 3000, 128, (2999,)),
+    (2, 1, 2, 70, 500, 300, 128, (300, 50)),             # more queries than own keys
+    (7, 1, 1, 3, 32, 32, 64, (0, 1, 2, 3, 4, 31, 32)),
+    (33, 2, 1, 1, 1500, 9, 128, None),
+]
+
+
+@pytest.mark.parametrize("v,out", [("fp16", torch.float32), ("int8", torch.float16), ("int8", torch.bfloat16)])
+@pytest.mark.parametrize("case", PREFIXES, ids=[f"{i}" for i in range(len(PREFIXES))])
+def test_prefix(ifa, case, v, out):
+    B, Hkv, G, Nq, Np, Nk, d, lens = case
+    s = ref.problem(8, B, Hkv, G, Nq, Nk, d, Np=Np, v=v)
+    want, tol = ref.attention(s, out, lens)
+    check(prefix(ifa, s, lens, out_dtype=out), want, tol)
+
+
+def test_what_no_query_sees_is_not_looked_at(ifa):
+    """Decode steps: NaN and infinities behind L_b and in front of the window, in V and in the scales of K."""
+    for d, G, L, w, sinks in ((128, 4, 900, 200, 5), (64, 1, 40, 7, 0), (128, 1, 3000, 1111, 33)):
+        Nk = L + 50
+        s = ref.problem(3, 1, 2, G, 1, Nk, d)
+        clean, tol = ref.attention(s, torch.float16, (L,), w, sinks)
+        hidden = torch.ones(Nk, dtype=torch.bool)
+        hidden[:sinks] = False
+        hidden[L - w:L] = False
+        for bad in (math.nan, math.inf, -65504.0):
+            s["v"][:, :, hidden] = bad
+            s["sk"][:, :, hidden] = bad
+            check(window(ifa, s, w, sinks, (L,)), clean, tol)
+
+
+def test_lengths_outside_the_buffer_count_as_the_nearer_end(ifa):
+    s = ref.problem(4, 3, 1, 2, 2, 50, 64)
+    a, b = window(ifa, s, 20, 2, (50, 0, 17)), window(ifa, s, 20, 2, (10 ** 9, -5, 17))
+    assert torch.equal(a, b) and bool((a[1] == 0).all())
+
+
+def test_out_workspace_and_stream(ifa):
+    s = ref.problem(5, 1, 1, 4, 1, 6000, 128)
+    t = ref.on_gpu(s)
+    need = ifa.window_workspace_bytes(1, 4, 1, 1, 6000, 128, 5000, 4)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out = torch.full((3, 1, 4, 1, 128), 7.0, dtype=torch.float32, device="cuda")
+    want = window(ifa, s, 5000, 4, out_dtype=torch.float32)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = ifa.int_flash_attn_fwd_window(t["q8"], t["k8"], t["v"], t["sq"], t["sk"], 5000, 4, out=out[1], workspace=ws)
+    side.synchronize()
+    assert got.data_ptr() == out[1].data_ptr() and torch.equal(out[1], want) and bool((out[0] == 7).all()) and bool((out[2] == 7).all())
+
+
+def test_graph_replays(ifa):
+    """Both calls in one captured graph, inputs changed between replays; every replay against the eager call."""
+    s, lens = ref.problem(6, 3, 2, 4, 1, 1500, 128, Np=2500), (1500, 3, 700)
+    t, ln = ref.on_gpu(s), dev_lens(lens)
+
+    def both():
+        return (ifa.int_flash_attn_fwd_window(t["q8"], t["k8"], t["v"], t["sq"], t["sk"], 1000, 4, lens=ln),
+                ifa.int_flash_attn_fwd_prefix(t["q8"], t["kp8"], t["vp"], t["k8"], t["v"], t["sq"], t["skp"], t["sk"], lens=ln))
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = both()
+    for k in range(3):
+        t["q8"].copy_(torch.roll(t["q8"], 1, -1))
+        ln.copy_(torch.tensor([1500 - 7 * k, 3 + k, 0], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, eager))
+
+
+def test_a_prefix_of_one_sequence_is_plain_attention(ifa):
+    """Shared keys in front of own ones are the same keys in one buffer; a window beyond it hides nothing."""
+    s = ref.problem(9, 1, 2, 2, 6, 200, 64, Np=320)
+    whole = {"q8": s["q8"], "sq": s["sq"], "k8": torch.cat([s["kp8"][None], s["k8"]], 2), "sk": torch.cat([s["skp"][None], s["sk"]], 2),
+             "v": torch.cat([s["vp"][None], s["v"]], 2), "sv": None}
+    want, tol = ref.attention(whole, torch.float32, None, 10 ** 6)
+    check(prefix(ifa, s, out_dtype=torch.float32), want, tol)
+    check(window(ifa, whole, 10 ** 6, 0, out_dtype=torch.float32), want, tol)
