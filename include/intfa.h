@@ -295,6 +295,30 @@ int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8,
                               int B, int H, int Hkv, int Nq, int Np, int Nk, int d, void *O, int o_dtype,
                               void *workspace, long workspace_bytes, void *hip_stream);
 
+/*
+ * The softmax weight that each own key draws, added up over the queries and over the heads of its group -- what an eviction goes by:
+ *   W_out[b, hk, j] = W[b, hk, j] + sum over i and over the heads h of group hk of exp(S_ij) / sum_j' exp(S_ij'),   j' over the keys that query i sees (j' <= p)
+ * in fp32 (the weights are not rounded to fp16).  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W.
+ *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
+ * row and key where a key head has up to 16 query rows, else 4 a key and slice of the rows.
+ */
+long ifa_key_weights_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d);
+
+int key_weights(const signed char *Q_i8, const signed char *K_i8, const float *s_Q, const float *s_K, const int *lens, const float *W,
+                int B, int H, int Hkv, int Nq, int Nk, int d, float *W_out, void *workspace, long workspace_bytes, void *hip_stream);
+
+/*
+ * The cache cut down to `keep` keys per key head: of the L_b keys of a sequence the first `sinks`, the last `recent` and, between them, those of the largest
+ * W (of equal ones the first; a NaN is below everything) stay, in their order; with L_b <= keep all do.
+ *   K_out [B, Hkv, keep, d], s_K_out, W_out [B, Hkv, keep], V_out [B, Hkv, keep, d] (V of v_bytes = 1 or 2 bytes an element): the rows that stay, then zeros
+ *   index [B, Hkv, keep] int32: which key each was, then -1;  lens_out [B] int32: min(L_b, keep)
+ * s_V of an INT8 V stays as it is.  1 <= keep <= Nk, sinks + recent <= keep; d a multiple of 16 up to 1024.  Nothing is evicted in place: outputs that overlap an input or each
+ * other are refused (IFA_ERR_UNSUPPORTED).  Two launches, no workspace.
+ */
+int evict_keys(const signed char *K_i8, const float *s_K, const void *V, int v_bytes, const float *W, const int *lens,
+               int B, int Hkv, int Nk, int d, int keep, int recent, int sinks,
+               signed char *K_out, float *s_K_out, void *V_out, float *W_out, int *index, int *lens_out, void *hip_stream);
+
 /* Key-block size of the half-INT8 kernel for (d, causal); 0 if that pair is unsupported. */
 int ifa_block_cols_half(int d, int causal);
 

@@ -41,6 +41,9 @@ SIGNATURES = {
     "int_flash_attn_fwd_window": (_i, [_vp] * 7 + [_i] * 8 + [_vp, _i, _vp, _l, _vp]),
     "ifa_prefix_workspace_bytes": (_l, [_i] * 7),
     "int_flash_attn_fwd_prefix": (_i, [_vp] * 11 + [_i] * 7 + [_vp, _i, _vp, _l, _vp]),
+    "ifa_key_weights_workspace_bytes": (_l, [_i] * 6),
+    "key_weights": (_i, [_vp] * 6 + [_i] * 6 + [_vp, _vp, _l, _vp]),
+    "evict_keys": (_i, [_vp] * 3 + [_i] + [_vp] * 2 + [_i] * 7 + [_vp] * 7),
     "ifa_block_cols_half": (_i, [_i, _i]),
     "ifa_debug_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
@@ -469,6 +472,58 @@ def int_flash_attn_fwd_prefix(Q_i8, Kp_i8, Vp, K_i8, V, s_Q, s_Kp, s_K, s_Vp=Non
     _check(lib().int_flash_attn_fwd_prefix(q, kp, vp, k, v, sq, skp, sk, svp, sv, ln, B, H, Hkv, Nq, Np, Nk, d, out.data_ptr(), _dtype_enum(out), ws, n, _stream()),
            "int_flash_attn_fwd_prefix")
     return out
+
+
+def key_weights_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: int) -> int:
+    """Bytes of workspace key_weights needs for this shape (-1: sizes that it refuses)."""
+    return int(lib().ifa_key_weights_workspace_bytes(int(B), int(H), int(Hkv), int(Nq), int(Nk), int(d)))
+
+
+def key_weights(Q_i8, K_i8, s_Q, s_K, W=None, lens=None, out=None, workspace=None):
+    """The softmax weight that each key of a cache draws, summed over the queries and the heads of its group, added to W [B, Hkv, Nk]
+    (None: zeros): fp32 [B, Hkv, Nk], into `out` if given (which may be W).  int8 Q [B, H, Nq, d], K [B, Hkv, Nk, d] with token-level scales; the queries
+    are the last Nq positions of the lens[b] keys of their sequence and see the keys up to their own."""
+    import torch
+    B, H, Hkv, Nq, Nk, d = _cache_sizes(Q_i8, K_i8)
+    dev = torch.cuda.current_device()
+    i8, f32, wshape = (torch.int8,), (torch.float32,), (B, Hkv, Nk)
+    at = (_operand(Q_i8, "Q_i8", i8, (B, H, Nq, d), dev), _operand(K_i8, "K_i8", i8, (B, Hkv, Nk, d), dev), _operand(s_Q, "s_Q", f32, (B, H, Nq), dev),
+          _operand(s_K, "s_K", f32, wshape, dev), None if lens is None else _operand(lens, "lens", (torch.int32,), (B,), dev),
+          None if W is None else _operand(W, "W", f32, wshape, dev))
+    if out is None:
+        out = _scales(K_i8, wshape)
+    ws, n, _keep = _workspace(workspace, key_weights_workspace_bytes(B, H, Hkv, Nq, Nk, d), dev)
+    _check(lib().key_weights(*at, B, H, Hkv, Nq, Nk, d, _operand(out, "out", f32, wshape, dev), ws, n, _stream()), "key_weights")
+    return out
+
+
+def evict_keys(K_i8, s_K, V, W, keep, recent=0, sinks=0, lens=None, out=None):
+    """The cache K_i8, V [B, Hkv, Nk, d] (V fp16 or int8), s_K, W [B, Hkv, Nk] cut down to `keep` keys a head: the first `sinks` of the lens[b]
+    keys, the last `recent` and those of the largest W between them (of equal ones the first), in their order.  Returns (K_i8, s_K, V, W
+    [B, Hkv, keep, ...], index [B, Hkv, keep] int32, lens [B] int32); past min(lens[b], keep) keys index is -1 and the rest zero.
+    out: optional tuple of those six tensors to write into, which overlap neither the inputs nor each other."""
+    import torch
+    if getattr(K_i8, "dim", int)() != 4 or K_i8.numel() == 0:
+        raise IntfaError("K is [B, Hkv, Nk, d] and not empty")
+    B, Hkv, Nk, d = K_i8.shape
+    dev = torch.cuda.current_device()
+    i8, f32, i32 = (torch.int8,), (torch.float32,), (torch.int32,)
+    keep, recent, sinks = int(keep), int(recent), int(sinks)
+    if not (1 <= keep <= Nk and recent >= 0 and sinks >= 0 and recent + sinks <= keep):
+        raise IntfaError(f"keep {keep} of {Nk} keys, {sinks} sinks and {recent} recent ones: 1 <= keep <= Nk, sinks + recent <= keep")
+    at = [_operand(K_i8, "K_i8", i8, (B, Hkv, Nk, d), dev), _operand(s_K, "s_K", f32, (B, Hkv, Nk), dev),
+          _operand(V, "V", (torch.int8, torch.float16), (B, Hkv, Nk, d), dev), _operand(W, "W", f32, (B, Hkv, Nk), dev)]
+    ln = None if lens is None else _operand(lens, "lens", i32, (B,), dev)
+    rows = (B, Hkv, keep)
+    if out is None:
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=K_i8.device)  # noqa: E731
+        out = (new(rows + (d,), torch.int8), new(rows, torch.float32), new(rows + (d,), V.dtype), new(rows, torch.float32), new(rows, torch.int32), new((B,), torch.int32))
+    elif len(out) != 6:
+        raise IntfaError("out: K_i8, s_K, V, W, index, lens")
+    to = [_operand(x, f"out[{i}]", (t,), s, dev) for i, (x, t, s) in enumerate(zip(out, (torch.int8, torch.float32, V.dtype, torch.float32, torch.int32, torch.int32),
+                                                                                  (rows + (d,), rows, rows + (d,), rows, rows, (B,))))]
+    _check(lib().evict_keys(at[0], at[1], at[2], V.element_size(), at[3], ln, B, Hkv, Nk, d, keep, recent, sinks, *to, _stream()), "evict_keys")
+    return tuple(out)
 
 
 def debug_fwd(Q_i8, K_i8, V_i8, s_Q, s_K, s_V, causal=False, P_in=None, fill=-1):

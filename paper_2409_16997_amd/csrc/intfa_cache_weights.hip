@@ -1,0 +1,536 @@
+// What an eviction from a quantized cache goes by, and the eviction, for gfx950.
+//
+// key_weights: W_j (+)= sum over the queries i and the heads of a group of P_ij = exp(S_ij - m_i) / l_i, S as in the attention calls.  A weight needs m and l of its
+// whole row, so the scores are gone through twice.  With few rows to a key head (a decode step) the first pass leaves the scores in the workspace and K is read once;
+// with many (a prompt) the second computes them again, now a key to a lane: 32x32 accumulators of Q K^T hold 16 queries of one key each, whose weights a lane adds up by itself.
+// All sums are in a fixed order (no atomics on floating point values): equal calls give equal results.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "intfa.h"
+#include "intfa_internal.h"
+#include "intfa_device.h"
+#include "intfa_cache.h"
+
+namespace {
+
+using namespace ifa_cache;
+
+struct WeightsCall {
+    const int8_t *Q, *K;
+    const float *sQ, *sK, *W;                                    // W null: zeros
+    const int *lens;
+    int B, Hkv, G, Nq, Nk;
+    int parts;                                                   // of the keys, in the first pass
+    int slices;                                                  // of the rows, in the second
+    float2 *stats;                                               // [part][B H Nq]: maximum (log2 units) and sum of a row over that part; then part 0: maximum, 1 / sum
+    float *scores;                                               // [unit][rows][score_stride] in log2 units, or null
+    long score_stride;
+    float *sums;                                                 // [slice][unit][Nk], or null: straight to out
+    float *out;
+};
+__device__ __forceinline__ long query_row(const WeightsCall &c, int unit, int row) {             // row (i, g) of unit (b, hk), in the order of Q
+    return (static_cast<long>(unit) * c.G + row % c.G) * c.Nq + row / c.G;
+}
+
+// ---- first pass: maximum and sum of 32 rows over a part of the keys, the wavefronts taking every fourth tile of 32 keys, each for itself -----------------
+constexpr int KW_WAVES = 4, KW_ST = 4;
+template <int D> struct SmemRows {
+    alignas(4096) int8_t k[KW_WAVES][KW_ST][32 * D];
+    alignas(128) float sk[KW_WAVES][KW_ST][32];
+    float2 ml[KW_WAVES][32];
+};
+
+template <int D>
+__global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(WeightsCall c, int units, int row_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemRows<D> sm;
+    constexpr int KS = D / 32, KB = 32 * D, PER_TILE = K_PIECES<D> + 1;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), rt = in8 >> 3;
+    const int unit = share / c.parts, part = share % c.parts;
+    if (unit >= units) return;
+    const int rows = c.G * c.Nq, row0 = 32 * rt, last_row = imin(row0 + 31, rows - 1), row = imin(row0 + r, rows - 1);
+    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
+    const int p0 = L - c.Nq + row0 / c.G, p1 = L - c.Nq + last_row / c.G, p = L - c.Nq + row / c.G;
+    const int keys = imax(0, p1 + 1);                            // that any of the rows sees
+    const int tiles = (keys + 31) / 32, per = (tiles + c.parts - 1) / c.parts, t0 = part * per, t1 = imin(tiles, t0 + per);
+    const BufRsrc rK = make_rsrc(c.K + static_cast<long>(unit) * c.Nk * D, keys * D), rS = make_rsrc(c.sK + static_cast<long>(unit) * c.Nk, keys * 4);
+
+    const Lane<D, true> lo(lane);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]);
+    auto stage = [&](int t, int slot) {
+        copy_pieces<K_PIECES<D>>(rK, kbuf + slot * KB, lo.gk, lo.gk, t < t1 ? 32 * t * D : NOTHING);
+        if (g == 0) lds_copy4(rS, skbuf + slot * 128, 4 * r, t < t1 ? 128 * t : NOTHING);
+    };
+    const int first = t0 + wave;
+#pragma unroll
+    for (int s = 0; s < KW_ST; ++s) stage(first + s * KW_WAVES, s);
+    const long qrow = query_row(c, unit, row);
+    v4i qf[KS];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
+    const float sq2 = c.sQ[qrow] * LOG2E;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));
+    v16i bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
+    asm volatile("" : "+v"(bias));
+
+    float m2 = -INFINITY, l = 0.0f;
+    float *const scores = c.scores ? c.scores + (static_cast<long>(unit) * rows + row0 + r) * c.score_stride + 4 * g : nullptr;
+    int slot = 0;
+    for (int t = first; t < t1; t += KW_WAVES) {
+        // (a stored score counts with the copies: no more of them than KW_ST - 1 tiles have can be behind this tile's)
+        wait_vmcnt<PER_TILE *(KW_ST - 1)>();
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        v4i kop[KS];
+        v4f skv[4];
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) kop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(kbuf + slot * KB, 32 * kk, lo.k0));
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) skv[vq] = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 128 + 16 * g + 32 * vq);
+        wait_lds();
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        v16i acc = bias;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc, 0, 0, 0);
+        float x[16], tmax = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = (__int_as_float(acc[v]) - ACC_BIAS_F) * skv[v >> 2][v & 3] * sq2;
+        if (32 * t + 31 > p0) {                                  // (wave-uniform) a row that does not see the whole tile
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (32 * t + 8 * (v >> 2) + 4 * g + (v & 3) > p) x[v] = -INFINITY;
+        }
+        if (scores && row0 + r < rows) {                         // (rows of whole tiles of 32: the last one is stored past the keys)
+#pragma unroll
+            for (int vq = 0; vq < 4; ++vq) *reinterpret_cast<v4f *>(scores + 32 * t + 8 * vq) = v4f{x[4 * vq], x[4 * vq + 1], x[4 * vq + 2], x[4 * vq + 3]};
+        }
+        stage(t + KW_ST * KW_WAVES, slot);                       // behind the scores, so that the wait above counts only copies that are younger than its tile
+        __builtin_amdgcn_sched_barrier(0);
+        slot = slot == KW_ST - 1 ? 0 : slot + 1;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) tmax = fmaxf(tmax, x[v]);
+        tmax = pair_max(tmax);
+        const float m_new = fmaxf(m2, tmax), m_at = m_new == -INFINITY ? 0.0f : m_new;
+        float s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s += __builtin_amdgcn_exp2f(x[v] - m_at);
+        l = __builtin_fmaf(l, __builtin_amdgcn_exp2f(m2 - m_at), s);
+        m2 = m_new;
+    }
+    wait_all_memory();
+    l += swap32(l);
+    if (g == 0) sm.ml[wave][r] = float2{m2, l};
+    __syncthreads();
+    if (tid < 32 && row0 + tid < rows) {
+        float m = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < KW_WAVES; ++w) m = fmaxf(m, sm.ml[w][tid].x);
+#pragma unroll
+        for (int w = 0; w < KW_WAVES; ++w)
+            if (sm.ml[w][tid].x != -INFINITY) sum += sm.ml[w][tid].y * __builtin_amdgcn_exp2f(sm.ml[w][tid].x - m);
+        const long at = static_cast<long>(units) * rows * part + query_row(c, unit, row0 + tid);
+        c.stats[at] = float2{m, sum};
+    }
+#endif
+}
+
+// maximum and 1 / sum of a row from its parts; a row that sees nothing: 0 and 0, so that its weights are 0
+__device__ __forceinline__ float2 join_parts(const float2 *stats, long at, long step, int parts) {
+    float m = -INFINITY, sum = 0.0f;
+    for (int i = 0; i < parts; ++i) m = fmaxf(m, stats[at + i * step].x);
+    if (m == -INFINITY) return float2{0.0f, 0.0f};
+    for (int i = 0; i < parts; ++i) {
+        const float2 x = stats[at + i * step];
+        if (x.x != -INFINITY) sum += x.y * __builtin_amdgcn_exp2f(x.x - m);
+    }
+    return float2{m, 1.0f / sum};
+}
+__global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, long rows) {
+    const long at = blockIdx.x * 256L + threadIdx.x;
+    if (at < rows) c.stats[at] = join_parts(c.stats, at, rows, c.parts);
+}
+
+// ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
+constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128)
+__global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, int units, int blocks) {
+    __shared__ float2 st[STORED_ROWS];
+    const int unit = blockIdx.x / blocks, j = (blockIdx.x % blocks * 256 + threadIdx.x) * 4, rows = c.G * c.Nq;
+    const int L = c.lens ? imax(0, imin(c.lens[unit / c.Hkv], c.Nk)) : c.Nk;
+    if (static_cast<int>(threadIdx.x) < rows)
+        st[threadIdx.x] = join_parts(c.stats, query_row(c, unit, threadIdx.x), static_cast<long>(units) * rows, c.parts);
+    __syncthreads();
+    if (j >= c.Nk) return;
+    v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (j < L) {
+        const float *x = c.scores + static_cast<long>(unit) * rows * c.score_stride + j;
+        for (int r = 0; r < rows; ++r) {
+            const float2 s = st[r];
+            // Tiles of 32 keys are stored up to the last that a row sees, and its scores are -inf behind what it sees.
+            const v4f y = *reinterpret_cast<const v4f *>(x + r * c.score_stride);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(y[e] - s.x), s.y, w[e]);
+        }
+    }
+    const long at = static_cast<long>(unit) * c.Nk + j;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (j + e < c.Nk) c.out[at + e] = (j + e < L ? w[e] : 0.0f) + (c.W ? c.W[at + e] : 0.0f);
+}
+
+// ---- second pass, scores computed again: 128 keys to a workgroup, a key to a lane ---------------------------------------------------------------
+// The rows go by in tiles of 64 queries of one head through LDS, shared by the four wavefronts of 32 keys; a slice of them per workgroup.
+constexpr int KW_ROWS = 64;
+template <int D> struct SmemKeys {
+    alignas(4096) int8_t q[2][KW_ROWS * D];
+    alignas(256) float sq[2][KW_ROWS];
+    alignas(256) float2 ml[2][KW_ROWS];
+};
+template <int D>
+__global__ __launch_bounds__(256) void key_weights_keys_kernel(WeightsCall c, int units, int key_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemKeys<D> sm;
+    constexpr int KS = D / 32, PIECES = KW_ROWS * D / 4096;      // copies of a wavefront to a tile
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kt = blockIdx.x % key_tiles, us = blockIdx.x / key_tiles, unit = us / c.slices, slice = us % c.slices;     // (the first keys, which most rows see, start first)
+    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
+    const int j0 = 128 * kt, j = j0 + 32 * wave + r, shift = L - c.Nq;
+    const int i0 = imax(0, j0 - shift);                          // the first query that sees any of the keys
+    const int per_head = j0 < L && i0 < c.Nq ? (c.Nq - i0 + KW_ROWS - 1) / KW_ROWS : 0, total = per_head * c.G;
+    const int per = (total + c.slices - 1) / c.slices, t0 = slice * per, t1 = imin(total, t0 + per);
+    float sum = 0.0f;
+    if (t0 < t1) {
+        const long kb = static_cast<long>(unit) * c.Nk;
+        v4i kop[KS];                                             // (keys at or beyond L: zeros, left out at the end)
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+            v4i x = {0, 0, 0, 0};
+            if (j < L) x = *reinterpret_cast<const v4i *>(c.K + (kb + j) * D + 32 * kk + 16 * g);
+            kop[kk] = x;
+        }
+        const float sk = j < L ? c.sK[kb + j] : 0.0f;
+        const Lane<D, true> lo(lane);
+        const lds_ptr qbuf = (lds_ptr)(&sm.q[0][0]), sqbuf = (lds_ptr)(&sm.sq[0][0]), mlbuf = (lds_ptr)(&sm.ml[0][0]);
+        auto stage = [&](int t, int slot) {
+            const int head = t / per_head, i = i0 + t % per_head * KW_ROWS;
+            const long row = (static_cast<long>(unit) * c.G + head) * c.Nq + i;
+            const int rows = c.Nq - i;                           // (more than a tile is no harm: the copy has 64)
+            const BufRsrc rQ = make_rsrc(c.Q + row * D, imin(rows, KW_ROWS) * D), rS = make_rsrc(c.sQ + row, imin(rows, KW_ROWS) * 4),
+                          rM = make_rsrc(c.stats + row, imin(rows, KW_ROWS) * 8);
+            copy_pieces<PIECES>(rQ, qbuf + slot * (KW_ROWS * D) + wave * PIECES * 1024, lo.gk, lo.gk, wave * PIECES * 1024);
+            if (wave == 0) lds_copy4(rS, sqbuf + slot * 256, 4 * lane, 0);
+            if (wave == 1) lds_copy4(rM, mlbuf + slot * 512, 4 * lane, 0);
+            if (wave == 2) lds_copy4(rM, mlbuf + slot * 512 + 256, 4 * lane, 256);
+        };
+        v16i bias;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
+        asm volatile("" : "+v"(bias));
+        stage(t0, 0);
+        wait_all_memory();
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int slot = (t - t0) & 1;
+            if (t + 1 < t1) stage(t + 1, slot ^ 1);
+            const int i = i0 + t % per_head * KW_ROWS;
+            const bool masked = shift + i < j0 + 127 || i + KW_ROWS > c.Nq;      // a query that does not see all of the keys, or none there
+#pragma unroll
+            for (int h = 0; h < KW_ROWS / 32; ++h) {
+                v4i qop[KS];
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) qop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(qbuf + slot * (KW_ROWS * D), 32 * kk, lo.k0) + 32 * h * D);
+                v16i acc = bias;
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(qop[kk], kop[kk], acc, 0, 0, 0);
+#pragma unroll
+                for (int vq = 0; vq < 4; ++vq) {
+                    const v4f sq = *reinterpret_cast<LDS_AS const v4f *>(sqbuf + slot * 256 + 128 * h + 32 * vq + 16 * g);
+                    const v4f ma = *reinterpret_cast<LDS_AS const v4f *>(mlbuf + slot * 512 + 256 * h + 64 * vq + 32 * g);
+                    const v4f mb = *reinterpret_cast<LDS_AS const v4f *>(mlbuf + slot * 512 + 256 * h + 64 * vq + 32 * g + 16);
+                    const float m[4] = {ma[0], ma[2], mb[0], mb[2]}, rl[4] = {ma[1], ma[3], mb[1], mb[3]};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float x = __builtin_fmaf((__int_as_float(acc[4 * vq + e]) - ACC_BIAS_F) * sk, sq[e] * LOG2E, -m[e]);
+                        const int q = i + 32 * h + 8 * vq + 4 * g + e;
+                        if (masked && (q + shift < j || q >= c.Nq)) x = -INFINITY;
+                        sum = __builtin_fmaf(__builtin_amdgcn_exp2f(x), rl[e], sum);
+                    }
+                }
+            }
+            wait_all_memory();
+            __syncthreads();
+        }
+    }
+    sum += swap32(sum);
+    if (g == 0 && j < c.Nk) {
+        const long at = static_cast<long>(unit) * c.Nk + j;
+        if (j >= L) sum = 0.0f;
+        if (c.sums) c.sums[static_cast<long>(slice) * units * c.Nk + at] = sum;
+        else c.out[at] = sum + (c.W ? c.W[at] : 0.0f);
+    }
+#endif
+}
+__global__ __launch_bounds__(256) void key_weights_add_kernel(WeightsCall c, long n) {
+    const long at = blockIdx.x * 256L + threadIdx.x;
+    if (at >= n) return;
+    float s = 0.0f;
+    for (int i = 0; i < c.slices; ++i) s += c.sums[i * n + at];
+    c.out[at] = s + (c.W ? c.W[at] : 0.0f);
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+struct Plan {
+    int parts, slices;
+    bool stored;
+    long stats, scores, sums;              // bytes
+    long stride;                           // of a row of scores
+    long bytes() const { return stats + scores + sums; }
+};
+long up(long n) { return (n + 255) / 256 * 256; }
+Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = (rows + 31) / 32;
+    Plan p = {};
+    long parts = (1024 + units * tiles - 1) / (units * tiles);
+    if (parts > (Nk + 511) / 512) parts = (Nk + 511) / 512;
+    p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    p.stats = up(units * rows * p.parts * 8);
+    p.stored = rows <= STORED_ROWS;
+    p.stride = (Nk + 31L) / 32 * 32;
+    if (p.stored) {
+        p.scores = up(units * rows * p.stride * 4);
+        p.slices = 1;
+    } else {
+        const long groups = units * ((Nk + 127) / 128), most = G * ((Nq + KW_ROWS - 1L) / KW_ROWS);
+        long slices = (1024 + groups - 1) / groups;
+        if (slices > most) slices = most;
+        p.slices = static_cast<int>(slices < 1 ? 1 : slices > 64 ? 64 : slices);
+        p.sums = p.slices > 1 ? up(units * Nk * 4L * p.slices) : 0;
+    }
+    return p;
+}
+
+template <int D> int launch(WeightsCall c, const Plan &plan, hipStream_t st) {
+    const int units = c.B * c.Hkv, row_tiles = (c.G * c.Nq + 31) / 32;
+    const long rows = static_cast<long>(units) * c.G * c.Nq;
+    const long grid = (static_cast<long>(units) * c.parts + 7) / 8 * 8 * row_tiles;
+    hipLaunchKernelGGL((key_weights_rows_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+    if (plan.stored) {
+        const int blocks = (c.Nk + 1023) / 1024;
+        hipLaunchKernelGGL(key_weights_stored_kernel, dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, units, blocks);
+    } else {
+        hipLaunchKernelGGL(key_weights_join_kernel, dim3(static_cast<unsigned>((rows + 255) / 256)), dim3(256), 0, st, c, rows);
+        const int key_tiles = (c.Nk + 127) / 128;
+        hipLaunchKernelGGL((key_weights_keys_kernel<D>), dim3(static_cast<unsigned>(key_tiles) * units * c.slices), dim3(256), 0, st, c, units, key_tiles);
+        if (c.sums) {
+            const long n = static_cast<long>(units) * c.Nk;
+            hipLaunchKernelGGL(key_weights_add_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, c, n);
+        }
+    }
+    return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
+}
+
+int refuse_sizes(int B, int H, int Hkv, int Nq, int Nk, int d) {
+    if (B <= 0 || H <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || d <= 0 || H % Hkv) return IFA_ERR_SHAPE;
+    const long heads = static_cast<long>(B) * H, N = Nq > Nk ? Nq : Nk;
+    if (heads > (1L << 40) / N / d) return IFA_ERR_SHAPE;
+    if (d != 64 && d != 128) return IFA_ERR_UNSUPPORTED;
+    if (static_cast<long>(Nk) * d * 2 > 0x7ff00000L || heads * Nq > 1L << 26 || heads > 1L << 23) return IFA_ERR_UNSUPPORTED;
+    if (static_cast<long>(B) * Hkv * Nk > 1L << 30) return IFA_ERR_UNSUPPORTED;      // (a launch has less than 2^32 threads: two to a key)
+    return IFA_OK;
+}
+
+// ---- eviction -----------------------------------------------------------------------------------------------------
+// One workgroup to a key head finds the weight of the last key that stays (radix selection, 11 bits at a time, over keys that are read from the caches again
+// each time) and writes the list of those that do, in order; a second launch moves the rows.
+struct EvictCall {
+    const int8_t *K, *V;
+    const float *sK, *W;
+    const int *lens;
+    int B, Hkv, Nk, d, v_row, keep, recent, sinks;               // v_row: bytes of a row of V
+    int8_t *K_out, *V_out;
+    float *sK_out, *W_out;
+    int *index, *lens_out;
+};
+constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64, BINS = 2048;
+
+// Larger weight, larger number; -0 is 0, a NaN is below everything
+__device__ __forceinline__ uint32_t order_of(float w) {
+    if (w != w) return 0;
+    const uint32_t u = __float_as_uint(w + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) {
+    __shared__ uint32_t bins[BINS];
+    __shared__ uint32_t wave_total[SEL_WAVES];
+    __shared__ uint32_t found[2];                                // digit, how many keys are wanted among those that have it
+    __shared__ int2 counts[2][SEL_WAVES];
+    const int unit = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = c.lens ? imax(0, imin(c.lens[unit / c.Hkv], c.Nk)) : c.Nk;
+    int *const index = c.index + static_cast<long>(unit) * c.keep;
+    if (unit % c.Hkv == 0 && tid == 0) c.lens_out[unit / c.Hkv] = imin(n, c.keep);
+    if (n <= c.keep) {
+        for (int s = tid; s < c.keep; s += SEL_THREADS) index[s] = s < n ? s : -1;
+        return;
+    }
+    const float *const W = c.W + static_cast<long>(unit) * c.Nk;
+    const int first = c.sinks, last = n - c.recent;              // the keys that are chosen from: [first, last)
+    uint32_t want = c.keep - c.sinks - c.recent, prefix = 0, mask = 0;
+    // 11 + 11 + 10 bits from the top: the digit in which the want-th largest lies
+    for (int pass = 0; pass < 3 && want; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+        for (int i = tid; i < BINS; i += SEL_THREADS) bins[i] = 0;
+        __syncthreads();
+        for (int j = first + tid; j < last; j += SEL_THREADS) {
+            const uint32_t u = order_of(W[j]);
+            if ((u & mask) == prefix) atomicAdd(&bins[(u >> shift) & ((1u << width) - 1)], 1u);
+        }
+        __syncthreads();
+        // from the top bin down: thread t has bins 2047 - 2 t and the one below
+        const int b0 = BINS - 1 - 2 * tid;
+        const uint32_t c0 = bins[b0], c1 = bins[b0 - 1];
+        uint32_t run = c0 + c1;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const uint32_t y = __shfl_up(run, s);
+            if (lane >= s) run += y;
+        }
+        if (lane == 63) wave_total[wave] = run;
+        __syncthreads();
+        uint32_t before = run - c0 - c1;
+        for (int w = 0; w < wave; ++w) before += wave_total[w];
+        if (before < want && want <= before + c0) found[0] = b0, found[1] = want - before;
+        else if (before + c0 < want && want <= before + c0 + c1) found[0] = b0 - 1, found[1] = want - before - c0;
+        __syncthreads();
+        prefix |= found[0] << shift;
+        mask |= ((1u << width) - 1) << shift;
+        want = found[1];
+    }
+    // `prefix` is the order of the last weight that stays, `want` how many of those equal to it do: the first ones.  (want = 0: none is chosen.)
+    const bool none = c.keep == c.sinks + c.recent;
+    int base = 0, equal_base = 0;
+    int parity = 0;
+    for (int j0 = 0; j0 < n; j0 += 4 * SEL_THREADS, parity ^= 1) {
+        bool more[4], equal[4];
+        int n_more = 0, n_equal = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int j = j0 + wave * 256 + e * 64 + lane;
+            const bool middle = j >= first && j < last && !none;
+            const uint32_t u = middle ? order_of(W[j]) : 0;
+            more[e] = j < n && (j < first || j >= last || (middle && u > prefix));
+            equal[e] = middle && u == prefix;
+            n_more += __popcll(__ballot(more[e]));
+            n_equal += __popcll(__ballot(equal[e]));
+        }
+        if (lane == 0) counts[parity][wave] = int2{n_more, n_equal};
+        __syncthreads();
+        int my_more = base, my_equal = equal_base;               // kept (without the equal ones) and equal ones in front of this wavefront's keys
+        for (int w = 0; w < SEL_WAVES; ++w) {
+            const int2 x = counts[parity][w];
+            if (w < wave) my_more += x.x, my_equal += x.y;
+            base += x.x, equal_base += x.y;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t bm = __ballot(more[e]), be = __ballot(equal[e]), below = (1ull << lane) - 1;
+            const int rank = my_equal + __popcll(be & below);
+            const bool stays = more[e] || (equal[e] && rank < static_cast<int>(want));
+            const int at = my_more + __popcll(bm & below) + imin(rank, static_cast<int>(want));
+            if (stays) index[at] = j0 + wave * 256 + e * 64 + lane;
+            my_more += __popcll(bm), my_equal += __popcll(be);
+        }
+    }
+}
+
+// 16 bytes of a row to a thread, `chunks` threads to a key; the scales and weights go with the first two
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int k_chunks, int chunks, long slots) {
+    const long at = (blockIdx.x * 256L + threadIdx.x) / chunks;
+    const int part = static_cast<int>((blockIdx.x * 256L + threadIdx.x) % chunks);
+    if (at >= slots) return;
+    const int j = c.index[at];
+    const long from = at / c.keep * c.Nk + (j < 0 ? 0 : j);
+    v4i x = {0, 0, 0, 0};
+    if (part < k_chunks) {
+        if (j >= 0) x = *reinterpret_cast<const v4i *>(c.K + from * c.d + 16 * part);
+        *reinterpret_cast<v4i *>(c.K_out + at * c.d + 16 * part) = x;
+    } else {
+        if (j >= 0) x = *reinterpret_cast<const v4i *>(c.V + from * c.v_row + 16 * (part - k_chunks));
+        *reinterpret_cast<v4i *>(c.V_out + at * c.v_row + 16 * (part - k_chunks)) = x;
+    }
+    if (part == 0) c.sK_out[at] = j < 0 ? 0.0f : c.sK[from];
+    if (part == 1) c.W_out[at] = j < 0 ? 0.0f : c.W[from];
+}
+
+bool overlap(const void *a, long na, const void *b, long nb) {
+    const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+    return x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" long ifa_key_weights_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d) {
+    if (refuse_sizes(B, H, Hkv, Nq, Nk, d)) return -1;
+    return plan_of(B, Hkv, H / Hkv, Nq, Nk).bytes();
+}
+
+extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, const float *s_Q, const float *s_K, const int *lens, const float *W,
+                           int B, int H, int Hkv, int Nq, int Nk, int d, float *W_out, void *workspace, long workspace_bytes, void *hip_stream) {
+    if (const int rc = refuse_sizes(B, H, Hkv, Nq, Nk, d)) return rc;
+    if (!Q_i8 || !K_i8 || !s_Q || !s_K || !W_out || !workspace) return IFA_ERR_NULL;
+    if (!ifa_aligned16(Q_i8) || !ifa_aligned16(K_i8) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return IFA_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(s_Q), static_cast<const void *>(s_K), static_cast<const void *>(lens), static_cast<const void *>(W), static_cast<const void *>(W_out)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
+    const Plan plan = plan_of(B, Hkv, H / Hkv, Nq, Nk);
+    if (workspace_bytes < plan.bytes()) return IFA_ERR_WORKSPACE;
+    WeightsCall c = {};
+    c.Q = Q_i8, c.K = K_i8, c.sQ = s_Q, c.sK = s_K, c.W = W, c.lens = lens, c.out = W_out;
+    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.parts = plan.parts, c.slices = plan.slices;
+    char *const ws = static_cast<char *>(workspace);
+    c.stats = reinterpret_cast<float2 *>(ws);
+    c.scores = plan.stored ? reinterpret_cast<float *>(ws + plan.stats) : nullptr;
+    c.score_stride = plan.stride;
+    c.sums = plan.sums ? reinterpret_cast<float *>(ws + plan.stats + plan.scores) : nullptr;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return d == 128 ? launch<128>(c, plan, st) : launch<64>(c, plan, st);
+}
+
+extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void *V, int v_bytes, const float *W, const int *lens,
+                          int B, int Hkv, int Nk, int d, int keep, int recent, int sinks,
+                          signed char *K_out, float *s_K_out, void *V_out, float *W_out, int *index, int *lens_out, void *hip_stream) {
+    if (!K_i8 || !s_K || !V || !W || !K_out || !s_K_out || !V_out || !W_out || !index || !lens_out) return IFA_ERR_NULL;
+    if (B <= 0 || Hkv <= 0 || Nk <= 0 || d <= 0 || keep <= 0 || recent < 0 || sinks < 0) return IFA_ERR_SHAPE;
+    const long units = static_cast<long>(B) * Hkv;
+    if (keep > Nk || static_cast<long>(recent) + sinks > keep || units > (1L << 40) / Nk / d) return IFA_ERR_SHAPE;
+    if (v_bytes != 1 && v_bytes != 2) return IFA_ERR_DTYPE;
+    if ((d & 15) || d > 1024 || Nk > 0x7fffffff - 8192 || units > 1L << 22 || units * keep > (1L << 35) / ((1 + v_bytes) * d)) return IFA_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(K_i8), V, static_cast<const void *>(K_out), static_cast<const void *>(V_out)})
+        if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(s_K), static_cast<const void *>(W), static_cast<const void *>(lens), static_cast<const void *>(s_K_out),
+                          static_cast<const void *>(W_out), static_cast<const void *>(index), static_cast<const void *>(lens_out)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
+    // rows move while others are still read: nothing is evicted in place
+    const long in = units * Nk, out = units * keep;
+    const struct { const void *p; long n; } read[] = {{K_i8, in * d}, {s_K, in * 4}, {V, in * d * v_bytes}, {W, in * 4}, {lens, lens ? 4L * B : 0}},
+        written[] = {{K_out, out * d}, {s_K_out, out * 4}, {V_out, out * d * v_bytes}, {W_out, out * 4}, {index, out * 4}, {lens_out, 4L * B}};
+    for (const auto &w : written) {
+        for (const auto &r : read)
+            if (overlap(w.p, w.n, r.p, r.n)) return IFA_ERR_UNSUPPORTED;
+        for (const auto &o : written)
+            if (&o != &w && overlap(w.p, w.n, o.p, o.n)) return IFA_ERR_UNSUPPORTED;
+    }
+    EvictCall c = {K_i8, static_cast<const int8_t *>(V), s_K, W, lens, B, Hkv, Nk, d, d * v_bytes, keep, recent, sinks,
+                   K_out, static_cast<int8_t *>(V_out), s_K_out, W_out, index, lens_out};
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    hipLaunchKernelGGL(evict_select_kernel, dim3(static_cast<unsigned>(units)), dim3(SEL_THREADS), 0, st, c);
+    const int k_chunks = d / 16, chunks = k_chunks * (1 + v_bytes);
+    hipLaunchKernelGGL(evict_move_kernel, dim3(static_cast<unsigned>((out * chunks + 255) / 256)), dim3(256), 0, st, c, k_chunks, chunks, out);
+    return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
+}

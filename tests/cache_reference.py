@@ -93,3 +93,46 @@ def attention(s, out_dtype, lens=None, window=None, sinks=0):
 
 def on_gpu(s):
     return {k: None if x is None else x.cuda() for k, x in s.items()}
+
+
+def key_weights(s, lens=None, W=None):
+    """(W_out, the most that an output may be off).  A weight is off relatively by what a score is (8 max |S| 2^-24) and exp2 and 1 / l are (2^-22 each), its l by the
+    same and by the rounding of the sum (2^-19, as above); the sum over the rows rounds at each of its n additions by 2^-24 of at most itself."""
+    B, H, Nq, _ = s["q8"].shape
+    Hkv, Nk = s["k8"].shape[1:3]
+    G = H // Hkv
+    out, tol = torch.zeros(B, Hkv, Nk, dtype=torch.float64), torch.zeros(B, Hkv, Nk, dtype=torch.float64)
+    for b in range(B):
+        for h in range(H):
+            S, L = scores(s, b, h, lens)
+            P = softmax(S)
+            finite = S[~S.isinf()]
+            rel = 2 * (8 * (finite.abs().max().item() if finite.numel() else 0.0) * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -22 + 2.0 ** -19
+            out[b, h // G, :L] += P.sum(0)
+            tol[b, h // G, :L] += rel * P.sum(0)
+    if W is not None:
+        out += W.double()
+    return out, tol + (G * Nq + 2) * 2.0 ** -24 * out.abs() + 1e-35
+
+
+def evict(s, W, keep, recent, sinks, lens=None):
+    """The six outputs, exactly."""
+    B, Hkv, Nk, d = s["k8"].shape
+    index = torch.full((B, Hkv, keep), -1, dtype=torch.int32)
+    n_of = [Nk if lens is None else max(0, min(int(lens[b]), Nk)) for b in range(B)]
+    for b, n in enumerate(n_of):
+        for h in range(Hkv):
+            if n <= keep:
+                stay = list(range(n))
+            else:
+                w = W[b, h].tolist()
+                middle = sorted(range(sinks, n - recent), key=lambda j: (w[j] != w[j], -w[j] if w[j] == w[j] else 0.0, j))
+                stay = list(range(sinks)) + sorted(middle[:keep - sinks - recent]) + list(range(n - recent, n))
+            index[b, h, :len(stay)] = torch.tensor(stay, dtype=torch.int32)
+    at, there = index.clamp_min(0).long(), index >= 0
+
+    def pick(x):
+        i = at if x.dim() == 3 else at.unsqueeze(-1).expand(B, Hkv, keep, d)
+        y = x.gather(2, i)
+        return torch.where(there if x.dim() == 3 else there.unsqueeze(-1), y, torch.zeros_like(y))
+    return pick(s["k8"]), pick(s["sk"]), pick(s["v"]), pick(W), index, torch.tensor([min(n, keep) for n in n_of], dtype=torch.int32)

@@ -56,6 +56,45 @@ def test_prefix(L):
     assert L.ifa_prefix_workspace_bytes(1, 4, 2, 1, 0, 100, 128) == -1
 
 
+def weights(L, q=P, k=P, sq=P, sk=P, lens=NULL, w=NULL, B=1, H=4, Hkv=2, Nq=1, Nk=100, d=128, o=P, ws=WS, n=1 << 40):
+    return L.key_weights(q, k, sq, sk, lens, w, B, H, Hkv, Nq, Nk, d, o, ws, n, None)
+
+
+def test_key_weights(L):
+    for name in ("q", "k", "sq", "sk", "o", "ws"):
+        assert weights(L, **{name: NULL}) == -1, name
+    for bad in (dict(B=0), dict(H=3), dict(Nq=0), dict(Nk=-1), dict(d=0)):
+        assert weights(L, **bad) == -2, bad
+    for bad in (dict(d=32), dict(q=ODD), dict(k=ODD), dict(ws=ODD), dict(w=ctypes.c_void_p(0x1002)), dict(o=ctypes.c_void_p(0x1002)), dict(Nk=0x7ff00000 // 256 + 1),
+                dict(Nq=1 << 25, Nk=1), dict(B=1 << 10, H=2, Nk=1 << 20, d=64)):
+        assert weights(L, **bad) == -4, bad
+    need = L.ifa_key_weights_workspace_bytes(1, 4, 2, 1, 100, 128)
+    assert need > 0 and weights(L, n=need - 1) == -6 and L.ifa_key_weights_workspace_bytes(1, 4, 2, 1, 100, 96) == -1
+
+
+def evict(L, at=None, vb=2, lens=NULL, B=1, Hkv=2, Nk=100, d=128, keep=50, recent=5, sinks=4):
+    """`at`: addresses of K, s_K, V, W and the six outputs."""
+    a = [ctypes.c_void_p(x) for x in at or [(1 + i) << 20 for i in range(10)]]
+    return L.evict_keys(a[0], a[1], a[2], vb, a[3], lens, B, Hkv, Nk, d, keep, recent, sinks, *a[4:], None)
+
+
+def test_evict_keys(L):
+    apart = [(1 + i) << 20 for i in range(10)]
+    for i in range(10):
+        assert evict(L, apart[:i] + [0] + apart[i + 1:]) == -1, i
+    for bad in (dict(B=0), dict(Hkv=0), dict(Nk=0), dict(d=0), dict(keep=0), dict(keep=101), dict(recent=-1), dict(sinks=-1), dict(recent=30, sinks=21)):
+        assert evict(L, **bad) == -2, bad
+    assert evict(L, vb=4) == -3
+    for bad in (dict(d=72), dict(d=1040), dict(B=1 << 22, Hkv=2, Nk=60, keep=50), dict(lens=ctypes.c_void_p(0x1002))):
+        assert evict(L, **bad) == -4, bad
+    for i in (0, 2, 4, 6):                               # K, V and their outputs: 16 bytes
+        assert evict(L, apart[:i] + [apart[i] + 8] + apart[i + 1:]) == -4, i
+    for i in range(4, 10):                               # an output on an input, on another output, or over the end of one
+        for j in (0, 1, 2, 3, 4 + (i - 3) % 6):
+            assert evict(L, apart[:i] + [apart[j]] + apart[i + 1:]) == -4, (i, j)
+    assert evict(L, apart[:4] + [apart[0] + 2 * 100 * 128 - 16] + apart[5:]) == -4
+
+
 def test_the_binding_names_the_operand(monkeypatch):
     q, k = torch.zeros(1, 4, 1, 64, dtype=torch.int8), torch.zeros(1, 2, 9, 64, dtype=torch.int8)
     v, sq, sk = torch.zeros(1, 2, 9, 64).half(), torch.ones(1, 4, 1), torch.ones(1, 2, 9)
