@@ -79,7 +79,8 @@ _native = None
 _NATIVE_PATH = os.path.join(_HERE, "_intfa_host.so")
 # the functions of the C ABI that the module calls, in its order
 _NATIVE_CALLS = ("quantize_tokenwise_ex", "quantize_headwise_ex", "quantize_blockwise", "quantize_qkv", "quantize_qk", "int_flash_attn_fwd_rect", "int_flash_attn_fwd_vblock_rect",
-                 "int_flash_attn_fwd_half_rect", "int_flash_attn_fwd_splitk", "int_flash_attn_fwd_splitk_static", "ifa_block_cols")
+                 "int_flash_attn_fwd_half_rect", "int_flash_attn_fwd_splitk", "int_flash_attn_fwd_splitk_static", "ifa_block_cols", "ifa_window_workspace_bytes", "int_flash_attn_fwd_window", "ifa_prefix_workspace_bytes",
+                 "int_flash_attn_fwd_prefix", "ifa_key_weights_workspace_bytes", "key_weights", "evict_keys")
 
 
 def _address(fn):
@@ -438,6 +439,10 @@ def int_flash_attn_fwd_window(Q_i8, K_i8, V, s_Q, s_K, window, sinks=0, s_V=None
     are its last Nq positions, and the query at position p sees keys j <= p with j > p - window or j < sinks.  A query that sees nothing
     gives zeros.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).  `workspace`: a uint8 device tensor of
     window_workspace_bytes(...) bytes (allocated here if not given)."""
+    if out is None:
+        r = (_native or _load_native()).window(Q_i8, K_i8, V, s_Q, s_K, window, sinks, s_V, lens, out_dtype, workspace)
+        if r is not None:
+            return r
     (B, H, Hkv, Nq, Nk, d), dev, at, out = _cache_operands(Q_i8, K_i8, V, s_Q, s_K, s_V, lens, out, out_dtype)
     window, sinks = min(int(window), 0x7fffffff), min(int(sinks), 0x7fffffff)
     if window < 1 or sinks < 0:
@@ -457,6 +462,10 @@ def int_flash_attn_fwd_prefix(Q_i8, Kp_i8, Vp, K_i8, V, s_Q, s_Kp, s_K, s_Vp=Non
     """Attention of a batch whose sequences begin with the same keys: shared Kp, Vp [Hkv, Np, d] with s_Kp [Hkv, Np], held once, in front of
     own K, V [B, Hkv, Nk, d] (lens[b] of them).  V and Vp are fp16, or int8 with s_V [B, Hkv] and s_Vp [Hkv].  Queries as in
     int_flash_attn_fwd_window, without the window: each sees all shared keys and its own keys j <= lens[b] - Nq + i."""
+    if out is None:
+        r = (_native or _load_native()).prefix(Q_i8, Kp_i8, Vp, K_i8, V, s_Q, s_Kp, s_K, s_Vp, s_V, lens, out_dtype, workspace)
+        if r is not None:
+            return r
     import torch
     (B, H, Hkv, Nq, Nk, d), dev, at, out = _cache_operands(Q_i8, K_i8, V, s_Q, s_K, s_V, lens, out, out_dtype)
     if getattr(Kp_i8, "dim", int)() != 3 or Kp_i8.shape[1] == 0:
@@ -483,6 +492,9 @@ def key_weights(Q_i8, K_i8, s_Q, s_K, W=None, lens=None, out=None, workspace=Non
     """The softmax weight that each key of a cache draws, summed over the queries and the heads of its group, added to W [B, Hkv, Nk]
     (None: zeros): fp32 [B, Hkv, Nk], into `out` if given (which may be W).  int8 Q [B, H, Nq, d], K [B, Hkv, Nk, d] with token-level scales; the queries
     are the last Nq positions of the lens[b] keys of their sequence and see the keys up to their own."""
+    r = (_native or _load_native()).weights(Q_i8, K_i8, s_Q, s_K, W, lens, out, workspace)
+    if r is not None:
+        return out if out is not None else r
     import torch
     B, H, Hkv, Nq, Nk, d = _cache_sizes(Q_i8, K_i8)
     dev = torch.cuda.current_device()
@@ -502,6 +514,10 @@ def evict_keys(K_i8, s_K, V, W, keep, recent=0, sinks=0, lens=None, out=None):
     keys, the last `recent` and those of the largest W between them (of equal ones the first), in their order.  Returns (K_i8, s_K, V, W
     [B, Hkv, keep, ...], index [B, Hkv, keep] int32, lens [B] int32); past min(lens[b], keep) keys index is -1 and the rest zero.
     out: optional tuple of those six tensors to write into, which overlap neither the inputs nor each other."""
+    if out is None:
+        r = (_native or _load_native()).evict(K_i8, s_K, V, W, keep, recent, sinks, lens)
+        if r is not None:
+            return r
     import torch
     if getattr(K_i8, "dim", int)() != 4 or K_i8.numel() == 0:
         raise IntfaError("K is [B, Hkv, Nk, d] and not empty")

@@ -33,6 +33,13 @@ struct Abi {
     decltype(&::int_flash_attn_fwd_splitk) splitk;
     decltype(&::int_flash_attn_fwd_splitk_static) splitk_static;
     decltype(&::ifa_block_cols) block_cols;
+    decltype(&::ifa_window_workspace_bytes) window_bytes;
+    decltype(&::int_flash_attn_fwd_window) window;
+    decltype(&::ifa_prefix_workspace_bytes) prefix_bytes;
+    decltype(&::int_flash_attn_fwd_prefix) prefix;
+    decltype(&::ifa_key_weights_workspace_bytes) weights_bytes;
+    decltype(&::key_weights) weights;
+    decltype(&::evict_keys) evict;
 } abi;
 constexpr int ABI_FUNCTIONS = sizeof(Abi) / sizeof(void *);
 PyObject *check = nullptr;                                       // the binding's: check(status, name of the call) raises what such a status raises
@@ -258,8 +265,135 @@ PyObject *splitk(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- a quantized cache in long use: 17 to 27 us of host a call through Python, 5 to 9 like this
+bool optional(PyObject *o, c10::DeviceIndex dev, const at::Tensor *&t) { return o == Py_None || (t = plain(o, dev)); }
+bool integer(PyObject *o, int &v) {                              // a plain int; what lies above INT_MAX means "all of them" everywhere here
+    int overflow = 0;
+    if (!PyLong_CheckExact(o)) return false;
+    const long x = PyLong_AsLongAndOverflow(o, &overflow);
+    if (overflow < 0 || x < 0) return false;
+    v = overflow || x > INT_MAX ? INT_MAX : static_cast<int>(x);
+    return true;
+}
+bool is(const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape) { return t->scalar_type() == type && t->sizes() == shape; }
+
+// Q [B, H, Nq, d] and s_Q against a cache K [B, Hkv, Nk, d], s_K, optional lens [B]
+struct Cached {
+    const at::Tensor *q, *k, *sq, *sk, *lens = nullptr;
+    int B, H, Hkv, Nq, Nk, d;
+    bool take(c10::DeviceIndex dev, PyObject *q_, PyObject *k_, PyObject *sq_, PyObject *sk_, PyObject *lens_) {
+        if (!(q = plain(q_, dev)) || !(k = plain(k_, dev)) || !(sq = plain(sq_, dev)) || !(sk = plain(sk_, dev)) || !optional(lens_, dev, lens)) return false;
+        if (q->dim() != 4 || k->dim() != 4 || q->scalar_type() != at::kChar || k->scalar_type() != at::kChar) return false;
+        for (const at::Tensor *t : {q, k})
+            for (const auto s : t->sizes()) if (s > INT_MAX) return false;
+        B = static_cast<int>(q->size(0)), H = static_cast<int>(q->size(1)), Nq = static_cast<int>(q->size(2)), d = static_cast<int>(q->size(3));
+        Hkv = static_cast<int>(k->size(1)), Nk = static_cast<int>(k->size(2));
+        return k->size(0) == B && k->size(3) == d && H % Hkv == 0 && is(sq, at::kFloat, {B, H, Nq}) && is(sk, at::kFloat, {B, Hkv, Nk}) && (!lens || is(lens, at::kInt, {B}));
+    }
+    const int *lengths() const { return lens ? static_cast<const int *>(lens->data_ptr()) : nullptr; }
+};
+// V [..., d] and its scale: fp16 and none, or INT8 and one of that shape
+bool values(const at::Tensor *v, const at::Tensor *sv, at::IntArrayRef shape, at::IntArrayRef scale_shape) {
+    return is(v, sv ? at::kChar : at::kHalf, shape) && (!sv || is(sv, at::kFloat, scale_shape));
+}
+bool output(const at::Tensor &q, PyObject *out_dtype, at::Tensor &out, int &o_dtype) {
+    const at::ScalarType ot = out_dtype == Py_None ? at::kHalf : THPDtype_Check(out_dtype) ? reinterpret_cast<THPDtype *>(out_dtype)->scalar_type : at::kChar;
+    if ((o_dtype = dtype_enum(ot)) < 0) return false;
+    out = like(q, ot);
+    return true;
+}
+// The caller's workspace, or one from the caching allocator, which keeps it for this stream
+struct Workspace {
+    at::Tensor own;
+    void *p = nullptr;
+    long bytes = 0;
+    bool take(const at::Tensor *given, long need, const at::Device &device) {
+        if (need < 0 || (given && given->scalar_type() != at::kByte)) return false;
+        if (!given && need > 0) own = at::detail::empty_cuda({need}, at::kByte, device, std::nullopt);
+        const at::Tensor *t = given ? given : own.defined() ? &own : nullptr;
+        if (t) p = t->data_ptr(), bytes = t->numel();
+        return true;
+    }
+};
+
+// window(Q, K, V, s_Q, s_K, window, sinks, s_V, lens, out_dtype, workspace)
+PyObject *window(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Cached c;
+        const at::Tensor *v, *sv = nullptr, *given = nullptr;
+        int w, sinks, o_dtype;
+        at::Tensor out;
+        Workspace ws;
+        if (n != 11 || !c.take(dev, a[0], a[1], a[3], a[4], a[8]) || !(v = plain(a[2], dev)) || !integer(a[5], w) || !integer(a[6], sinks) || !optional(a[7], dev, sv) || !optional(a[10], dev, given) ||
+            !values(v, sv, c.k->sizes(), {c.B, c.Hkv}) || !output(*c.q, a[9], out, o_dtype) || !ws.take(given, abi.window_bytes(c.B, c.H, c.Hkv, c.Nq, c.Nk, c.d, w, sinks), c.q->device())) return nullptr;
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.window, i8(*c.q), i8(*c.k), v->data_ptr(), f32(*c.sq), f32(*c.sk), sv ? f32(*sv) : nullptr, c.lengths(), c.B, c.H, c.Hkv, c.Nq, c.Nk, c.d, w, sinks, out.data_ptr(), o_dtype,
+                                ws.p, ws.bytes, st);
+        return succeeded(rc, "int_flash_attn_fwd_window") ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+// prefix(Q, Kp, Vp, K, V, s_Q, s_Kp, s_K, s_Vp, s_V, lens, out_dtype, workspace)
+PyObject *prefix(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Cached c;
+        const at::Tensor *kp, *vp, *v, *skp, *svp = nullptr, *sv = nullptr, *given = nullptr;
+        int o_dtype;
+        at::Tensor out;
+        Workspace ws;
+        if (n != 13 || !c.take(dev, a[0], a[3], a[5], a[7], a[10]) || !(kp = plain(a[1], dev)) || !(vp = plain(a[2], dev)) || !(v = plain(a[4], dev)) || !(skp = plain(a[6], dev)) ||
+            !optional(a[8], dev, svp) || !optional(a[9], dev, sv) || !optional(a[12], dev, given) || !svp != !sv || kp->dim() != 3 || kp->size(1) > INT_MAX) return nullptr;
+        const int Np = static_cast<int>(kp->size(1));
+        if (!is(kp, at::kChar, {c.Hkv, Np, c.d}) || !is(skp, at::kFloat, {c.Hkv, Np}) || !values(vp, svp, kp->sizes(), {c.Hkv}) || !values(v, sv, c.k->sizes(), {c.B, c.Hkv}) ||
+            !output(*c.q, a[11], out, o_dtype) || !ws.take(given, abi.prefix_bytes(c.B, c.H, c.Hkv, c.Nq, Np, c.Nk, c.d), c.q->device())) return nullptr;
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.prefix, i8(*c.q), i8(*kp), vp->data_ptr(), i8(*c.k), v->data_ptr(), f32(*c.sq), f32(*skp), f32(*c.sk), svp ? f32(*svp) : nullptr, sv ? f32(*sv) : nullptr, c.lengths(),
+                                c.B, c.H, c.Hkv, c.Nq, Np, c.Nk, c.d, out.data_ptr(), o_dtype, ws.p, ws.bytes, st);
+        return succeeded(rc, "int_flash_attn_fwd_prefix") ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+// weights(Q, K, s_Q, s_K, W, lens, out, workspace)
+PyObject *weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Cached c;
+        const at::Tensor *w = nullptr, *to = nullptr, *given = nullptr;
+        Workspace ws;
+        if (n != 8 || !c.take(dev, a[0], a[1], a[2], a[3], a[5]) || !optional(a[4], dev, w) || !optional(a[6], dev, to) || !optional(a[7], dev, given)) return nullptr;
+        if ((w && !is(w, at::kFloat, c.sk->sizes())) || (to && !is(to, at::kFloat, c.sk->sizes()))) return nullptr;
+        if (!ws.take(given, abi.weights_bytes(c.B, c.H, c.Hkv, c.Nq, c.Nk, c.d), c.q->device())) return nullptr;
+        const at::Tensor out = to ? *to : like(*c.sk, at::kFloat);
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.weights, i8(*c.q), i8(*c.k), f32(*c.sq), f32(*c.sk), c.lengths(), w ? f32(*w) : nullptr, c.B, c.H, c.Hkv, c.Nq, c.Nk, c.d, f32(out), ws.p, ws.bytes, st);
+        return succeeded(rc, "key_weights") ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+// evict(K, s_K, V, W, keep, recent, sinks, lens)
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        const at::Tensor *k, *sk, *v, *w, *lens = nullptr;
+        int keep, recent, sinks;
+        if (n != 8 || !(k = plain(a[0], dev)) || !(sk = plain(a[1], dev)) || !(v = plain(a[2], dev)) || !(w = plain(a[3], dev)) || !integer(a[4], keep) || !integer(a[5], recent) || !integer(a[6], sinks) ||
+            !optional(a[7], dev, lens) || k->dim() != 4 || k->scalar_type() != at::kChar) return nullptr;
+        for (const auto s : k->sizes()) if (s > INT_MAX) return nullptr;
+        const int B = static_cast<int>(k->size(0)), Hkv = static_cast<int>(k->size(1)), Nk = static_cast<int>(k->size(2)), d = static_cast<int>(k->size(3));
+        const at::ScalarType vt = v->scalar_type();
+        if (!is(sk, at::kFloat, {B, Hkv, Nk}) || !is(w, at::kFloat, {B, Hkv, Nk}) || (vt != at::kChar && vt != at::kHalf) || v->sizes() != k->sizes() || (lens && !is(lens, at::kInt, {B}))) return nullptr;
+        if (keep < 1 || keep > Nk || static_cast<long>(recent) + sinks > keep) return nullptr;
+        const at::Device device = k->device();
+        auto rows = [&](at::ScalarType type) { return at::detail::empty_cuda({B, Hkv, keep}, type, device, std::nullopt); };
+        auto wide = [&](at::ScalarType type) { return at::detail::empty_cuda({B, Hkv, keep, d}, type, device, std::nullopt); };
+        const at::Tensor k2 = wide(at::kChar), sk2 = rows(at::kFloat), v2 = wide(vt), w2 = rows(at::kFloat), index = rows(at::kInt), left = at::detail::empty_cuda({B}, at::kInt, device, std::nullopt);
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.evict, i8(*k), f32(*sk), v->data_ptr(), static_cast<int>(v->element_size()), f32(*w), lens ? static_cast<const int *>(lens->data_ptr()) : nullptr, B, Hkv, Nk, d, keep, recent, sinks,
+                                i8(k2), f32(sk2), v2.data_ptr(), f32(w2), static_cast<int *>(index.data_ptr()), static_cast<int *>(left.data_ptr()), st);
+        return succeeded(rc, "evict_keys") ? tuple({k2, sk2, v2, w2, index, left}) : nullptr;
+    });
+}
+
 #define FASTCALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FASTCALL(init), FASTCALL(tokenwise), FASTCALL(headwise), FASTCALL(blockwise), FASTCALL(qkv), FASTCALL(qk), FASTCALL(fwd), FASTCALL(half), FASTCALL(splitk), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FASTCALL(init), FASTCALL(tokenwise), FASTCALL(headwise), FASTCALL(blockwise), FASTCALL(qkv), FASTCALL(qk), FASTCALL(fwd), FASTCALL(half), FASTCALL(splitk), FASTCALL(window), FASTCALL(prefix), FASTCALL(weights), FASTCALL(evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_intfa_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
