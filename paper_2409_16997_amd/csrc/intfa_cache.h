@@ -127,6 +127,10 @@ __device__ __forceinline__ h8 v_operand(lds_ptr vs, unsigned v0, int dt, int key
     }
 }
 
+// Which of 64 keys count for a row, a bit each: key k iff k <= hi and (k >= from or k < sink)
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t keys_seen(int hi, int from, int sink) { return below(hi + 1) & (~below(from) | below(sink)); }
+
 // N pieces of 1 KB, one after the other (N a power of two up to 8)
 template <int N> __device__ __forceinline__ void copy_pieces(const BufRsrc &r, lds_ptr lds, unsigned even, unsigned odd, int soff) {
     if constexpr (N <= 4) lds_copy16_run<N>(r, lds, even, odd, soff);

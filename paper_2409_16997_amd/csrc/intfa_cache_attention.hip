@@ -10,6 +10,7 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_bf16.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "intfa.h"
 #include "intfa_internal.h"
@@ -155,11 +156,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
         if (!clear) {
             const int hi = inA ? (shared || p >= 0 ? runs.lenA - 1 : -1) - j0 : p - runs.lo - j0;
             const int from = inA ? 0 : p - runs.lo - c.window + 1 - j0, sink = inA ? 0 : c.sinks - runs.lo - j0;
+            const uint32_t seen = static_cast<uint32_t>(keys_seen(hi, from, sink)) >> (4 * g);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int k = 8 * (v >> 2) + 4 * g + (v & 3);
-                if (k > hi || (k < from && k >= sink)) a[v] = -INFINITY;
-            }
+            for (int v = 0; v < 16; ++v)
+                if (!(seen & (1u << (8 * (v >> 2) + (v & 3))))) a[v] = -INFINITY;
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v) tmax = fmaxf(tmax, a[v]);
@@ -240,6 +240,236 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 #endif
 }
 
+// ---- many rows: tiles of 128 ----------------------------------------------------------------------------------------
+// Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered).  What bounds it is the vector unit: 32 keys of 32 rows are 12 matrix
+// instructions (384 cycles at d = 128), and of the vector instructions on each of their scores (subtract the start value, s_K, the maximum, s_Q and m, exp2, the conversion
+// in pairs, the sum in pairs) exp2 alone takes 16 cycles.  So nothing else is left to the vector unit:
+//   - the running maximum only moves when a block exceeds it by 2^8 (a row by itself: what a row gives does not depend on its neighbours), which an fp16 weight holds
+//     as well as a weight of 1, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made;
+//   - the weights are rounded toward zero, two to an instruction.  They are too small by 2^-11 on average, in O and in l alike; what is left of the quotient's error is
+//     within half a step (2^-11) of each weight, as with rounding to nearest.
+constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
+template <int D, bool VI8> struct SmemTile {
+    alignas(4096) int8_t k[2][TILE_KEYS * D];
+    alignas(4096) int8_t v[2][TILE_KEYS * V_ROW<D, VI8>];
+    alignas(256) float sk[2][TILE_KEYS];
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+template <int D> struct RowState {
+    float m2, l;                                                 // m2: the maximum that the weights refer to, log2 units
+    v16f o[D / 32];
+};
+constexpr float SLACK = 8.0f;
+
+// 64 keys in LDS against the wavefront's rows.  MASKED: those of `seen` count.
+template <int D, bool VI8, bool MASKED>
+__device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, const Lane<D, VI8> &lo, const v4i (&qf)[D / 32], float sq2, uint64_t seen, int g,
+                                           const v16i &bias, RowState<D> &st) {
+    constexpr int KS = D / 32, DT = D / 32;
+    v16i acc[2];
+    float a[2][16];
+    v4i kop[KS];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) kop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(ks, 32 * kk, lo.k0) + 32 * mt * D);
+        acc[mt] = bias;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) acc[mt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc[mt], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float bmax = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) {
+            const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(sk + 16 * g + 128 * mt + 32 * vq);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = (__int_as_float(acc[mt][4 * vq + e]) - ACC_BIAS_F) * skv[e];
+                if (MASKED) {
+                    if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * vq + e)))) x = -INFINITY;
+                }
+                a[mt][4 * vq + e] = x;
+                bmax = fmaxf(bmax, x);
+            }
+        }
+    __builtin_amdgcn_sched_barrier(0);
+    const float top = pair_max(bmax) * sq2;
+    const bool moves = top > st.m2 + SLACK;                      // (st.m2 = -inf: whenever a key counts)
+    if (__any(moves)) {
+        const float m_new = moves ? top : st.m2;
+        const float alpha = moves ? __builtin_amdgcn_exp2f(st.m2 - m_new) : 1.0f;
+        st.m2 = m_new;
+        st.l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) st.o[dt][v] *= alpha;
+    }
+    const float m = MASKED && st.m2 == -INFINITY ? 0.0f : st.m2; // a row that has seen nothing yet: weights of 0, no NaN
+    const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+        h2 ph[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ph[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)),
+                                                                      __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e + 1], sq2, -m))));
+            st.l = __builtin_amdgcn_fdot2(ph[e], ones, st.l, false);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const h8 pb = {ph[4 * s][0], ph[4 * s][1], ph[4 * s + 1][0], ph[4 * s + 1][1], ph[4 * s + 2][0], ph[4 * s + 2][1], ph[4 * s + 3][0], ph[4 * s + 3][1]};
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand<D, VI8>(vs, lo.v0, dt, 32 * mt + 16 * s), pb, st.o[dt], 0, 0, 0);
+        }
+    }
+}
+
+// A wavefront's 32 x D outputs through 64 D bytes of LDS of its own, so that whole (fp32: half) rows are stored.  at(row): where row `row` goes, null for nowhere.
+template <int D, typename OutT, typename Val, typename At>
+__device__ __forceinline__ void store_rows(lds_ptr stage, int lane, Val val, At at) {
+    constexpr int PASSES = sizeof(OutT) / 2, DTP = (D / 32) / PASSES, CH = D * 2 / 16, ROWS = 64 / CH;
+    const int r = lane & 31, g = lane >> 5, cc = lane % CH, rr = lane / CH;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+#pragma unroll
+        for (int dl = 0; dl < DTP; ++dl)
+#pragma unroll
+            for (int vq = 0; vq < 4; ++vq) {
+                const int dt = pass * DTP + dl;
+                if constexpr (sizeof(OutT) == 2)
+                    *reinterpret_cast<LDS_AS uint2 *>(stage + r * (2 * D) + (((4 * dl + vq) ^ (r & (CH - 1))) * 16) + 8 * g) =
+                        Pack4<OutT>::pack(val(dt, 4 * vq), val(dt, 4 * vq + 1), val(dt, 4 * vq + 2), val(dt, 4 * vq + 3));
+                else
+                    *reinterpret_cast<LDS_AS v4f *>(stage + r * (2 * D) + (((8 * dl + 2 * vq + g) ^ (r & (CH - 1))) * 16)) =
+                        v4f{val(dt, 4 * vq), val(dt, 4 * vq + 1), val(dt, 4 * vq + 2), val(dt, 4 * vq + 3)};
+            }
+#pragma unroll
+        for (int rd = 0; rd < 32 / ROWS; ++rd) {
+            const int row = rd * ROWS + rr;
+            const v4i x = *reinterpret_cast<LDS_AS const v4i *>(stage + row * (2 * D) + ((cc ^ (row & (CH - 1))) * 16));
+            char *const to = at(row);
+            if (to) __builtin_nontemporal_store(x, reinterpret_cast<v4i *>(to + pass * (2 * D) + 16 * cc));
+        }
+    }
+}
+#endif
+
+template <int D, bool VI8, bool ALL>
+__global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, int units, int row_tiles, int head_group) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemTile<D, VI8> sm;
+    constexpr int DT = D / 32, KB = TILE_KEYS * D, VB = TILE_KEYS * V_ROW<D, VI8>, KP = KB / 4096, VP = VB / 4096;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
+    map_workgroup(blockIdx.x, units, row_tiles * c.splits, head_group, !ALL, unit, ord);
+    const int rt = row_tiles - 1 - ord / c.splits, split = ord % c.splits;
+    const int b = ALL ? 0 : unit / c.Hkv, hk = ALL ? unit : unit % c.Hkv;
+    const bool shared = ALL || c.Kp != nullptr;
+    const int L = ALL ? 0 : keys_of(c.lens, b, c.Nk);
+    const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), w0 = imin(row0 + 32 * wave, last_row), w1 = imin(row0 + 32 * wave + 31, last_row);
+    const int row = imin(row0 + 32 * wave + r, last_row);
+    const int shift = L - c.Nq;
+    const Runs runs(shared, c.Np, c.window, c.sinks, ALL ? -1 : shift + row0 / c.G, ALL ? -1 : shift + last_row / c.G);
+    // positions of the wavefront's first and last row and of this lane's, from the first key of run B on
+    const int p0 = ALL ? -1 : shift + w0 / c.G - runs.lo, p1 = ALL ? -1 : shift + w1 / c.G - runs.lo, p = ALL ? -1 : shift + row / c.G - runs.lo;
+    const bool some = shared || p1 + runs.lo >= 0, every = shared || p0 + runs.lo >= 0, mine = shared || p + runs.lo >= 0;      // whether the rows see run A
+    const int sink = c.sinks - runs.lo;
+    const int blocksA = (runs.lenA + TILE_KEYS - 1) / TILE_KEYS, blocks = blocksA + (runs.lenB + TILE_KEYS - 1) / TILE_KEYS;
+    const int per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
+
+    const long kA = shared ? static_cast<long>(hk) * c.Np : static_cast<long>(unit) * c.Nk, kB = static_cast<long>(unit) * c.Nk + runs.lo;
+    const int8_t *vA = static_cast<const int8_t *>(shared ? c.Vp : c.V), *vB = static_cast<const int8_t *>(c.V);
+    const BufRsrc rKA = make_rsrc((shared ? c.Kp : c.K) + kA * D, runs.lenA * D), rVA = make_rsrc(vA + kA * V_ROW<D, VI8>, runs.lenA * V_ROW<D, VI8>),
+                  rSA = make_rsrc((shared ? c.sKp : c.sK) + kA, runs.lenA * 4);
+    const BufRsrc rKB = ALL ? rKA : make_rsrc(c.K + kB * D, runs.lenB * D), rVB = ALL ? rVA : make_rsrc(vB + kB * V_ROW<D, VI8>, runs.lenB * V_ROW<D, VI8>),
+                  rSB = ALL ? rSA : make_rsrc(c.sK + kB, runs.lenB * 4);
+
+    const Lane<D, VI8> lo(lane);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]);
+    auto stage = [&](int t, int slot) {                          // a quarter of the block to each wavefront
+        const bool inA = t < blocksA;
+        const int j0 = TILE_KEYS * (inA ? t : t - blocksA);
+        copy_pieces<KP>(pick(inA, rKA, rKB), kbuf + slot * KB + wave * KP * 1024, lo.gk, lo.gk, j0 * D + wave * KP * 1024);
+        copy_pieces<VP>(pick(inA, rVA, rVB), vbuf + slot * VB + wave * VP * 1024, lo.gv[0], lo.gv[1], j0 * V_ROW<D, VI8> + wave * VP * 1024);
+        if (wave == 3) lds_copy4(pick(inA, rSA, rSB), skbuf + slot * 256, 4 * lane, j0 * 4);
+    };
+    if (t0 < t1) stage(t0, 0);
+
+    const long qrow = row_of(c, ALL, unit, row);
+    v4i qf[D / 32];
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
+    const float sq2 = c.sQ[qrow] * LOG2E;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
+    v16i bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
+    asm volatile("" : "+v"(bias));
+    RowState<D> st;
+    st.m2 = -INFINITY, st.l = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
+    float unit_of_o = 1.0f;
+    if (VI8) unit_of_o = ALL || t0 < blocksA ? (shared ? c.sVp[hk] : c.sV[unit]) : c.sV[unit];
+
+    wait_all_memory();
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int slot = (t - t0) & 1;
+        if (t + 1 < t1) stage(t + 1, slot ^ 1);
+        const bool inA = t < blocksA;
+        const int j0 = TILE_KEYS * (inA ? t : t - blocksA);
+        if (VI8 && !ALL && t == blocksA && t > t0 && shared) {   // from the shared keys' scale of V to the own ones', once
+            const float f = unit_of_o / c.sV[unit];
+            unit_of_o = c.sV[unit];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) st.o[dt][v] *= f;
+        }
+        // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
+        const bool any = inA ? some : p1 >= j0 && (p0 - c.window < j0 + TILE_KEYS - 1 || j0 < sink);
+        const bool clear = inA ? every && j0 + TILE_KEYS <= runs.lenA : p0 >= j0 + TILE_KEYS - 1 && (p1 - c.window < j0 || j0 + TILE_KEYS <= sink);
+        if (clear) tile_block<D, VI8, false>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, 0, g, bias, st);
+        else if (any) tile_block<D, VI8, true>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2,
+                                               inA ? keys_seen((mine ? runs.lenA - 1 : -1) - j0, 0, 0) : keys_seen(p - j0, p - c.window + 1 - j0, sink - j0), g, bias, st);
+        wait_all_memory();                                       // my part of the next block has landed
+        __syncthreads();                                         // everyone's has, and this one's place is free
+    }
+
+    const float l = st.l + swap32(st.l);
+    const lds_ptr stage_out = (lds_ptr)(&sm) + wave * (64 * D);
+    const int first = row0 + 32 * wave;
+    if (c.part_o) {
+        const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows;
+        const int n = c.rows;
+        float *const po = c.part_o + pr * D;
+        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * unit_of_o; },
+                             [&](int k) { return first + k < n ? reinterpret_cast<char *>(po + static_cast<long>(first + k) * D) : nullptr; });
+        if (g == 0 && first + r < n) c.part_ml[pr + first + r] = float2{st.m2, l};
+        return;
+    }
+    const float f = l > 0.0f ? unit_of_o / l : 0.0f;             // a row that sees nothing: zeros
+    auto store = [&](auto type) {
+        using OutT = decltype(type);
+        store_rows<D, OutT>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * f; },
+                            [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(static_cast<OutT *>(c.O) + row_of(c, ALL, unit, first + k) * D) : nullptr; });
+    };
+    if (c.o_dtype == IFA_F32) store(float{});
+    else if (c.o_dtype == IFA_F16) store(__half{});
+    else store(__hip_bfloat16{});
+#endif
+}
+
 // ---- the parts of a row joined -----------------------------------------------------------------------------------
 // One row to D / 4 threads.  `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.
 struct Parts {
@@ -291,13 +521,15 @@ int parts_for(long groups, long keys) {
     return static_cast<int>(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
 }
 
+long tiles_of(long rows) { return rows > 32 ? (rows + TILE_ROWS - 1) / TILE_ROWS : 1; }
+
 Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sinks) {
-    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = (rows + 31) / 32;
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = tiles_of(rows);
     Plan p = {};
     const long span = static_cast<long>(window) + imin(Nq, 32) + sinks, keys = Nk < span ? Nk : span;
     p.own = parts_for(units * tiles, keys);
     if (Np > 0) {
-        const long all = rows * B, all_tiles = (all + 31) / 32;
+        const long all = rows * B, all_tiles = tiles_of(all);
         p.shared = parts_for(Hkv * all_tiles, Np);
         p.rows_shared = Hkv * all * p.shared;
     }
@@ -317,7 +549,13 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
         ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
         parts = {o, o + plan.rows_shared * D, ml, ml + plan.rows_shared, plan.shared, plan.own};
     }
-    auto few = [&](auto all, Call k, int n_units) {
+    auto run = [&](auto all, Call k, int n_units) {
+        if (k.rows > 32) {
+            const int row_tiles = (k.rows + TILE_ROWS - 1) / TILE_ROWS, head_group = head_group_for(true, 0, 0);
+            const long grid = static_cast<long>(n_units) * row_tiles * k.splits;
+            hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, k, n_units, row_tiles, head_group);
+            return;
+        }
         const int row_tiles = (k.rows + 31) / 32;
         const long grid = (static_cast<long>(n_units) * k.splits + 7) / 8 * 8 * row_tiles;
         hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, n_units, row_tiles);
@@ -327,12 +565,12 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
         k.rows = c.rows * c.B;
         k.splits = plan.shared;
         k.part_o = o, k.part_ml = ml;
-        few(std::true_type{}, k, c.Hkv);
+        run(std::true_type{}, k, c.Hkv);
         c.Kp = nullptr, c.Np = 0;                                // (the own keys alone from here on)
     }
     c.splits = plan.own;
     if (plan.join()) c.part_o = o + plan.rows_shared * D, c.part_ml = ml + plan.rows_shared;
-    few(std::false_type{}, c, units);
+    run(std::false_type{}, c, units);
     if (plan.join()) {
         c.Kp = Kp;
         const long all_rows = static_cast<long>(units) * c.rows;
