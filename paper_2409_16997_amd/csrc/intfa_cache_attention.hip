@@ -471,35 +471,75 @@ __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, in
 }
 
 // ---- the parts of a row joined -----------------------------------------------------------------------------------
-// One row to D / 4 threads.  `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.
+// `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.  P groups of D / 4 threads take every P-th part of a
+// row, each with a maximum of its own, and meet in LDS: what there is to wait for is a few loads in a row, not one for each part.
 struct Parts {
     const float *o_shared, *o_own;
     const float2 *ml_shared, *ml_own;
     int shared, own;
 };
-template <int D>
+template <int D, int P>
 __global__ __launch_bounds__(256) void cache_attention_join_kernel(Call c, Parts parts, long all_rows) {
-    constexpr int TPR = D / 4;
-    const long idx = blockIdx.x * (256L / TPR) + threadIdx.x / TPR;
-    const int cc = threadIdx.x % TPR;
-    if (idx >= all_rows) return;
-    const int per = c.Nq * c.G, unit = static_cast<int>(idx / per), in = static_cast<int>(idx % per), b = unit / c.Hkv, hk = unit % c.Hkv;
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * P);
+    __shared__ v4f so[P > 1 ? P : 1][ROWS][TPR];
+    __shared__ float2 sml[P > 1 ? P : 1][ROWS];
+    const int cc = threadIdx.x % TPR, pg = threadIdx.x / TPR % P, in_block = threadIdx.x / (TPR * P);
+    const long idx = static_cast<long>(blockIdx.x) * ROWS + in_block;
+    const bool valid = idx < all_rows;
+    const int per = c.Nq * c.G, unit = static_cast<int>(idx / per), in = static_cast<int>(idx % per), b = unit / c.Hkv, hk = unit % c.Hkv, n = valid ? parts.shared + parts.own : 0;
     const long s0 = static_cast<long>(hk) * parts.shared * c.B * per + static_cast<long>(b) * per + in, s_step = static_cast<long>(c.B) * per;
     const long o0 = static_cast<long>(unit) * parts.own * per + in;
-    float m = -INFINITY;
-    for (int i = 0; i < parts.shared; ++i) m = fmaxf(m, parts.ml_shared[s0 + i * s_step].x);
-    for (int i = 0; i < parts.own; ++i) m = fmaxf(m, parts.ml_own[o0 + static_cast<long>(i) * per].x);
-    float l = 0.0f;
+    float m = -INFINITY, l = 0.0f;
     v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](const float *po, const float2 *pml, long at) {
-        const float2 x = pml[at];
-        const float f = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);
-        const v4f y = *reinterpret_cast<const v4f *>(po + at * D + 4 * cc);
-        l += x.y * f;
-        s += y * f;
-    };
-    for (int i = 0; i < parts.shared; ++i) add(parts.o_shared, parts.ml_shared, s0 + i * s_step);
-    for (int i = 0; i < parts.own; ++i) add(parts.o_own, parts.ml_own, o0 + static_cast<long>(i) * per);
+    constexpr int AT_ONCE = 4;
+    for (int i0 = pg; i0 < n; i0 += AT_ONCE * P) {
+        float2 x[AT_ONCE];
+        v4f y[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = i0 + k * P;
+            x[k] = float2{-INFINITY, 0.0f};
+            y[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i < n) {
+                const bool first = i < parts.shared;
+                const long at = first ? s0 + i * s_step : o0 + static_cast<long>(i - parts.shared) * per;
+                x[k] = (first ? parts.ml_shared : parts.ml_own)[at];
+                y[k] = *reinterpret_cast<const v4f *>((first ? parts.o_shared : parts.o_own) + at * D + 4 * cc);
+            }
+        }
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) m_new = fmaxf(m_new, x[k].x);
+        if (m_new == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(m - m_new);       // exp2(-inf) = 0
+        l *= f, s *= f, m = m_new;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float w = __builtin_amdgcn_exp2f(x[k].x - m);
+            l += x[k].y * w;
+            s += y[k] * w;
+        }
+    }
+    if constexpr (P > 1) {
+        so[pg][in_block][cc] = s;
+        if (cc == 0) sml[pg][in_block] = float2{m, l};
+        __syncthreads();
+        if (pg) return;
+        float m_all = m;
+#pragma unroll
+        for (int k = 1; k < P; ++k) m_all = fmaxf(m_all, sml[k][in_block].x);
+        if (m_all != -INFINITY) {
+            const float f = __builtin_amdgcn_exp2f(m - m_all);
+            l *= f, s *= f;
+#pragma unroll
+            for (int k = 1; k < P; ++k) {
+                const float w = __builtin_amdgcn_exp2f(sml[k][in_block].x - m_all);
+                l += sml[k][in_block].y * w;
+                s += so[k][in_block][cc] * w;
+            }
+        }
+    }
+    if (!valid) return;
     const float q = l > 0.0f ? 1.0f / l : 0.0f;
     store4(c.O, c.o_dtype, row_of(c, false, unit, in) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
 }
@@ -514,23 +554,22 @@ struct Plan {
 };
 constexpr int MOST_PARTS = 64;
 
-// parts so that about two workgroups a CU have work, of at least 256 keys each
-int parts_for(long groups, long keys) {
-    long parts = (512 + groups - 1) / groups;
+// Parts where there is less than a workgroup for each place on the chip (two to a CU, of the kernel for 32 rows one), as many as there are places, of at least 256 keys each.
+int parts_for(long rows_of_unit, long units, long keys) {
+    const long groups = units * ((rows_of_unit + TILE_ROWS - 1) / TILE_ROWS), places = rows_of_unit > 32 ? 512 : 256;
+    long parts = places / groups;
     if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
     return static_cast<int>(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
 }
 
-long tiles_of(long rows) { return rows > 32 ? (rows + TILE_ROWS - 1) / TILE_ROWS : 1; }
-
 Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sinks) {
-    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = tiles_of(rows);
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     Plan p = {};
-    const long span = static_cast<long>(window) + imin(Nq, 32) + sinks, keys = Nk < span ? Nk : span;
-    p.own = parts_for(units * tiles, keys);
+    const long span = static_cast<long>(window) + imin(Nq, TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
+    p.own = parts_for(rows, units, keys);
     if (Np > 0) {
-        const long all = rows * B, all_tiles = tiles_of(all);
-        p.shared = parts_for(Hkv * all_tiles, Np);
+        const long all = rows * B;
+        p.shared = parts_for(all, Hkv, Np);
         p.rows_shared = Hkv * all * p.shared;
     }
     p.rows_own = units * rows * p.own;
@@ -574,7 +613,12 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
     if (plan.join()) {
         c.Kp = Kp;
         const long all_rows = static_cast<long>(units) * c.rows;
-        hipLaunchKernelGGL((cache_attention_join_kernel<D>), dim3(static_cast<unsigned>((all_rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, c, parts, all_rows);
+        auto join = [&](auto p) {
+            constexpr int P = decltype(p)::value, ROWS = 1024 / D / P;
+            hipLaunchKernelGGL((cache_attention_join_kernel<D, P>), dim3(static_cast<unsigned>((all_rows + ROWS - 1) / ROWS)), dim3(256), 0, st, c, parts, all_rows);
+        };
+        if (plan.shared + plan.own > 8) join(std::integral_constant<int, 8>{});
+        else join(std::integral_constant<int, 1>{});
     }
     return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
 }
