@@ -262,9 +262,10 @@ template <int D> struct RowState {
 };
 constexpr float SLACK = 8.0f;
 
-// 64 keys in LDS against the wavefront's rows.  MASKED: those of `seen` count.
-template <int D, bool VI8, bool MASKED>
-__device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, const Lane<D, VI8> &lo, const v4i (&qf)[D / 32], float sq2, uint64_t seen, int g,
+// 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.  (One body for both, with a branch around
+// the mask alone: two bodies and o would be moved from one's registers to the other's at every block.)
+template <int D, bool VI8>
+__device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, const Lane<D, VI8> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen, int g,
                                            const v16i &bias, RowState<D> &st) {
     constexpr int KS = D / 32, DT = D / 32;
     v16i acc[2];
@@ -279,22 +280,26 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
         for (int kk = 0; kk < KS; ++kk) acc[mt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc[mt], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    float bmax = -INFINITY;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int vq = 0; vq < 4; ++vq) {
             const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(sk + 16 * g + 128 * mt + 32 * vq);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = (__int_as_float(acc[mt][4 * vq + e]) - ACC_BIAS_F) * skv[e];
-                if (MASKED) {
-                    if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * vq + e)))) x = -INFINITY;
-                }
-                a[mt][4 * vq + e] = x;
-                bmax = fmaxf(bmax, x);
-            }
+            for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[mt][4 * vq + e]) - ACC_BIAS_F) * skv[e];
         }
+    if (!clear) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * (v >> 2) + (v & 3))))) a[mt][v] = -INFINITY;
+    }
+    float bmax = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
     __builtin_amdgcn_sched_barrier(0);
     const float top = pair_max(bmax) * sq2;
     const bool moves = top > st.m2 + SLACK;                      // (st.m2 = -inf: whenever a key counts)
@@ -308,7 +313,7 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
 #pragma unroll
             for (int v = 0; v < 16; ++v) st.o[dt][v] *= alpha;
     }
-    const float m = MASKED && st.m2 == -INFINITY ? 0.0f : st.m2; // a row that has seen nothing yet: weights of 0, no NaN
+    const float m = st.m2 == -INFINITY ? 0.0f : st.m2; // a row that has seen nothing yet: weights of 0, no NaN
     const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
@@ -439,9 +444,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, in
         // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
         const bool any = inA ? some : p1 >= j0 && (p0 - c.window < j0 + TILE_KEYS - 1 || j0 < sink);
         const bool clear = inA ? every && j0 + TILE_KEYS <= runs.lenA : p0 >= j0 + TILE_KEYS - 1 && (p1 - c.window < j0 || j0 + TILE_KEYS <= sink);
-        if (clear) tile_block<D, VI8, false>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, 0, g, bias, st);
-        else if (any) tile_block<D, VI8, true>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2,
-                                               inA ? keys_seen((mine ? runs.lenA - 1 : -1) - j0, 0, 0) : keys_seen(p - j0, p - c.window + 1 - j0, sink - j0), g, bias, st);
+        const uint64_t seen = clear ? 0 : inA ? keys_seen((mine ? runs.lenA - 1 : -1) - j0, 0, 0) : keys_seen(p - j0, p - c.window + 1 - j0, sink - j0);
+        if (any) tile_block<D, VI8>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, clear, seen, g, bias, st);
         wait_all_memory();                                       // my part of the next block has landed
         __syncthreads();                                         // everyone's has, and this one's place is free
     }
