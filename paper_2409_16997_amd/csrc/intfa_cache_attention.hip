@@ -315,23 +315,37 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
     }
     const float m = st.m2 == -INFINITY ? 0.0f : st.m2; // a row that has seen nothing yet: weights of 0, no NaN
     const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-        h2 ph[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ph[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)),
+    h2 ph[2][8];
+    auto weights = [&](int mt, int e) {
+        ph[mt][e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)),
                                                                       __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e + 1], sq2, -m))));
-            st.l = __builtin_amdgcn_fdot2(ph[e], ones, st.l, false);
-        }
+        st.l = __builtin_amdgcn_fdot2(ph[mt][e], ones, st.l, false);
+    };
+    // the weights of the second 32 keys between the products of the first
+    h8 vop[DT][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const h8 pb = {ph[4 * s][0], ph[4 * s][1], ph[4 * s + 1][0], ph[4 * s + 1][1], ph[4 * s + 2][0], ph[4 * s + 2][1], ph[4 * s + 3][0], ph[4 * s + 3][1]};
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand<D, VI8>(vs, lo.v0, dt, 32 * mt + 16 * s), pb, st.o[dt], 0, 0, 0);
+        for (int s = 0; s < 2; ++s) vop[dt][s] = v_operand<D, VI8>(vs, lo.v0, dt, 16 * s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) weights(0, e);
+    __builtin_amdgcn_s_setprio(3);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const h8 pb = {ph[mt][4 * s][0], ph[mt][4 * s][1], ph[mt][4 * s + 1][0], ph[mt][4 * s + 1][1], ph[mt][4 * s + 2][0], ph[mt][4 * s + 2][1], ph[mt][4 * s + 3][0], ph[mt][4 * s + 3][1]};
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vop[dt][s], pb, st.o[dt], 0, 0, 0);
+                if (mt == 0) vop[dt][s] = v_operand<D, VI8>(vs, lo.v0, dt, 32 + 16 * s);
+            }
+            if (mt == 0) {
+#pragma unroll
+                for (int q = 0; q < 8 / DT; ++q) weights(1, dt * (8 / DT) + q);
+            }
         }
-    }
+    __builtin_amdgcn_s_setprio(0);
 }
 
 // A wavefront's 32 x D outputs through 64 D bytes of LDS of its own, so that whole (fp32: half) rows are stored.  at(row): where row `row` goes, null for nowhere.
@@ -374,35 +388,49 @@ __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, in
     int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
     map_workgroup(blockIdx.x, units, row_tiles * c.splits, head_group, !ALL, unit, ord);
     const int rt = row_tiles - 1 - ord / c.splits, split = ord % c.splits;
-    const int b = ALL ? 0 : unit / c.Hkv, hk = ALL ? unit : unit % c.Hkv;
-    const bool shared = ALL || c.Kp != nullptr;
-    const int L = ALL ? 0 : keys_of(c.lens, b, c.Nk);
-    const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), w0 = imin(row0 + 32 * wave, last_row), w1 = imin(row0 + 32 * wave + 31, last_row);
-    const int row = imin(row0 + 32 * wave + r, last_row);
-    const int shift = L - c.Nq;
-    const Runs runs(shared, c.Np, c.window, c.sinks, ALL ? -1 : shift + row0 / c.G, ALL ? -1 : shift + last_row / c.G);
-    // positions of the wavefront's first and last row and of this lane's, from the first key of run B on
-    const int p0 = ALL ? -1 : shift + w0 / c.G - runs.lo, p1 = ALL ? -1 : shift + w1 / c.G - runs.lo, p = ALL ? -1 : shift + row / c.G - runs.lo;
-    const bool some = shared || p1 + runs.lo >= 0, every = shared || p0 + runs.lo >= 0, mine = shared || p + runs.lo >= 0;      // whether the rows see run A
-    const int sink = c.sinks - runs.lo;
-    const int blocksA = (runs.lenA + TILE_KEYS - 1) / TILE_KEYS, blocks = blocksA + (runs.lenB + TILE_KEYS - 1) / TILE_KEYS;
-    const int per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
+    const int L = ALL ? c.Np : keys_of(c.lens, unit / c.Hkv, c.Nk), window = ALL ? c.Np : c.window;
+    const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), row = imin(row0 + 32 * wave + r, last_row);
+    // the position of a row; every row sees all of the shared keys
+    auto position = [&](int i) { return ALL ? L - 1 : L - c.Nq + i / c.G; };
+    const int pos0 = position(row0), pos1 = position(last_row);
+    // The two runs one after the other, cut into blocks of 64 with no seam: key v of them is key v for v < lenA, else key v + gap.  All of it lies in front of key pos1 + 1.
+    const Runs runs(false, 0, window, ALL ? 0 : c.sinks, pos0, pos1);
+    const int lenA = runs.lenA, gap = runs.lo - lenA, keys = lenA + runs.lenB;
+    const int blocks = (keys + TILE_KEYS - 1) / TILE_KEYS, per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
+    // a row at p sees key v iff v <= p - gap and (v > p - gap - window or v < sink); one at p < 0 none
+    const int p = position(row), hi = p < 0 ? -1 : p - gap, sink = imax(lenA, (ALL ? 0 : c.sinks) - gap);
+    const int w0 = position(imin(row0 + 32 * wave, last_row)), w1 = position(imin(row0 + 32 * wave + 31, last_row));      // of the wavefront's first and last row
+    const int hi0 = w0 < 0 ? -1 : w0 - gap, hi1 = w1 < 0 ? -1 : w1 - gap;
 
-    const long kA = shared ? static_cast<long>(hk) * c.Np : static_cast<long>(unit) * c.Nk, kB = static_cast<long>(unit) * c.Nk + runs.lo;
-    const int8_t *vA = static_cast<const int8_t *>(shared ? c.Vp : c.V), *vB = static_cast<const int8_t *>(c.V);
-    const BufRsrc rKA = make_rsrc((shared ? c.Kp : c.K) + kA * D, runs.lenA * D), rVA = make_rsrc(vA + kA * V_ROW<D, VI8>, runs.lenA * V_ROW<D, VI8>),
-                  rSA = make_rsrc((shared ? c.sKp : c.sK) + kA, runs.lenA * 4);
-    const BufRsrc rKB = ALL ? rKA : make_rsrc(c.K + kB * D, runs.lenB * D), rVB = ALL ? rVA : make_rsrc(vB + kB * V_ROW<D, VI8>, runs.lenB * V_ROW<D, VI8>),
-                  rSB = ALL ? rSA : make_rsrc(c.sK + kB, runs.lenB * 4);
-
+    const int8_t *const K = ALL ? c.Kp : c.K, *const V = static_cast<const int8_t *>(ALL ? c.Vp : c.V);
+    const float *const sK = ALL ? c.sKp : c.sK;
+    const long first_key = static_cast<long>(unit) * (ALL ? c.Np : c.Nk);
+    const int seen_end = imax(0, pos1 + 1);
+    const BufRsrc rK = make_rsrc(K + first_key * D, seen_end * D), rV = make_rsrc(V + first_key * V_ROW<D, VI8>, seen_end * V_ROW<D, VI8>), rS = make_rsrc(sK + first_key, seen_end * 4);
     const Lane<D, VI8> lo(lane);
     const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]);
     auto stage = [&](int t, int slot) {                          // a quarter of the block to each wavefront
-        const bool inA = t < blocksA;
-        const int j0 = TILE_KEYS * (inA ? t : t - blocksA);
-        copy_pieces<KP>(pick(inA, rKA, rKB), kbuf + slot * KB + wave * KP * 1024, lo.gk, lo.gk, j0 * D + wave * KP * 1024);
-        copy_pieces<VP>(pick(inA, rVA, rVB), vbuf + slot * VB + wave * VP * 1024, lo.gv[0], lo.gv[1], j0 * V_ROW<D, VI8> + wave * VP * 1024);
-        if (wave == 3) lds_copy4(pick(inA, rSA, rSB), skbuf + slot * 256, 4 * lane, j0 * 4);
+        const lds_ptr kl = kbuf + slot * KB + wave * KP * 1024, vl = vbuf + slot * VB + wave * VP * 1024, sl = skbuf + slot * 256;
+        int v0 = TILE_KEYS * t;
+        if (v0 < lenA && v0 + TILE_KEYS > lenA) {                // the block with the seam: row by row
+            constexpr int K_ROWS = 1024 / D, V_ROWS = 1024 / V_ROW<D, VI8>;
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+                const int at = v0 + (wave * KP + i) * K_ROWS + lane / (D / 16);
+                lds_copy16(rK, kl + 1024 * i, lo.gk + (at < lenA ? 0 : gap * D), v0 * D + (wave * KP + i) * 1024);
+            }
+#pragma unroll
+            for (int i = 0; i < VP; ++i) {
+                const int at = v0 + (wave * VP + i) * V_ROWS + lane / (V_ROW<D, VI8> / 16);
+                lds_copy16(rV, vl + 1024 * i, lo.gv[i & 1] + 1024 * (i & 1) + (at < lenA ? 0 : gap * V_ROW<D, VI8>), v0 * V_ROW<D, VI8> + (wave * VP + (i & ~1)) * 1024);
+            }
+            if (wave == 3) lds_copy4(rS, sl, 4 * (lane + (v0 + lane < lenA ? 0 : gap)), v0 * 4);
+            return;
+        }
+        if (v0 >= lenA) v0 += gap;
+        copy_pieces<KP>(rK, kl, lo.gk, lo.gk, v0 * D + wave * KP * 1024);
+        copy_pieces<VP>(rV, vl, lo.gv[0], lo.gv[1], v0 * V_ROW<D, VI8> + wave * VP * 1024);
+        if (wave == 3) lds_copy4(rS, sl, 4 * lane, v0 * 4);
     };
     if (t0 < t1) stage(t0, 0);
 
@@ -423,28 +451,17 @@ __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, in
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
-    float unit_of_o = 1.0f;
-    if (VI8) unit_of_o = ALL || t0 < blocksA ? (shared ? c.sVp[hk] : c.sV[unit]) : c.sV[unit];
+    const float unit_of_o = VI8 ? (ALL ? c.sVp : c.sV)[unit] : 1.0f;
 
     wait_all_memory();
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-        const int slot = (t - t0) & 1;
+        const int slot = (t - t0) & 1, v0 = TILE_KEYS * t;
         if (t + 1 < t1) stage(t + 1, slot ^ 1);
-        const bool inA = t < blocksA;
-        const int j0 = TILE_KEYS * (inA ? t : t - blocksA);
-        if (VI8 && !ALL && t == blocksA && t > t0 && shared) {   // from the shared keys' scale of V to the own ones', once
-            const float f = unit_of_o / c.sV[unit];
-            unit_of_o = c.sV[unit];
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) st.o[dt][v] *= f;
-        }
         // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
-        const bool any = inA ? some : p1 >= j0 && (p0 - c.window < j0 + TILE_KEYS - 1 || j0 < sink);
-        const bool clear = inA ? every && j0 + TILE_KEYS <= runs.lenA : p0 >= j0 + TILE_KEYS - 1 && (p1 - c.window < j0 || j0 + TILE_KEYS <= sink);
-        const uint64_t seen = clear ? 0 : inA ? keys_seen((mine ? runs.lenA - 1 : -1) - j0, 0, 0) : keys_seen(p - j0, p - c.window + 1 - j0, sink - j0);
+        const bool any = hi1 >= v0 && (hi0 - window < v0 + TILE_KEYS - 1 || v0 < sink);
+        const bool clear = hi0 >= v0 + TILE_KEYS - 1 && (hi1 - window < v0 || v0 + TILE_KEYS <= sink);
+        const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
         if (any) tile_block<D, VI8>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, clear, seen, g, bias, st);
         wait_all_memory();                                       // my part of the next block has landed
         __syncthreads();                                         // everyone's has, and this one's place is free
