@@ -28,7 +28,7 @@ struct Call {
     const int *lens;                                             // null: Nk everywhere
     int B, Hkv, G, Nq, Nk, Np, window, sinks;                    // window <= Nk
     int rows, splits;                                            // rows of a unit; workgroups that share the keys of a unit
-    float *part_o;                                               // [unit][split][rows][d] and [unit][split][rows] (m, l), if splits > 1 or a merge follows
+    float *part_o;                                               // [unit][split][rows][d] and [unit][split][rows] (m, l): where parts go (null: straight to O)
     float2 *part_ml;
     void *O;
     int o_dtype;
@@ -131,12 +131,12 @@ __device__ __forceinline__ h8 v_operand(lds_ptr vs, unsigned v0, int dt, int key
 __device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 __device__ __forceinline__ uint64_t keys_seen(int hi, int from, int sink) { return below(hi + 1) & (~below(from) | below(sink)); }
 
-// N pieces of 1 KB, one after the other (N a power of two up to 8)
-template <int N> __device__ __forceinline__ void copy_pieces(const BufRsrc &r, lds_ptr lds, unsigned even, unsigned odd, int soff) {
-    if constexpr (N <= 4) lds_copy16_run<N>(r, lds, even, odd, soff);
+// N pieces of 1 KB, one after the other (N a power of two up to 8); NT: bytes that are read once
+template <int N, bool NT = false> __device__ __forceinline__ void copy_pieces(const BufRsrc &r, lds_ptr lds, unsigned even, unsigned odd, int soff) {
+    if constexpr (N <= 4) lds_copy16_run<N, NT>(r, lds, even, odd, soff);
     else {
-        copy_pieces<N / 2>(r, lds, even, odd, soff);
-        copy_pieces<N / 2>(r, lds + N / 2 * 1024, even, odd, soff + N / 2 * 1024);
+        copy_pieces<N / 2, NT>(r, lds, even, odd, soff);
+        copy_pieces<N / 2, NT>(r, lds + N / 2 * 1024, even, odd, soff + N / 2 * 1024);
     }
 }
 // Offset of a request that fetches nothing: past the end of any tensor (the scalar offset takes part in the range check), so the copy writes zeros.

@@ -38,33 +38,31 @@ __device__ __forceinline__ long row_of(const Call &c, bool all, int unit, int ro
 // ---- 32 rows against many keys: every wavefront for itself -------------------------------------------------------
 // The four wavefronts of a workgroup hold the same 32 rows and take every fourth tile of 32 keys each, with an online softmax of their own; they meet
 // once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
-// asks for the one that goes into its place before it computes.
+// asks for the one that goes into its place before it computes.  What bounds it is memory: 32 sequences x 8 heads on 4096 keys of d = 128 in 66.5 us, 6.1 TB/s.
 constexpr int FEW_WAVES = 4;
-template <int D, bool VI8> struct SmemFew {
-    static constexpr int ST = 3, KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
+template <int D, bool VI8, int ST> struct SmemFew {
+    static constexpr int KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
     union {
         struct {
             alignas(4096) int8_t k[FEW_WAVES][ST][KB];
             alignas(4096) int8_t v[FEW_WAVES][ST][VB];
             alignas(128) float sk[FEW_WAVES][ST][32];
         };
-        float o[FEW_WAVES][32][D];                               // when the loop is over
+        float o[FEW_WAVES][32][64];                              // when the loop is over: 64 columns at a time
     };
     float2 ml[FEW_WAVES][32];
 };
-static_assert(sizeof(SmemFew<128, false>) <= 160 * 1024, "LDS budget");
 
 // ALL: unit = key head, rows of the whole batch, the shared keys alone.  Otherwise unit = (sequence, key head), shared keys (if any) and its own.
-template <int D, bool VI8, bool ALL>
-__global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Call c, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ SmemFew<D, VI8> sm;
-    constexpr int KS = D / 32, DT = D / 32, ST = SmemFew<D, VI8>::ST, KB = SmemFew<D, VI8>::KB, VB = SmemFew<D, VI8>::VB;
+template <int D, bool VI8, bool ALL, int ST, bool NT>
+__device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, const Call &c, int block, int units, int row_tiles) {
+    constexpr int KS = D / 32, DT = D / 32, KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
     constexpr int PER_TILE = K_PIECES<D> + V_PIECES<D, VI8> + 1;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // the row tiles of one share of the keys run 8 apart: on one XCD
-    const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), rt = in8 >> 3;
+    const int in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), rt = in8 >> 3;
     const int unit = share / c.splits, split = share % c.splits;
     if (unit >= units) return;
     const int b = ALL ? 0 : unit / c.Hkv, hk = ALL ? unit : unit % c.Hkv;
@@ -91,8 +89,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
         const bool inA = t < tilesA;
         const int j0 = 32 * (inA ? t : t - tilesA);
         const bool real = t < t1;
-        copy_pieces<K_PIECES<D>>(pick(inA, rKA, rKB), kbuf + slot * KB, lo.gk, lo.gk, real ? j0 * D : NOTHING);
-        copy_pieces<V_PIECES<D, VI8>>(pick(inA, rVA, rVB), vbuf + slot * VB, lo.gv[0], lo.gv[1], real ? j0 * V_ROW<D, VI8> : NOTHING);
+        copy_pieces<K_PIECES<D>, NT>(pick(inA, rKA, rKB), kbuf + slot * KB, lo.gk, lo.gk, real ? j0 * D : NOTHING);
+        copy_pieces<V_PIECES<D, VI8>, NT>(pick(inA, rVA, rVB), vbuf + slot * VB, lo.gv[0], lo.gv[1], real ? j0 * V_ROW<D, VI8> : NOTHING);
         if (g == 0) lds_copy4(pick(inA, rSA, rSB), skbuf + slot * 128, 4 * r, real ? j0 * 4 : NOTHING);
     };
     const int first = t0 + wave;
@@ -205,38 +203,49 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 #pragma unroll
     for (int w = 0; w < FEW_WAVES; ++w) m_all = fmaxf(m_all, sm.ml[w][r].x);
     const float f = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_all) * unit_of_o;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int vq = 0; vq < 4; ++vq) {
-            // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
-            const int chunk = (8 * dt + 2 * vq + g) ^ (r & 7);
-            *reinterpret_cast<v4f *>(&sm.o[wave][r][4 * chunk]) = v4f{o[dt][4 * vq] * f, o[dt][4 * vq + 1] * f, o[dt][4 * vq + 2] * f, o[dt][4 * vq + 3] * f};
-        }
-    __syncthreads();
-    constexpr int TPR = D / 4;                                   // threads to a row
     const int valid = last_row - row0 + 1;
-    for (int at = tid; at < valid * TPR; at += 64 * FEW_WAVES) {
-        const int rr = at / TPR, cc = at % TPR;
-        float m = -INFINITY, ls = 0.0f;
-        v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int half = 0; half < D / 64; ++half) {
+        if (half) __syncthreads();
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, sm.ml[w][rr].x);
+        for (int dt = 0; dt < DT; ++dt)
+            if (dt >> 1 == half) {
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) {
-            const float2 x = sm.ml[w][rr];
-            ls += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - m);
-            s += *reinterpret_cast<const v4f *>(&sm.o[w][rr][4 * (cc ^ (rr & 7))]);
-        }
-        if (c.part_o) {
-            const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows + row0 + rr;
-            *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = s;
-            if (cc == 0) c.part_ml[pr] = float2{m, ls};
-        } else {
-            const float q = ls > 0.0f ? 1.0f / ls : 0.0f;        // a row that sees nothing: zeros
-            store4(c.O, c.o_dtype, row_of(c, ALL, unit, row0 + rr) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
+                for (int vq = 0; vq < 4; ++vq) {
+                    // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
+                    const int chunk = (8 * (dt & 1) + 2 * vq + g) ^ (r & 7);
+                    *reinterpret_cast<v4f *>(&sm.o[wave][r][4 * chunk]) = v4f{o[dt][4 * vq] * f, o[dt][4 * vq + 1] * f, o[dt][4 * vq + 2] * f, o[dt][4 * vq + 3] * f};
+                }
+            }
+        __syncthreads();
+        for (int at = tid; at < valid * 16; at += 64 * FEW_WAVES) {
+            const int rr = at / 16, cc = at % 16;
+            float m = -INFINITY, ls = 0.0f;
+            v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, sm.ml[w][rr].x);
+#pragma unroll
+            for (int w = 0; w < FEW_WAVES; ++w) {
+                const float2 x = sm.ml[w][rr];
+                ls += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - m);
+                s += *reinterpret_cast<const v4f *>(&sm.o[w][rr][4 * (cc ^ (rr & 7))]);
+            }
+            if (c.part_o) {
+                const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows + row0 + rr;
+                *reinterpret_cast<v4f *>(c.part_o + pr * D + 64 * half + 4 * cc) = s;
+                if (cc == 0 && half == 0) c.part_ml[pr] = float2{m, ls};
+            } else {
+                const float q = ls > 0.0f ? 1.0f / ls : 0.0f;    // a row that sees nothing: zeros
+                store4(c.O, c.o_dtype, row_of(c, ALL, unit, row0 + rr) * D + 64 * half + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
+            }
         }
     }
+}
+#endif
+template <int D, bool VI8, bool ALL, int ST, bool NT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Call c, int units, int row_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemFew<D, VI8, ST> sm;
+    few_rows_of_a_unit<D, VI8, ALL, ST, NT>(sm, c, blockIdx.x, units, row_tiles);
 #endif
 }
 
@@ -378,15 +387,14 @@ __device__ __forceinline__ void store_rows(lds_ptr stage, int lane, Val val, At 
 }
 #endif
 
-template <int D, bool VI8, bool ALL>
-__global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, int units, int row_tiles, int head_group) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ SmemTile<D, VI8> sm;
+template <int D, bool VI8, bool ALL>
+__device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call &c, int block, int units, int row_tiles, int head_group) {
     constexpr int DT = D / 32, KB = TILE_KEYS * D, VB = TILE_KEYS * V_ROW<D, VI8>, KP = KB / 4096, VP = VB / 4096;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
-    map_workgroup(blockIdx.x, units, row_tiles * c.splits, head_group, !ALL, unit, ord);
+    map_workgroup(block, units, row_tiles * c.splits, head_group, !ALL, unit, ord);
     const int rt = row_tiles - 1 - ord / c.splits, split = ord % c.splits;
     const int L = ALL ? c.Np : keys_of(c.lens, unit / c.Hkv, c.Nk), window = ALL ? c.Np : c.window;
     const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), row = imin(row0 + 32 * wave + r, last_row);
@@ -488,12 +496,34 @@ __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, in
     if (c.o_dtype == IFA_F32) store(float{});
     else if (c.o_dtype == IFA_F16) store(__half{});
     else store(__hip_bfloat16{});
+}
+#endif
+template <int D, bool VI8, bool ALL>
+__global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, int units, int row_tiles, int head_group) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemTile<D, VI8> sm;
+    tile_of_a_unit<D, VI8, ALL>(sm, c, blockIdx.x, units, row_tiles, head_group);
+#endif
+}
+
+// ---- shared keys and own keys in one launch --------------------------------------------------------------------------
+// The first `blocks` workgroups take the shared keys for the whole batch (TILE: in tiles of 128 rows, otherwise 32), the others every sequence's own: the former are bound by their
+// arithmetic, the latter by memory, and neither waits for the end of the other.
+template <int D, bool VI8, bool TILE>
+__global__ __launch_bounds__(256, 2) void cache_attention_both_kernel(Call shared, Call own, int blocks, int shared_tiles, int own_units, int own_tiles, int head_group) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ union {
+        SmemTile<D, VI8> tile;
+        SmemFew<D, VI8, 1> few;
+    } sm;
+    if (static_cast<int>(blockIdx.x) >= blocks) few_rows_of_a_unit<D, VI8, false, 1, false>(sm.few, own, blockIdx.x - blocks, own_units, own_tiles);
+    else if constexpr (TILE) tile_of_a_unit<D, VI8, true>(sm.tile, shared, blockIdx.x, shared.Hkv, shared_tiles, head_group);
+    else few_rows_of_a_unit<D, VI8, true, 1, false>(sm.few, shared, blockIdx.x, shared.Hkv, shared_tiles);
 #endif
 }
 
 // ---- the parts of a row joined -----------------------------------------------------------------------------------
-// `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.  P groups of D / 4 threads take every P-th part of a
-// row, each with a maximum of its own, and meet in LDS: what there is to wait for is a few loads in a row, not one for each part.
+// `shared` > 0: that many parts of the shared keys first (unit hk, row (b, i, g)), then `own` of the sequence's own.  P groups of D / 4 threads take every P-th part of a row, each with a maximum of its own, and meet in LDS: what there is to wait for is a few loads in a row, not one for each part.
 struct Parts {
     const float *o_shared, *o_own;
     const float2 *ml_shared, *ml_own;
@@ -507,9 +537,9 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(Call c, Parts
     const int cc = threadIdx.x % TPR, pg = threadIdx.x / TPR % P, in_block = threadIdx.x / (TPR * P);
     const long idx = static_cast<long>(blockIdx.x) * ROWS + in_block;
     const bool valid = idx < all_rows;
-    const int per = c.Nq * c.G, unit = static_cast<int>(idx / per), in = static_cast<int>(idx % per), b = unit / c.Hkv, hk = unit % c.Hkv, n = valid ? parts.shared + parts.own : 0;
-    const long s0 = static_cast<long>(hk) * parts.shared * c.B * per + static_cast<long>(b) * per + in, s_step = static_cast<long>(c.B) * per;
-    const long o0 = static_cast<long>(unit) * parts.own * per + in;
+    const int per = c.Nq * c.G, unit = static_cast<int>(idx / per), in = static_cast<int>(idx % per), n = valid ? parts.shared + parts.own : 0;
+    const long s_step = static_cast<long>(c.B) * per, s0 = static_cast<long>(unit % c.Hkv) * parts.shared * s_step + static_cast<long>(unit / c.Hkv) * per + in;
+    const long o0 = (static_cast<long>(unit) * parts.own - parts.shared) * per + in;
     float m = -INFINITY, l = 0.0f;
     v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int AT_ONCE = 4;
@@ -522,10 +552,10 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(Call c, Parts
             x[k] = float2{-INFINITY, 0.0f};
             y[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             if (i < n) {
-                const bool first = i < parts.shared;
-                const long at = first ? s0 + i * s_step : o0 + static_cast<long>(i - parts.shared) * per;
-                x[k] = (first ? parts.ml_shared : parts.ml_own)[at];
-                y[k] = *reinterpret_cast<const v4f *>((first ? parts.o_shared : parts.o_own) + at * D + 4 * cc);
+                const bool shared = i < parts.shared;
+                const long at = shared ? s0 + i * s_step : o0 + static_cast<long>(i) * per;
+                x[k] = (shared ? parts.ml_shared : parts.ml_own)[at];
+                y[k] = *reinterpret_cast<const v4f *>((shared ? parts.o_shared : parts.o_own) + at * D + 4 * cc);
             }
         }
         float m_new = m;
@@ -571,15 +601,20 @@ struct Plan {
     int shared, own;                       // parts of the shared keys taken for the whole batch (0: every sequence reads them), and of the own keys
     long rows_shared, rows_own;            // rows of parts: all units x parts x rows
     bool join() const { return shared > 0 || own > 1; }
-    long bytes(int d) const { return join() ? (rows_shared + rows_own) * (4L * d + 8) + 512 : 0; }
+    long bytes(int d) const { return (rows_shared + rows_own) * (4L * d + 8); }
 };
 constexpr int MOST_PARTS = 64;
 
-// Parts where there is less than a workgroup for each place on the chip (two to a CU, of the kernel for 32 rows one), as many as there are places, of at least 256 keys each.
-int parts_for(long rows_of_unit, long units, long keys) {
-    const long groups = units * ((rows_of_unit + TILE_ROWS - 1) / TILE_ROWS), places = rows_of_unit > 32 ? 512 : 256;
-    long parts = places / groups;
-    if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
+long row_tiles(bool few, long rows) { return few ? (rows + 31) / 32 : (rows + TILE_ROWS - 1) / TILE_ROWS; }
+// The kernel for 32 rows, whose wavefronts share the keys out among themselves, or tiles of 128.  Own keys: 32 rows as long as that leaves half of the CUs without one (us, 32 rows / 128, 8 key heads,
+// groups of 4, window 4096: 64 queries 20.8 / 22.6, 256 queries 41.6 / 34.7; 2 x 4 heads of d = 64, 300 queries, window 1000: 9.9 / 12.8).  Shared keys: the tiles read them once for
+// 128 rows of the batch (64 sequences x 4 rows on 8192 keys 43 / 30 in all).
+bool few_rows(bool all, long units, long rows) { return rows <= 32 || (!all && units * ((rows + 31) / 32) <= 128); }
+// Parts where there is less than a workgroup for each of `places`, as many as there are, of at least `least` keys each.  Under 512 keys the second launch that joins them costs more than it
+// gains (one sequence on 261 keys 6.2 us whole, 7.5 in two; 16 x 8 heads on 4096 of up to 16384 keys 39 in two parts each, 44 in four; one x 8 on 4096 12 in 32, 13 in 16).
+int parts_for(long places, long groups, long keys, long least) {
+    long parts = keys < 512 ? 1 : places / groups;
+    if (parts > keys / least) parts = keys / least;
     return static_cast<int>(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
 }
 
@@ -587,52 +622,75 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sink
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     Plan p = {};
     const long span = static_cast<long>(window) + imin(Nq, TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
-    p.own = parts_for(rows, units, keys);
-    if (Np > 0) {
+    const bool few = few_rows(false, units, rows);
+    p.own = parts_for(few ? 256 : 512, units * row_tiles(few, rows), keys, few ? 128 : 256);
+    // Few keys: every sequence reads the shared ones, too (2 sequences on 300 + 40 keys 6.2 us, with a launch for the parts 7.4; on 600 + 100 12.1 and 9.1)
+    if (Np > 0 && !(few && static_cast<long>(Np) + Nk < 512)) {
         const long all = rows * B;
-        p.shared = parts_for(all, Hkv, Np);
+        p.shared = parts_for(few ? 256 : 512, Hkv * row_tiles(few_rows(true, Hkv, all), all), Np, 256);
         p.rows_shared = Hkv * all * p.shared;
     }
-    p.rows_own = units * rows * p.own;
+    p.rows_own = p.join() ? units * rows * p.own : 0;
     return p;
 }
 
 template <int D, bool VI8>
 int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv;
-    const int8_t *const Kp = c.Kp;
-    Parts parts = {};
-    float *o = nullptr;
-    float2 *ml = nullptr;
-    if (plan.join()) {
-        o = static_cast<float *>(workspace);
-        ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
-        parts = {o, o + plan.rows_shared * D, ml, ml + plan.rows_shared, plan.shared, plan.own};
-    }
-    auto run = [&](auto all, Call k, int n_units) {
-        if (k.rows > 32) {
-            const int row_tiles = (k.rows + TILE_ROWS - 1) / TILE_ROWS, head_group = head_group_for(true, 0, 0);
-            const long grid = static_cast<long>(n_units) * row_tiles * k.splits;
-            hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, k, n_units, row_tiles, head_group);
+    float *const o = static_cast<float *>(workspace);
+    float2 *const ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
+    auto run = [&](auto all, const Call &k, int n_units) {
+        constexpr bool ALL = decltype(all)::value;
+        const bool few = few_rows(ALL, n_units, k.rows);
+        const int tiles = static_cast<int>(row_tiles(few, k.rows));
+        if (!few) {
+            const long grid = static_cast<long>(n_units) * tiles * k.splits;
+            hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, ALL>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, k, n_units, tiles, head_group_for(true, 0, 0));
             return;
         }
-        const int row_tiles = (k.rows + 31) / 32;
-        const long grid = (static_cast<long>(n_units) * k.splits + 7) / 8 * 8 * row_tiles;
-        hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, n_units, row_tiles);
+        const long grid = (static_cast<long>(n_units) * k.splits + 7) / 8 * 8 * tiles;
+        auto launch_few = [&](auto stages, auto nt) {
+            hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, ALL, decltype(stages)::value, decltype(nt)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, n_units, tiles);
+        };
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 2> two{};
+        if constexpr (ALL) launch_few(one, std::false_type{});
+        else {
+            // with the non-temporal hint where what is read once does not stay in the caches anyway: 32 x 8 heads on 4096 keys 67 us against 76, 64 x 8 on 512 26 / 28; 4 x 8 on 4096 (50 MB) the same
+            const long keys = imin(k.Nk, imin(k.window, k.Nk - k.sinks) + k.sinks);
+            const bool once = tiles == 1 && n_units * keys * (D + V_ROW<D, VI8>) > 64L << 20;
+            // One workgroup to a CU copies two tiles ahead; more of them fit with one (64 x 8 heads on 512 keys 26 us, with two 27; 16 x 8 on 4096 in 256 workgroups 41 and 39)
+            if (grid > 256) once ? launch_few(one, std::true_type{}) : launch_few(one, std::false_type{});
+            else once ? launch_few(two, std::true_type{}) : launch_few(two, std::false_type{});
+        }
     };
+    Call shared = {};
     if (plan.shared > 0) {
         Call k = c;
         k.rows = c.rows * c.B;
         k.splits = plan.shared;
         k.part_o = o, k.part_ml = ml;
-        run(std::true_type{}, k, c.Hkv);
-        c.Kp = nullptr, c.Np = 0;                                // (the own keys alone from here on)
+        c.Kp = nullptr, c.Np = 0;                                // the own keys alone
+        shared = k;
     }
     c.splits = plan.own;
     if (plan.join()) c.part_o = o + plan.rows_shared * D, c.part_ml = ml + plan.rows_shared;
-    run(std::false_type{}, c, units);
+    if (plan.shared > 0 && few_rows(false, units, c.rows)) {
+        const bool few = few_rows(true, c.Hkv, shared.rows);
+        const int shared_tiles = static_cast<int>(row_tiles(few, shared.rows)), own_tiles = static_cast<int>(row_tiles(true, c.rows));
+        const long blocks = few ? (static_cast<long>(c.Hkv) * shared.splits + 7) / 8 * 8 * shared_tiles : static_cast<long>(c.Hkv) * shared_tiles * shared.splits;
+        const long grid = blocks + (static_cast<long>(units) * c.splits + 7) / 8 * 8 * own_tiles;
+        auto both = [&](auto tile) {
+            hipLaunchKernelGGL((cache_attention_both_kernel<D, VI8, decltype(tile)::value>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, shared, c, static_cast<int>(blocks), shared_tiles,
+                               units, own_tiles, head_group_for(true, 0, 0));
+        };
+        few ? both(std::false_type{}) : both(std::true_type{});
+    } else {
+        if (plan.shared > 0) run(std::true_type{}, shared, c.Hkv);
+        run(std::false_type{}, c, units);
+    }
     if (plan.join()) {
-        c.Kp = Kp;
+        const Parts parts = {o, c.part_o, ml, c.part_ml, plan.shared, plan.own};
         const long all_rows = static_cast<long>(units) * c.rows;
         auto join = [&](auto p) {
             constexpr int P = decltype(p)::value, ROWS = 1024 / D / P;
@@ -653,7 +711,7 @@ int refuse(const Call &c, int d, const void *workspace, long workspace_bytes, co
         if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
     for (const void *p : {static_cast<const void *>(c.sQ), static_cast<const void *>(c.sK), static_cast<const void *>(c.sV), static_cast<const void *>(c.sKp), static_cast<const void *>(c.sVp), static_cast<const void *>(c.lens)})
         if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
-    if (plan.join()) {
+    if (plan.bytes(d)) {
         if (!workspace) return IFA_ERR_NULL;
         if (reinterpret_cast<uintptr_t>(workspace) & 255) return IFA_ERR_UNSUPPORTED;
         if (workspace_bytes < plan.bytes(d)) return IFA_ERR_WORKSPACE;

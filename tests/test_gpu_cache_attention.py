@@ -54,6 +54,11 @@ WINDOWS = [
     (1, 3, 1, 300, 300, 128, 129, 1, (290,)),
     (4, 1, 1, 2, 4, 64, 2, 1, (4, 3, 2, 1)),
     (1, 1, 1, 700, 700, 128, 256, 4, None),
+    (2, 8, 2, 200, 500, 64, 64, 100, (500, 333)),        # tiles of 128 rows: the seam between sinks and window inside a block, behind one, ...
+    (1, 16, 3, 170, 333, 128, 70, 64, (331,)),           # ... at its end
+    (3, 4, 4, 130, 130, 128, 40, 3, (130, 0, 77)),       # padded in front
+    (1, 12, 1, 400, 650, 64, 1, 1, None),
+    (2, 6, 4, 129, 700, 128, 10 ** 6, 0, (700, 650)),
     (9, 1, 5, 3, 64, 64, 7, 1, (64, 0, 1, 2, 3, 4, 31, 32, 33)),
 ]
 
@@ -78,6 +83,8 @@ PREFIXES = [
     (2, 1, 2, 70, 500, 300, 128, (300, 50)),             # more queries than own keys
     (7, 1, 1, 3, 32, 32, 64, (0, 1, 2, 3, 4, 31, 32)),
     (33, 2, 1, 1, 1500, 9, 128, None),
+    (4, 4, 4, 80, 600, 300, 64, (300, 0, 81, 200)),      # prompts behind a prefix: tiles of 128 rows for both
+    (3, 8, 2, 100, 70, 100, 128, (100, 99, 1)),
 ]
 
 
@@ -103,6 +110,19 @@ def test_what_no_query_sees_is_not_looked_at(ifa):
             s["v"][:, :, hidden] = bad
             s["sk"][:, :, hidden] = bad
             check(window(ifa, s, w, sinks, (L,)), clean, tol)
+
+
+def test_what_no_query_of_a_prompt_sees_is_not_looked_at(ifa):
+    """Chunks of a prompt (tiles of 128 rows): the same in front of the first query's window."""
+    s = ref.problem(3, 1, 16, 2, 160, 900, 64)
+    clean, tol = ref.attention(s, torch.float16, (880,), 100, 70)
+    hidden = torch.ones(900, dtype=torch.bool)
+    hidden[:70] = False
+    hidden[880 - 160 - 99:880] = False
+    for bad in (math.nan, math.inf):
+        s["v"][:, :, hidden] = bad
+        s["sk"][:, :, hidden] = bad
+        check(window(ifa, s, 100, 70, (880,)), clean, tol)
 
 
 def test_lengths_outside_the_buffer_count_as_the_nearer_end(ifa):
