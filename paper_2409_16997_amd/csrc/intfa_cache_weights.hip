@@ -23,7 +23,8 @@ struct WeightsCall {
     int B, Hkv, G, Nq, Nk;
     int parts;                                                   // of the keys, in the first pass
     int slices;                                                  // of the rows, in the second
-    float2 *stats;                                               // [part][B H Nq]: maximum (log2 units) and sum of a row over that part; then part 0: maximum, 1 / sum
+    float2 *stats;                                               // [part][B H Nq]: maximum (log2 units) and sum of a row over that part
+    float2 *rows_out;                                            // [B H Nq]: maximum + log2(sum) of a row (inf: it sees nothing) and s_Q log2(e); null with stored scores
     float *scores;                                               // [unit][rows][score_stride] in log2 units, or null
     long score_stride;
     float *sums;                                                 // [slice][unit][Nk], or null: straight to out
@@ -31,6 +32,15 @@ struct WeightsCall {
 };
 __device__ __forceinline__ long query_row(const WeightsCall &c, int unit, int row) {             // row (i, g) of unit (b, hk), in the order of Q
     return (static_cast<long>(unit) * c.G + row % c.G) * c.Nq + row / c.G;
+}
+
+// what the second pass takes of a row
+__device__ __forceinline__ float2 row_of_second_pass(float m, float sum, float sq) {
+    return float2{m == -INFINITY ? INFINITY : m + __builtin_amdgcn_logf(sum), sq * LOG2E};
+}
+[[maybe_unused]] __device__ __forceinline__ void write_stats(const WeightsCall &c, int units, int part, long row, float m, float sum) {
+    if (c.rows_out && c.parts == 1) c.rows_out[row] = row_of_second_pass(m, sum, c.sQ[row]);
+    else c.stats[static_cast<long>(part) * units * c.G * c.Nq + row] = float2{m, sum};
 }
 
 // ---- first pass: maximum and sum of 32 rows over a part of the keys, the wavefronts taking every fourth tile of 32 keys, each for itself -----------------
@@ -135,26 +145,122 @@ __global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(Weights
 #pragma unroll
         for (int w = 0; w < KW_WAVES; ++w)
             if (sm.ml[w][tid].x != -INFINITY) sum += sm.ml[w][tid].y * __builtin_amdgcn_exp2f(sm.ml[w][tid].x - m);
-        const long at = static_cast<long>(units) * rows * part + query_row(c, unit, row0 + tid);
-        c.stats[at] = float2{m, sum};
+        write_stats(c, units, part, query_row(c, unit, row0 + tid), m, sum);
     }
 #endif
 }
 
-// maximum and 1 / sum of a row from its parts; a row that sees nothing: 0 and 0, so that its weights are 0
+// ---- the same for tiles of 128 rows, which share the keys, 64 at a time, through LDS ------------------------------------------------
+// A score costs the vector unit a subtraction, s_K, half a maximum, s_Q and m, exp2 (16 cycles) and an addition, four times the 8 cycles of its products.  The maximum that
+// a sum refers to moves only when a block exceeds it by 2^8, a row by itself.
+constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
+template <int D> struct SmemRowTile {
+    alignas(4096) int8_t k[2][TILE_KEYS * D];
+    alignas(256) float sk[2][TILE_KEYS];
+};
+template <int D>
+__global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCall c, int units, int row_tiles, int head_group) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemRowTile<D> sm;
+    constexpr int KS = D / 32, KB = TILE_KEYS * D, KP = KB / 4096;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit, ord;
+    map_workgroup(blockIdx.x, units, row_tiles * c.parts, head_group, true, unit, ord);
+    const int rt = row_tiles - 1 - ord / c.parts, part = ord % c.parts;
+    const int rows = c.G * c.Nq, row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, rows - 1), row = imin(row0 + 32 * wave + r, last_row);
+    const int shift = keys_of(c.lens, unit / c.Hkv, c.Nk) - c.Nq;
+    const int keys = imax(0, shift + last_row / c.G + 1), p = shift + row / c.G;
+    const int w0 = shift + imin(row0 + 32 * wave, last_row) / c.G, w1 = shift + imin(row0 + 32 * wave + 31, last_row) / c.G;     // of the wavefront's first and last row
+    const int blocks = (keys + TILE_KEYS - 1) / TILE_KEYS, per = (blocks + c.parts - 1) / c.parts, t0 = part * per, t1 = imin(blocks, t0 + per);
+    const BufRsrc rK = make_rsrc(c.K + static_cast<long>(unit) * c.Nk * D, keys * D), rS = make_rsrc(c.sK + static_cast<long>(unit) * c.Nk, keys * 4);
+    const Lane<D, true> lo(lane);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]);
+    auto stage = [&](int t, int slot) {
+        copy_pieces<KP>(rK, kbuf + slot * KB + wave * KP * 1024, lo.gk, lo.gk, t * KB + wave * KP * 1024);
+        if (wave == 3) lds_copy4(rS, skbuf + slot * 256, 4 * lane, t * 256);
+    };
+    if (t0 < t1) stage(t0, 0);
+    const long qrow = query_row(c, unit, row);
+    v4i qf[KS];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
+    const float sq2 = c.sQ[qrow] * LOG2E;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));
+    v16i bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
+    asm volatile("" : "+v"(bias));
+    float m2 = -INFINITY, l = 0.0f;
+    wait_all_memory();
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int slot = (t - t0) & 1, j0 = TILE_KEYS * t;
+        if (t + 1 < t1) stage(t + 1, slot ^ 1);
+        if (w1 >= j0) {                                          // (wave-uniform)
+            float a[2][16];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                v16i acc = bias;
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk)
+                    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<LDS_AS const v4i *>(lds_xor(kbuf + slot * KB, 32 * kk, lo.k0) + 32 * mt * D), qf[kk], acc, 0, 0, 0);
+#pragma unroll
+                for (int vq = 0; vq < 4; ++vq) {
+                    const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 256 + 16 * g + 128 * mt + 32 * vq);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[4 * vq + e]) - ACC_BIAS_F) * skv[e];
+                }
+            }
+            if (w0 < j0 + TILE_KEYS - 1) {
+                const uint64_t seen = keys_seen(p - j0, 0, 0);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * (v >> 2) + (v & 3))))) a[mt][v] = -INFINITY;
+            }
+            float bmax = -INFINITY;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
+            const float top = pair_max(bmax) * sq2;
+            if (top > m2 + 8.0f) {
+                l *= __builtin_amdgcn_exp2f(m2 - top);           // exp2(-inf) = 0
+                m2 = top;
+            }
+            const float m = m2 == -INFINITY ? 0.0f : m2;
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[v & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][v], sq2, -m));
+            l += (s[0] + s[1]) + (s[2] + s[3]);
+        }
+        wait_all_memory();
+        __syncthreads();
+    }
+    l += swap32(l);
+    if (g == 0 && row0 + 32 * wave + r < rows) write_stats(c, units, part, qrow, m2, l);
+#endif
+}
+
 __device__ __forceinline__ float2 join_parts(const float2 *stats, long at, long step, int parts) {
     float m = -INFINITY, sum = 0.0f;
     for (int i = 0; i < parts; ++i) m = fmaxf(m, stats[at + i * step].x);
-    if (m == -INFINITY) return float2{0.0f, 0.0f};
     for (int i = 0; i < parts; ++i) {
         const float2 x = stats[at + i * step];
         if (x.x != -INFINITY) sum += x.y * __builtin_amdgcn_exp2f(x.x - m);
     }
-    return float2{m, 1.0f / sum};
+    return float2{m, sum};
 }
 __global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, long rows) {
     const long at = blockIdx.x * 256L + threadIdx.x;
-    if (at < rows) c.stats[at] = join_parts(c.stats, at, rows, c.parts);
+    if (at >= rows) return;
+    const float2 x = join_parts(c.stats, at, rows, c.parts);
+    c.rows_out[at] = row_of_second_pass(x.x, x.y, c.sQ[at]);
 }
 
 // ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
@@ -163,19 +269,27 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
     __shared__ float2 st[STORED_ROWS];
     const int unit = blockIdx.x / blocks, j = (blockIdx.x % blocks * 256 + threadIdx.x) * 4, rows = c.G * c.Nq;
     const int L = c.lens ? imax(0, imin(c.lens[unit / c.Hkv], c.Nk)) : c.Nk;
-    if (static_cast<int>(threadIdx.x) < rows)
-        st[threadIdx.x] = join_parts(c.stats, query_row(c, unit, threadIdx.x), static_cast<long>(units) * rows, c.parts);
+    if (static_cast<int>(threadIdx.x) < rows) {                  // maximum and 1 / sum; a row that sees nothing: 0 and 0, so that its weights are 0
+        const float2 x = join_parts(c.stats, query_row(c, unit, threadIdx.x), static_cast<long>(units) * rows, c.parts);
+        st[threadIdx.x] = x.x == -INFINITY ? float2{0.0f, 0.0f} : float2{x.x, 1.0f / x.y};
+    }
     __syncthreads();
     if (j >= c.Nk) return;
     v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
     if (j < L) {
         const float *x = c.scores + static_cast<long>(unit) * rows * c.score_stride + j;
-        for (int r = 0; r < rows; ++r) {
-            const float2 s = st[r];
+        for (int r0 = 0; r0 < rows; r0 += 4) {
             // Tiles of 32 keys are stored up to the last that a row sees, and its scores are -inf behind what it sees.
-            const v4f y = *reinterpret_cast<const v4f *>(x + r * c.score_stride);
+            v4f y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(y[e] - s.x), s.y, w[e]);
+            for (int k = 0; k < 4; ++k) y[k] = *reinterpret_cast<const v4f *>(x + imin(r0 + k, rows - 1) * c.score_stride);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 s = st[imin(r0 + k, rows - 1)];
+                const float f = r0 + k < rows ? s.y : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(y[k][e] - s.x), f, w[e]);
+            }
         }
     }
     const long at = static_cast<long>(unit) * c.Nk + j;
@@ -184,50 +298,55 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
         if (j + e < c.Nk) c.out[at + e] = (j + e < L ? w[e] : 0.0f) + (c.W ? c.W[at + e] : 0.0f);
 }
 
-// ---- second pass, scores computed again: 128 keys to a workgroup, a key to a lane ---------------------------------------------------------------
-// The rows go by in tiles of 64 queries of one head through LDS, shared by the four wavefronts of 32 keys; a slice of them per workgroup.
-constexpr int KW_ROWS = 64;
+// ---- second pass, scores computed again: 256 keys to a workgroup, a key to a lane ---------------------------------------------------------------
+// The rows go by in tiles of 64 queries of one head through LDS, shared by the four wavefronts of 64 keys (two operands of K in registers, so that what is read of the rows counts
+// twice); a slice of them per workgroup.  The vector unit's part of a score: s_Q s_K, the subtraction of the start value, their product less the row's maximum + log2(sum), exp2 and the
+// addition.  (Maximum and log2 in one number: it rounds by 2^-24 of itself, as scores do, and the rows' errors do not add up.)
+constexpr int KW_ROWS = 64, KW_KEYS = 256;
 template <int D> struct SmemKeys {
     alignas(4096) int8_t q[2][KW_ROWS * D];
-    alignas(256) float sq[2][KW_ROWS];
-    alignas(256) float2 ml[2][KW_ROWS];
+    alignas(256) float2 row[2][KW_ROWS];
 };
 template <int D>
-__global__ __launch_bounds__(256) void key_weights_keys_kernel(WeightsCall c, int units, int key_tiles) {
+__global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c, int units, int key_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemKeys<D> sm;
-    constexpr int KS = D / 32, PIECES = KW_ROWS * D / 4096;      // copies of a wavefront to a tile
+    constexpr int KS = D / 32, QB = KW_ROWS * D, PIECES = QB / 4096;             // copies of a wavefront to a tile
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kt = blockIdx.x % key_tiles, us = blockIdx.x / key_tiles, unit = us / c.slices, slice = us % c.slices;     // (the first keys, which most rows see, start first)
-    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
-    const int j0 = 128 * kt, j = j0 + 32 * wave + r, shift = L - c.Nq;
+    // the workgroups of a unit on one XCD as far as units go round; the first keys, which most rows see, first
+    const int per_unit = key_tiles * c.slices, x = blockIdx.x & 7, s = blockIdx.x >> 3;
+    const int unit = s / per_unit * 8 + x, kt = s % per_unit / c.slices, slice = s % c.slices;
+    if (unit >= units) return;
+    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk), shift = L - c.Nq;
+    const int j0 = KW_KEYS * kt, jw = j0 + 64 * wave;
     const int i0 = imax(0, j0 - shift);                          // the first query that sees any of the keys
     const int per_head = j0 < L && i0 < c.Nq ? (c.Nq - i0 + KW_ROWS - 1) / KW_ROWS : 0, total = per_head * c.G;
     const int per = (total + c.slices - 1) / c.slices, t0 = slice * per, t1 = imin(total, t0 + per);
-    float sum = 0.0f;
+    float sum[2] = {0.0f, 0.0f};
     if (t0 < t1) {
         const long kb = static_cast<long>(unit) * c.Nk;
-        v4i kop[KS];                                             // (keys at or beyond L: zeros, left out at the end)
+        v4i kop[2][KS];                                          // (keys at or beyond L: zeros, left out at the end)
+        float sk[2];
 #pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-            v4i x = {0, 0, 0, 0};
-            if (j < L) x = *reinterpret_cast<const v4i *>(c.K + (kb + j) * D + 32 * kk + 16 * g);
-            kop[kk] = x;
+        for (int h = 0; h < 2; ++h) {
+            const int j = jw + 32 * h + r;
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) {
+                v4i y = {0, 0, 0, 0};
+                if (j < L) y = *reinterpret_cast<const v4i *>(c.K + (kb + j) * D + 32 * kk + 16 * g);
+                kop[h][kk] = y;
+            }
+            sk[h] = j < L ? c.sK[kb + j] : 0.0f;
         }
-        const float sk = j < L ? c.sK[kb + j] : 0.0f;
         const Lane<D, true> lo(lane);
-        const lds_ptr qbuf = (lds_ptr)(&sm.q[0][0]), sqbuf = (lds_ptr)(&sm.sq[0][0]), mlbuf = (lds_ptr)(&sm.ml[0][0]);
+        const lds_ptr qbuf = (lds_ptr)(&sm.q[0][0]), rbuf = (lds_ptr)(&sm.row[0][0]);
         auto stage = [&](int t, int slot) {
-            const int head = t / per_head, i = i0 + t % per_head * KW_ROWS;
+            const int head = t / per_head, i = i0 + t % per_head * KW_ROWS, rows = imin(c.Nq - i, KW_ROWS);
             const long row = (static_cast<long>(unit) * c.G + head) * c.Nq + i;
-            const int rows = c.Nq - i;                           // (more than a tile is no harm: the copy has 64)
-            const BufRsrc rQ = make_rsrc(c.Q + row * D, imin(rows, KW_ROWS) * D), rS = make_rsrc(c.sQ + row, imin(rows, KW_ROWS) * 4),
-                          rM = make_rsrc(c.stats + row, imin(rows, KW_ROWS) * 8);
-            copy_pieces<PIECES>(rQ, qbuf + slot * (KW_ROWS * D) + wave * PIECES * 1024, lo.gk, lo.gk, wave * PIECES * 1024);
-            if (wave == 0) lds_copy4(rS, sqbuf + slot * 256, 4 * lane, 0);
-            if (wave == 1) lds_copy4(rM, mlbuf + slot * 512, 4 * lane, 0);
-            if (wave == 2) lds_copy4(rM, mlbuf + slot * 512 + 256, 4 * lane, 256);
+            const BufRsrc rQ = make_rsrc(c.Q + row * D, rows * D), rM = make_rsrc(c.rows_out + row, rows * 8);
+            copy_pieces<PIECES>(rQ, qbuf + slot * QB + wave * PIECES * 1024, lo.gk, lo.gk, wave * PIECES * 1024);
+            if (wave < 2) lds_copy4(rM, rbuf + slot * 512 + 256 * wave, 4 * lane, 256 * wave);
         };
         v16i bias;
 #pragma unroll
@@ -240,40 +359,56 @@ __global__ __launch_bounds__(256) void key_weights_keys_kernel(WeightsCall c, in
             const int slot = (t - t0) & 1;
             if (t + 1 < t1) stage(t + 1, slot ^ 1);
             const int i = i0 + t % per_head * KW_ROWS;
-            const bool masked = shift + i < j0 + 127 || i + KW_ROWS > c.Nq;      // a query that does not see all of the keys, or none there
 #pragma unroll
-            for (int h = 0; h < KW_ROWS / 32; ++h) {
+            for (int q = 0; q < KW_ROWS / 32; ++q) {
+                const int p0 = shift + i + 32 * q;               // position of the first of these queries
+                if (p0 + 31 < jw || i + 32 * q >= c.Nq) continue;                // (wave-uniform) none sees any of the wavefront's keys
                 v4i qop[KS];
+                v4f row[4][2];
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk) qop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(qbuf + slot * (KW_ROWS * D), 32 * kk, lo.k0) + 32 * h * D);
-                v16i acc = bias;
+                for (int kk = 0; kk < KS; ++kk) qop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(qbuf + slot * QB, 32 * kk, lo.k0) + 32 * q * D);
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(qop[kk], kop[kk], acc, 0, 0, 0);
+                for (int vq = 0; vq < 4; ++vq)
 #pragma unroll
-                for (int vq = 0; vq < 4; ++vq) {
-                    const v4f sq = *reinterpret_cast<LDS_AS const v4f *>(sqbuf + slot * 256 + 128 * h + 32 * vq + 16 * g);
-                    const v4f ma = *reinterpret_cast<LDS_AS const v4f *>(mlbuf + slot * 512 + 256 * h + 64 * vq + 32 * g);
-                    const v4f mb = *reinterpret_cast<LDS_AS const v4f *>(mlbuf + slot * 512 + 256 * h + 64 * vq + 32 * g + 16);
-                    const float m[4] = {ma[0], ma[2], mb[0], mb[2]}, rl[4] = {ma[1], ma[3], mb[1], mb[3]};
+                    for (int e = 0; e < 2; ++e) row[vq][e] = *reinterpret_cast<LDS_AS const v4f *>(rbuf + slot * 512 + 256 * q + 64 * vq + 32 * g + 16 * e);
+                const bool masked = p0 < jw + 63 || i + 32 * q + 32 > c.Nq;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x = __builtin_fmaf((__int_as_float(acc[4 * vq + e]) - ACC_BIAS_F) * sk, sq[e] * LOG2E, -m[e]);
-                        const int q = i + 32 * h + 8 * vq + 4 * g + e;
-                        if (masked && (q + shift < j || q >= c.Nq)) x = -INFINITY;
-                        sum = __builtin_fmaf(__builtin_amdgcn_exp2f(x), rl[e], sum);
+                for (int h = 0; h < 2; ++h) {
+                    v16i acc = bias;
+#pragma unroll
+                    for (int kk = 0; kk < KS; ++kk) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(qop[kk], kop[h][kk], acc, 0, 0, 0);
+                    float y[16];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const v4f &x4 = row[v >> 2][(v & 3) >> 1];
+                        y[v] = __builtin_fmaf(__int_as_float(acc[v]) - ACC_BIAS_F, sk[h] * x4[2 * (v & 1) + 1], -x4[2 * (v & 1)]);
                     }
+                    if (masked) {
+                        // query 32 q + k counts iff k >= first (it sees the key) and k < end
+                        const int first = jw + 32 * h + r - p0, end = c.Nq - i - 32 * q;
+                        const uint32_t seen = static_cast<uint32_t>(below(end) & ~below(first)) >> (4 * g);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if (!(seen & (1u << (8 * (v >> 2) + (v & 3))))) y[v] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sum[h] += __builtin_amdgcn_exp2f(y[v]);
                 }
             }
             wait_all_memory();
             __syncthreads();
         }
     }
-    sum += swap32(sum);
-    if (g == 0 && j < c.Nk) {
-        const long at = static_cast<long>(unit) * c.Nk + j;
-        if (j >= L) sum = 0.0f;
-        if (c.sums) c.sums[static_cast<long>(slice) * units * c.Nk + at] = sum;
-        else c.out[at] = sum + (c.W ? c.W[at] : 0.0f);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int j = jw + 32 * h + r;
+        float w = sum[h] + swap32(sum[h]);
+        if (g == 0 && j < c.Nk) {
+            const long at = static_cast<long>(unit) * c.Nk + j;
+            if (j >= L) w = 0.0f;
+            if (c.sums) c.sums[static_cast<long>(slice) * units * c.Nk + at] = w;
+            else c.out[at] = w + (c.W ? c.W[at] : 0.0f);
+        }
     }
 #endif
 }
@@ -288,26 +423,28 @@ __global__ __launch_bounds__(256) void key_weights_add_kernel(WeightsCall c, lon
 // ---- host --------------------------------------------------------------------------------------------------------
 struct Plan {
     int parts, slices;
-    bool stored;
-    long stats, scores, sums;              // bytes
+    bool stored, few;
+    long stats, rows, scores, sums;        // bytes
     long stride;                           // of a row of scores
-    long bytes() const { return stats + scores + sums; }
+    long bytes() const { return stats + rows + scores + sums; }
 };
 long up(long n) { return (n + 255) / 256 * 256; }
 Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
-    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq, tiles = (rows + 31) / 32;
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     Plan p = {};
-    long parts = (1024 + units * tiles - 1) / (units * tiles);
-    if (parts > (Nk + 511) / 512) parts = (Nk + 511) / 512;
-    p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
-    p.stats = up(units * rows * p.parts * 8);
     p.stored = rows <= STORED_ROWS;
+    p.few = rows <= 32 || units * ((rows + 31) / 32) <= 128;
+    long parts = p.few ? (1024 + units * ((rows + 31) / 32) - 1) / (units * ((rows + 31) / 32)) : 1024 / (units * ((rows + TILE_ROWS - 1) / TILE_ROWS));
+    if (parts > Nk / 512) parts = Nk / 512;
+    p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    p.stats = p.parts > 1 || p.stored ? up(units * rows * p.parts * 8) : 0;
     p.stride = (Nk + 31L) / 32 * 32;
     if (p.stored) {
         p.scores = up(units * rows * p.stride * 4);
         p.slices = 1;
     } else {
-        const long groups = units * ((Nk + 127) / 128), most = G * ((Nq + KW_ROWS - 1L) / KW_ROWS);
+        p.rows = up(units * rows * 8);
+        const long groups = units * ((Nk + KW_KEYS - 1) / KW_KEYS), most = G * ((Nq + KW_ROWS - 1L) / KW_ROWS);
         long slices = (1024 + groups - 1) / groups;
         if (slices > most) slices = most;
         p.slices = static_cast<int>(slices < 1 ? 1 : slices > 64 ? 64 : slices);
@@ -317,17 +454,23 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
 }
 
 template <int D> int launch(WeightsCall c, const Plan &plan, hipStream_t st) {
-    const int units = c.B * c.Hkv, row_tiles = (c.G * c.Nq + 31) / 32;
-    const long rows = static_cast<long>(units) * c.G * c.Nq;
-    const long grid = (static_cast<long>(units) * c.parts + 7) / 8 * 8 * row_tiles;
-    hipLaunchKernelGGL((key_weights_rows_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+    const int units = c.B * c.Hkv, unit_rows = c.G * c.Nq;
+    const long rows = static_cast<long>(units) * unit_rows;
+    if (plan.few) {
+        const int row_tiles = (unit_rows + 31) / 32;
+        const long grid = (static_cast<long>(units) * c.parts + 7) / 8 * 8 * row_tiles;
+        hipLaunchKernelGGL((key_weights_rows_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+    } else {
+        const int row_tiles = (unit_rows + TILE_ROWS - 1) / TILE_ROWS;
+        hipLaunchKernelGGL((key_weights_row_tiles_kernel<D>), dim3(static_cast<unsigned>(static_cast<long>(units) * row_tiles * c.parts)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
+    }
     if (plan.stored) {
         const int blocks = (c.Nk + 1023) / 1024;
         hipLaunchKernelGGL(key_weights_stored_kernel, dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, units, blocks);
     } else {
-        hipLaunchKernelGGL(key_weights_join_kernel, dim3(static_cast<unsigned>((rows + 255) / 256)), dim3(256), 0, st, c, rows);
-        const int key_tiles = (c.Nk + 127) / 128;
-        hipLaunchKernelGGL((key_weights_keys_kernel<D>), dim3(static_cast<unsigned>(key_tiles) * units * c.slices), dim3(256), 0, st, c, units, key_tiles);
+        if (c.parts > 1) hipLaunchKernelGGL(key_weights_join_kernel, dim3(static_cast<unsigned>((rows + 255) / 256)), dim3(256), 0, st, c, rows);
+        const int key_tiles = (c.Nk + KW_KEYS - 1) / KW_KEYS;
+        hipLaunchKernelGGL((key_weights_keys_kernel<D>), dim3(static_cast<unsigned>(key_tiles) * ((units + 7) / 8 * 8) * c.slices), dim3(256), 0, st, c, units, key_tiles);
         if (c.sums) {
             const long n = static_cast<long>(units) * c.Nk;
             hipLaunchKernelGGL(key_weights_add_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, c, n);
@@ -495,9 +638,10 @@ extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, con
     c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.parts = plan.parts, c.slices = plan.slices;
     char *const ws = static_cast<char *>(workspace);
     c.stats = reinterpret_cast<float2 *>(ws);
+    c.rows_out = plan.stored ? nullptr : reinterpret_cast<float2 *>(ws + plan.stats);
     c.scores = plan.stored ? reinterpret_cast<float *>(ws + plan.stats) : nullptr;
     c.score_stride = plan.stride;
-    c.sums = plan.sums ? reinterpret_cast<float *>(ws + plan.stats + plan.scores) : nullptr;
+    c.sums = plan.sums ? reinterpret_cast<float *>(ws + plan.stats + plan.rows) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return d == 128 ? launch<128>(c, plan, st) : launch<64>(c, plan, st);
 }
