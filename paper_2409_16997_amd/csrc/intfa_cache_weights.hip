@@ -44,14 +44,14 @@ __device__ __forceinline__ float2 row_of_second_pass(float m, float sum, float s
 }
 
 // ---- first pass: maximum and sum of 32 rows over a part of the keys, the wavefronts taking every fourth tile of 32 keys, each for itself -----------------
-constexpr int KW_WAVES = 4, KW_ST = 4;
+constexpr int KW_WAVES = 4, KW_ST = 2;
 template <int D> struct SmemRows {
     alignas(4096) int8_t k[KW_WAVES][KW_ST][32 * D];
     alignas(128) float sk[KW_WAVES][KW_ST][32];
     float2 ml[KW_WAVES][32];
 };
 
-template <int D>
+template <int D, bool NT>
 __global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(WeightsCall c, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemRows<D> sm;
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(Weights
     const Lane<D, true> lo(lane);
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]);
     auto stage = [&](int t, int slot) {
-        copy_pieces<K_PIECES<D>>(rK, kbuf + slot * KB, lo.gk, lo.gk, t < t1 ? 32 * t * D : NOTHING);
+        copy_pieces<K_PIECES<D>, NT>(rK, kbuf + slot * KB, lo.gk, lo.gk, t < t1 ? 32 * t * D : NOTHING);
         if (g == 0) lds_copy4(rS, skbuf + slot * 128, 4 * r, t < t1 ? 128 * t : NOTHING);
     };
     const int first = t0 + wave;
@@ -247,32 +247,51 @@ __global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCa
 #endif
 }
 
-__device__ __forceinline__ float2 join_parts(const float2 *stats, long at, long step, int parts) {
+// parts first, first + step, ... of a row, eight loads at a time
+__device__ __forceinline__ float2 join_parts(const float2 *stats, long stride, int parts, int first, int step) {
     float m = -INFINITY, sum = 0.0f;
-    for (int i = 0; i < parts; ++i) m = fmaxf(m, stats[at + i * step].x);
-    for (int i = 0; i < parts; ++i) {
-        const float2 x = stats[at + i * step];
-        if (x.x != -INFINITY) sum += x.y * __builtin_amdgcn_exp2f(x.x - m);
+    for (int i0 = first; i0 < parts; i0 += 8 * step) {
+        float2 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            x[k] = float2{-INFINITY, 0.0f};
+            if (i0 + k * step < parts) x[k] = stats[(i0 + k * step) * stride];
+        }
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m_new = fmaxf(m_new, x[k].x);
+        if (m_new == -INFINITY) continue;
+        sum *= __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += x[k].y * __builtin_amdgcn_exp2f(x[k].x - m);
     }
     return float2{m, sum};
 }
 __global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, long rows) {
     const long at = blockIdx.x * 256L + threadIdx.x;
     if (at >= rows) return;
-    const float2 x = join_parts(c.stats, at, rows, c.parts);
+    const float2 x = join_parts(c.stats + at, rows, c.parts, 0, 1);
     c.rows_out[at] = row_of_second_pass(x.x, x.y, c.sQ[at]);
 }
 
 // ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
 constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128)
-__global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, int units, int blocks) {
+__global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, int units, int blocks, bool whole) {
     __shared__ float2 st[STORED_ROWS];
     const int unit = blockIdx.x / blocks, j = (blockIdx.x % blocks * 256 + threadIdx.x) * 4, rows = c.G * c.Nq;
     const int L = c.lens ? imax(0, imin(c.lens[unit / c.Hkv], c.Nk)) : c.Nk;
-    if (static_cast<int>(threadIdx.x) < rows) {                  // maximum and 1 / sum; a row that sees nothing: 0 and 0, so that its weights are 0
-        const float2 x = join_parts(c.stats, query_row(c, unit, threadIdx.x), static_cast<long>(units) * rows, c.parts);
-        st[threadIdx.x] = x.x == -INFINITY ? float2{0.0f, 0.0f} : float2{x.x, 1.0f / x.y};
+    static_assert(STORED_ROWS * 16 == 256, "16 lanes to a row");
+    const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
+    float2 x = row < rows ? join_parts(c.stats + query_row(c, unit, row), static_cast<long>(units) * rows, c.parts, lane, 16) : float2{-INFINITY, 0.0f};
+#pragma unroll
+    for (int s = 8; s; s >>= 1) {
+        const float2 y = {__shfl_xor(x.x, s), __shfl_xor(x.y, s)};
+        const float m = fmaxf(x.x, y.x), at = m == -INFINITY ? 0.0f : m;
+        x = float2{m, x.y * __builtin_amdgcn_exp2f(x.x - at) + y.y * __builtin_amdgcn_exp2f(y.x - at)};
     }
+    // maximum and 1 / sum; a row that sees nothing: 0 and 0, so that its weights are 0
+    if (lane == 0) st[row] = x.x == -INFINITY ? float2{0.0f, 0.0f} : float2{x.x, 1.0f / x.y};
     __syncthreads();
     if (j >= c.Nk) return;
     v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -293,6 +312,14 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
         }
     }
     const long at = static_cast<long>(unit) * c.Nk + j;
+    if (whole) {                                                 // rows of W of whole 16 bytes
+        v4f old = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (c.W) old = *reinterpret_cast<const v4f *>(c.W + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) old[e] = (j + e < L ? w[e] : 0.0f) + old[e];
+        *reinterpret_cast<v4f *>(c.out + at) = old;
+        return;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (j + e < c.Nk) c.out[at + e] = (j + e < L ? w[e] : 0.0f) + (c.W ? c.W[at + e] : 0.0f);
@@ -434,7 +461,7 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
     Plan p = {};
     p.stored = rows <= STORED_ROWS;
     p.few = rows <= 32 || units * ((rows + 31) / 32) <= 128;
-    long parts = p.few ? (1024 + units * ((rows + 31) / 32) - 1) / (units * ((rows + 31) / 32)) : 1024 / (units * ((rows + TILE_ROWS - 1) / TILE_ROWS));
+    long parts = p.few ? 1024 / (units * ((rows + 31) / 32)) : 1024 / (units * ((rows + TILE_ROWS - 1) / TILE_ROWS));
     if (parts > Nk / 512) parts = Nk / 512;
     p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
     p.stats = p.parts > 1 || p.stored ? up(units * rows * p.parts * 8) : 0;
@@ -459,14 +486,18 @@ template <int D> int launch(WeightsCall c, const Plan &plan, hipStream_t st) {
     if (plan.few) {
         const int row_tiles = (unit_rows + 31) / 32;
         const long grid = (static_cast<long>(units) * c.parts + 7) / 8 * 8 * row_tiles;
-        hipLaunchKernelGGL((key_weights_rows_kernel<D>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+        // with the non-temporal hint where K is read once and does not stay in the caches anyway (16 x 8 heads on up to 16384 keys 45.0 us against 47.4)
+        const bool once = plan.stored && static_cast<long>(units) * c.Nk * D > 64L << 20;
+        if (once) hipLaunchKernelGGL((key_weights_rows_kernel<D, true>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+        else hipLaunchKernelGGL((key_weights_rows_kernel<D, false>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
     } else {
         const int row_tiles = (unit_rows + TILE_ROWS - 1) / TILE_ROWS;
         hipLaunchKernelGGL((key_weights_row_tiles_kernel<D>), dim3(static_cast<unsigned>(static_cast<long>(units) * row_tiles * c.parts)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
     }
     if (plan.stored) {
         const int blocks = (c.Nk + 1023) / 1024;
-        hipLaunchKernelGGL(key_weights_stored_kernel, dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, units, blocks);
+        const bool whole = c.Nk % 4 == 0 && ifa_aligned16(c.W) && ifa_aligned16(c.out);
+        hipLaunchKernelGGL(key_weights_stored_kernel, dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, units, blocks, whole);
     } else {
         if (c.parts > 1) hipLaunchKernelGGL(key_weights_join_kernel, dim3(static_cast<unsigned>((rows + 255) / 256)), dim3(256), 0, st, c, rows);
         const int key_tiles = (c.Nk + KW_KEYS - 1) / KW_KEYS;

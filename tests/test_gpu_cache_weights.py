@@ -34,6 +34,9 @@ WEIGHTS = [
     (2, 2, 3, 200, 200, 128, (200, 130)),                # prompts, one padded in front
     (1, 1, 1, 64, 5000, 64, (4999,)),
     (1, 1, 2, 700, 900, 128, None),
+    (2, 8, 2, 150, 1200, 128, (1200, 700)),              # tiles of 128 rows, the keys in parts
+    (1, 20, 3, 80, 200, 64, (190,)),                     # ... in one
+    (2, 1, 4, 1, 20000, 64, (20000, 19999)),             # many parts of stored scores
     (5, 1, 1, 31, 31, 128, (31, 30, 1, 0, 16)),
 ]
 
