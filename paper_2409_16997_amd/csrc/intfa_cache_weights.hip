@@ -6,6 +6,7 @@
 // All sums are in a fixed order (no atomics on floating point values): equal calls give equal results.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "intfa.h"
 #include "intfa_internal.h"
@@ -521,8 +522,8 @@ int refuse_sizes(int B, int H, int Hkv, int Nq, int Nk, int d) {
 }
 
 // ---- eviction -----------------------------------------------------------------------------------------------------
-// One workgroup to a key head finds the weight of the last key that stays (radix selection, 11 bits at a time, over keys that are read from the caches again
-// each time) and writes the list of those that do, in order; a second launch moves the rows.
+// One workgroup to a key head finds the weight of the last key that stays (radix selection, 11 bits at a time) and writes the list of those that do, in order; a second launch moves the
+// rows.  What bounds the pair is memory: 16 sequences x 8 heads, 4096 of 16384 keys of d = 128 with fp16 V, 421 MB moved.
 struct EvictCall {
     const int8_t *K, *V;
     const float *sK, *W;
@@ -532,7 +533,7 @@ struct EvictCall {
     float *sK_out, *W_out;
     int *index, *lens_out;
 };
-constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64, BINS = 2048;
+constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64, SEL_ROUND = 4 * SEL_THREADS, BINS = 2048;
 
 // Larger weight, larger number; -0 is 0, a NaN is below everything
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -541,6 +542,9 @@ __device__ __forceinline__ uint32_t order_of(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// The keys go by in rounds of 4096: wavefront w has 256 of them in a row, its lanes 64 at a time.  ROUNDS: of buffers of at most so many rounds the weights are read once and stay in
+// registers; 0: longer ones are read again each time (from the caches: 4 bytes a key).
+template <int ROUNDS>
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) {
     __shared__ uint32_t bins[BINS];
     __shared__ uint32_t wave_total[SEL_WAVES];
@@ -556,16 +560,49 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
     }
     const float *const W = c.W + static_cast<long>(unit) * c.Nk;
     const int first = c.sinks, last = n - c.recent;              // the keys that are chosen from: [first, last)
+    const int mine = wave * 256 + lane;                          // (of a round: and 64, 128, 192 further on)
+    uint32_t kept[ROUNDS > 0 ? ROUNDS : 1][4];
+    if constexpr (ROUNDS > 0) {
+        float w[ROUNDS][4];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = i * SEL_ROUND + mine + 64 * e;
+                w[i][e] = j < n ? W[j] : 0.0f;
+            }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kept[i][e] = order_of(w[i][e]);
+    }
+    // f(round, e, key, order of its weight) for every place of a round; all of them, so that wavefronts stay together
+    auto rounds = [&](auto f, auto after) {
+        auto one = [&](int i, int slot) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = i * SEL_ROUND + mine + 64 * e;
+                f(e, j, ROUNDS > 0 ? kept[slot][e] : j < n ? order_of(W[j]) : 0u);
+            }
+            after(i);
+        };
+        if constexpr (ROUNDS > 0) {
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i)
+                if (i * SEL_ROUND < n) one(i, i);
+        } else
+            for (int i = 0; i * SEL_ROUND < n; ++i) one(i, 0);
+    };
     uint32_t want = c.keep - c.sinks - c.recent, prefix = 0, mask = 0;
+    const bool none = want == 0;
     // 11 + 11 + 10 bits from the top: the digit in which the want-th largest lies
-    for (int pass = 0; pass < 3 && want; ++pass) {
+    for (int pass = 0; pass < 3 && !none; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
         for (int i = tid; i < BINS; i += SEL_THREADS) bins[i] = 0;
         __syncthreads();
-        for (int j = first + tid; j < last; j += SEL_THREADS) {
-            const uint32_t u = order_of(W[j]);
-            if ((u & mask) == prefix) atomicAdd(&bins[(u >> shift) & ((1u << width) - 1)], 1u);
-        }
+        rounds([&](int, int j, uint32_t u) {
+            if (j >= first && j < last && (u & mask) == prefix) atomicAdd(&bins[(u >> shift) & ((1u << width) - 1)], 1u);
+        }, [](int) {});
         __syncthreads();
         // from the top bin down: thread t has bins 2047 - 2 t and the one below
         const int b0 = BINS - 1 - 2 * tid;
@@ -587,60 +624,77 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
         mask |= ((1u << width) - 1) << shift;
         want = found[1];
     }
-    // `prefix` is the order of the last weight that stays, `want` how many of those equal to it do: the first ones.  (want = 0: none is chosen.)
-    const bool none = c.keep == c.sinks + c.recent;
-    int base = 0, equal_base = 0;
-    int parity = 0;
-    for (int j0 = 0; j0 < n; j0 += 4 * SEL_THREADS, parity ^= 1) {
-        bool more[4], equal[4];
-        int n_more = 0, n_equal = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int j = j0 + wave * 256 + e * 64 + lane;
-            const bool middle = j >= first && j < last && !none;
-            const uint32_t u = middle ? order_of(W[j]) : 0;
-            more[e] = j < n && (j < first || j >= last || (middle && u > prefix));
-            equal[e] = middle && u == prefix;
-            n_more += __popcll(__ballot(more[e]));
-            n_equal += __popcll(__ballot(equal[e]));
-        }
-        if (lane == 0) counts[parity][wave] = int2{n_more, n_equal};
+    // `prefix` is the order of the last weight that stays, `want` how many of those equal to it do: the first ones
+    int base = 0, equal_base = 0, n_more = 0, n_equal = 0;
+    uint64_t more[4], equal[4];                                  // ballots
+    rounds([&](int e, int j, uint32_t u) {
+        const bool middle = j >= first && j < last && !none;
+        more[e] = __ballot(j < n && (j < first || j >= last || (middle && u > prefix)));
+        equal[e] = __ballot(middle && u == prefix);
+        n_more += __popcll(more[e]), n_equal += __popcll(equal[e]);
+    }, [&](int i) {
+        int2 *const all = counts[i & 1];
+        if (lane == 0) all[wave] = int2{n_more, n_equal};
         __syncthreads();
         int my_more = base, my_equal = equal_base;               // kept (without the equal ones) and equal ones in front of this wavefront's keys
         for (int w = 0; w < SEL_WAVES; ++w) {
-            const int2 x = counts[parity][w];
+            const int2 x = all[w];
             if (w < wave) my_more += x.x, my_equal += x.y;
             base += x.x, equal_base += x.y;
         }
+        const uint64_t in_front = (1ull << lane) - 1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint64_t bm = __ballot(more[e]), be = __ballot(equal[e]), below = (1ull << lane) - 1;
-            const int rank = my_equal + __popcll(be & below);
-            const bool stays = more[e] || (equal[e] && rank < static_cast<int>(want));
-            const int at = my_more + __popcll(bm & below) + imin(rank, static_cast<int>(want));
-            if (stays) index[at] = j0 + wave * 256 + e * 64 + lane;
-            my_more += __popcll(bm), my_equal += __popcll(be);
+            const int rank = my_equal + __popcll(equal[e] & in_front);
+            const bool stays = (more[e] >> lane & 1) || ((equal[e] >> lane & 1) && rank < static_cast<int>(want));
+            if (stays) index[my_more + __popcll(more[e] & in_front) + imin(rank, static_cast<int>(want))] = i * SEL_ROUND + mine + 64 * e;
+            my_more += __popcll(more[e]), my_equal += __popcll(equal[e]);
         }
-    }
+        n_more = n_equal = 0;
+    });
 }
 
-// 16 bytes of a row to a thread, `chunks` threads to a key; the scales and weights go with the first two
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int k_chunks, int chunks, long slots) {
-    const long at = (blockIdx.x * 256L + threadIdx.x) / chunks;
-    const int part = static_cast<int>((blockIdx.x * 256L + threadIdx.x) % chunks);
-    if (at >= slots) return;
-    const int j = c.index[at];
-    const long from = at / c.keep * c.Nk + (j < 0 ? 0 : j);
-    v4i x = {0, 0, 0, 0};
-    if (part < k_chunks) {
-        if (j >= 0) x = *reinterpret_cast<const v4i *>(c.K + from * c.d + 16 * part);
-        *reinterpret_cast<v4i *>(c.K_out + at * c.d + 16 * part) = x;
-    } else {
-        if (j >= 0) x = *reinterpret_cast<const v4i *>(c.V + from * c.v_row + 16 * (part - k_chunks));
-        *reinterpret_cast<v4i *>(c.V_out + at * c.v_row + 16 * (part - k_chunks)) = x;
+// d / 16 lanes to a key, each with 16 bytes of K and of V (fp16: twice) of four keys at a time; the scales and weights go with the first two lanes
+constexpr int MOVE_AT_ONCE = 4;
+template <int VB>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int lanes, int blocks) {
+    const int unit = blockIdx.x / blocks, per_block = 256 / lanes, in = threadIdx.x / lanes, part = threadIdx.x % lanes;
+    if (in >= per_block) return;
+    const long from = static_cast<long>(unit) * c.Nk, to = static_cast<long>(unit) * c.keep;
+    const int s0 = blockIdx.x % blocks * per_block * MOVE_AT_ONCE + in;
+    int j[MOVE_AT_ONCE];
+    v4i k[MOVE_AT_ONCE], v[MOVE_AT_ONCE][VB];
+    float x[MOVE_AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < MOVE_AT_ONCE; ++i) {
+        const int s = s0 + i * per_block;
+        j[i] = s < c.keep ? c.index[to + s] : -1;
     }
-    if (part == 0) c.sK_out[at] = j < 0 ? 0.0f : c.sK[from];
-    if (part == 1) c.W_out[at] = j < 0 ? 0.0f : c.W[from];
+    const float *const small = part == 0 ? c.sK : c.W;
+#pragma unroll
+    for (int i = 0; i < MOVE_AT_ONCE; ++i) {
+        k[i] = v4i{0, 0, 0, 0};
+        x[i] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < VB; ++e) v[i][e] = v4i{0, 0, 0, 0};
+        if (j[i] >= 0) {
+            k[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i *>(c.K + (from + j[i]) * c.d + 16 * part));
+#pragma unroll
+            for (int e = 0; e < VB; ++e) v[i][e] = __builtin_nontemporal_load(reinterpret_cast<const v4i *>(c.V + (from + j[i]) * c.v_row + 16 * (part + e * lanes)));
+            if (part < 2) x[i] = small[from + j[i]];
+        }
+    }
+    float *const small_out = part == 0 ? c.sK_out : c.W_out;
+#pragma unroll
+    for (int i = 0; i < MOVE_AT_ONCE; ++i) {
+        const int s = s0 + i * per_block;
+        if (s >= c.keep) continue;
+        __builtin_nontemporal_store(k[i], reinterpret_cast<v4i *>(c.K_out + (to + s) * c.d + 16 * part));
+#pragma unroll
+        for (int e = 0; e < VB; ++e) __builtin_nontemporal_store(v[i][e], reinterpret_cast<v4i *>(c.V_out + (to + s) * c.v_row + 16 * (part + e * lanes)));
+        if (part < 2) small_out[to + s] = x[i];
+        if (lanes == 1) c.W_out[to + s] = j[i] < 0 ? 0.0f : c.W[from + j[i]];
+    }
 }
 
 bool overlap(const void *a, long na, const void *b, long nb) {
@@ -685,7 +739,7 @@ extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void 
     const long units = static_cast<long>(B) * Hkv;
     if (keep > Nk || static_cast<long>(recent) + sinks > keep || units > (1L << 40) / Nk / d) return IFA_ERR_SHAPE;
     if (v_bytes != 1 && v_bytes != 2) return IFA_ERR_DTYPE;
-    if ((d & 15) || d > 1024 || Nk > 0x7fffffff - 8192 || units > 1L << 22 || units * keep > (1L << 35) / ((1 + v_bytes) * d)) return IFA_ERR_UNSUPPORTED;
+    if ((d & 15) || d > 1024 || Nk > 0x7fffffff - 8192 || units > 1L << 22 || units * keep > (1L << 35) / d) return IFA_ERR_UNSUPPORTED;
     for (const void *p : {static_cast<const void *>(K_i8), V, static_cast<const void *>(K_out), static_cast<const void *>(V_out)})
         if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
     for (const void *p : {static_cast<const void *>(s_K), static_cast<const void *>(W), static_cast<const void *>(lens), static_cast<const void *>(s_K_out),
@@ -704,8 +758,13 @@ extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void 
     EvictCall c = {K_i8, static_cast<const int8_t *>(V), s_K, W, lens, B, Hkv, Nk, d, d * v_bytes, keep, recent, sinks,
                    K_out, static_cast<int8_t *>(V_out), s_K_out, W_out, index, lens_out};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    hipLaunchKernelGGL(evict_select_kernel, dim3(static_cast<unsigned>(units)), dim3(SEL_THREADS), 0, st, c);
-    const int k_chunks = d / 16, chunks = k_chunks * (1 + v_bytes);
-    hipLaunchKernelGGL(evict_move_kernel, dim3(static_cast<unsigned>((out * chunks + 255) / 256)), dim3(256), 0, st, c, k_chunks, chunks, out);
+    auto select = [&](auto rounds) { hipLaunchKernelGGL((evict_select_kernel<decltype(rounds)::value>), dim3(static_cast<unsigned>(units)), dim3(SEL_THREADS), 0, st, c); };
+    if (Nk <= 1 * SEL_ROUND) select(std::integral_constant<int, 1>{});
+    else if (Nk <= 4 * SEL_ROUND) select(std::integral_constant<int, 4>{});
+    else select(std::integral_constant<int, 0>{});
+    const int lanes = d / 16, per_block = 256 / lanes * MOVE_AT_ONCE, blocks = (keep + per_block - 1) / per_block;
+    auto move = [&](auto vb) { hipLaunchKernelGGL((evict_move_kernel<decltype(vb)::value>), dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, lanes, blocks); };
+    if (v_bytes == 1) move(std::integral_constant<int, 1>{});
+    else move(std::integral_constant<int, 2>{});
     return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
 }

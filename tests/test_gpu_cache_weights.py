@@ -80,6 +80,8 @@ EVICTIONS = [
     (1, 3, 300, 128, 100, 60, 40, None),                 # nothing is chosen by weight
     (1, 1, 4097, 64, 4096, 0, 0, None),
     (1, 2, 260, 32, 37, 3, 2, (259,)),
+    (1, 1, 20000, 16, 300, 7, 1, (19999,)),              # weights read again in each pass
+    (2, 1, 16384, 48, 16000, 0, 0, None),
 ]
 
 
