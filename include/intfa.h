@@ -299,7 +299,7 @@ int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8,
  * The softmax weight that each own key draws, added up over the queries and over the heads of its group -- what an eviction goes by:
  *   W_out[b, hk, j] = W[b, hk, j] + sum over i and over the heads h of group hk of exp(S_ij) / sum_j' exp(S_ij'),   j' over the keys that query i sees (j' <= p)
  * in fp32 (the weights are not rounded to fp16).  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W.
- *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
+ *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30, G Nq d <= 0x7ff00000.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
  * row and key where a key head has up to 16 query rows, else 4 a key and slice of the rows.
  */
 long ifa_key_weights_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d);

@@ -22,10 +22,11 @@ struct WeightsCall {
     const float *sQ, *sK, *W;                                    // W null: zeros
     const int *lens;
     int B, Hkv, G, Nq, Nk;
+    unsigned G_inverse;                                          // 2^32 / G, rounded up (G > 1)
     int parts;                                                   // of the keys, in the first pass
     int slices;                                                  // of the rows, in the second
-    float2 *stats;                                               // [part][B H Nq]: maximum (log2 units) and sum of a row over that part
-    float2 *rows_out;                                            // [B H Nq]: maximum + log2(sum) of a row (inf: it sees nothing) and s_Q log2(e); null with stored scores
+    float2 *stats;                                               // [part][unit][rows]: maximum (log2 units) and sum of a row over that part
+    float2 *rows_out;                                            // [unit][rows]: maximum + log2(sum) of a row (inf: it sees nothing) and s_Q log2(e); null with stored scores
     float *scores;                                               // [unit][rows][score_stride] in log2 units, or null
     long score_stride;
     float *sums;                                                 // [slice][unit][Nk], or null: straight to out
@@ -39,9 +40,10 @@ __device__ __forceinline__ long query_row(const WeightsCall &c, int unit, int ro
 __device__ __forceinline__ float2 row_of_second_pass(float m, float sum, float sq) {
     return float2{m == -INFINITY ? INFINITY : m + __builtin_amdgcn_logf(sum), sq * LOG2E};
 }
-[[maybe_unused]] __device__ __forceinline__ void write_stats(const WeightsCall &c, int units, int part, long row, float m, float sum) {
-    if (c.rows_out && c.parts == 1) c.rows_out[row] = row_of_second_pass(m, sum, c.sQ[row]);
-    else c.stats[static_cast<long>(part) * units * c.G * c.Nq + row] = float2{m, sum};
+[[maybe_unused]] __device__ __forceinline__ void write_stats(const WeightsCall &c, int units, int part, int unit, int row, float m, float sum) {
+    const long rows = static_cast<long>(c.G) * c.Nq, at = unit * rows + row;
+    if (c.rows_out && c.parts == 1) c.rows_out[at] = row_of_second_pass(m, sum, c.sQ[query_row(c, unit, row)]);
+    else c.stats[part * units * rows + at] = float2{m, sum};
 }
 
 // ---- first pass: maximum and sum of 32 rows over a part of the keys, the wavefronts taking every fourth tile of 32 keys, each for itself -----------------
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(Weights
 #pragma unroll
         for (int w = 0; w < KW_WAVES; ++w)
             if (sm.ml[w][tid].x != -INFINITY) sum += sm.ml[w][tid].y * __builtin_amdgcn_exp2f(sm.ml[w][tid].x - m);
-        write_stats(c, units, part, query_row(c, unit, row0 + tid), m, sum);
+        write_stats(c, units, part, unit, row0 + tid, m, sum);
     }
 #endif
 }
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCa
         __syncthreads();
     }
     l += swap32(l);
-    if (g == 0 && row0 + 32 * wave + r < rows) write_stats(c, units, part, qrow, m2, l);
+    if (g == 0 && row0 + 32 * wave + r < rows) write_stats(c, units, part, unit, row, m2, l);
 #endif
 }
 
@@ -273,7 +275,8 @@ __global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, lo
     const long at = blockIdx.x * 256L + threadIdx.x;
     if (at >= rows) return;
     const float2 x = join_parts(c.stats + at, rows, c.parts, 0, 1);
-    c.rows_out[at] = row_of_second_pass(x.x, x.y, c.sQ[at]);
+    const int per = c.G * c.Nq;
+    c.rows_out[at] = row_of_second_pass(x.x, x.y, c.sQ[query_row(c, static_cast<int>(at / per), static_cast<int>(at % per))]);
 }
 
 // ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
@@ -284,7 +287,7 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
     const int L = c.lens ? imax(0, imin(c.lens[unit / c.Hkv], c.Nk)) : c.Nk;
     static_assert(STORED_ROWS * 16 == 256, "16 lanes to a row");
     const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
-    float2 x = row < rows ? join_parts(c.stats + query_row(c, unit, row), static_cast<long>(units) * rows, c.parts, lane, 16) : float2{-INFINITY, 0.0f};
+    float2 x = row < rows ? join_parts(c.stats + static_cast<long>(unit) * rows + row, static_cast<long>(units) * rows, c.parts, lane, 16) : float2{-INFINITY, 0.0f};
 #pragma unroll
     for (int s = 8; s; s >>= 1) {
         const float2 y = {__shfl_xor(x.x, s), __shfl_xor(x.y, s)};
@@ -327,8 +330,8 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
 }
 
 // ---- second pass, scores computed again: 256 keys to a workgroup, a key to a lane ---------------------------------------------------------------
-// The rows go by in tiles of 64 queries of one head through LDS, shared by the four wavefronts of 64 keys (two operands of K in registers, so that what is read of the rows counts
-// twice); a slice of them per workgroup.  The vector unit's part of a score: s_Q s_K, the subtraction of the start value, their product less the row's maximum + log2(sum), exp2 and the
+// The rows go by in tiles of 64 through LDS, shared by the four wavefronts of 64 keys (two operands of K in registers, so that what is read of the rows counts
+// twice); a slice of them per workgroup.  They are packed like everywhere, row (i, g) with g fastest: a row is a copy from a place of its own, and a few queries of many heads fill a tile.  The vector unit's part of a score: s_Q s_K, the subtraction of the start value, their product less the row's maximum + log2(sum), exp2 and the
 // addition.  (Maximum and log2 in one number: it rounds by 2^-24 of itself, as scores do, and the rows' errors do not add up.)
 constexpr int KW_ROWS = 64, KW_KEYS = 256;
 template <int D> struct SmemKeys {
@@ -348,8 +351,9 @@ __global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c,
     if (unit >= units) return;
     const int L = keys_of(c.lens, unit / c.Hkv, c.Nk), shift = L - c.Nq;
     const int j0 = KW_KEYS * kt, jw = j0 + 64 * wave;
-    const int i0 = imax(0, j0 - shift);                          // the first query that sees any of the keys
-    const int per_head = j0 < L && i0 < c.Nq ? (c.Nq - i0 + KW_ROWS - 1) / KW_ROWS : 0, total = per_head * c.G;
+    const int rows = c.G * c.Nq;
+    auto first_row = [&](int j) { return imin(imax(0, j - shift), c.Nq) * c.G; };               // the first row that sees key j
+    const int r0 = first_row(j0), total = j0 < L ? (rows - r0 + KW_ROWS - 1) / KW_ROWS : 0;
     const int per = (total + c.slices - 1) / c.slices, t0 = slice * per, t1 = imin(total, t0 + per);
     float sum[2] = {0.0f, 0.0f};
     if (t0 < t1) {
@@ -367,14 +371,22 @@ __global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c,
             }
             sk[h] = j < L ? c.sK[kb + j] : 0.0f;
         }
+        const int lane_first[2] = {first_row(jw + r), first_row(jw + 32 + r)}, wave_first = first_row(jw), wave_last = first_row(jw + 63);
         const Lane<D, true> lo(lane);
         const lds_ptr qbuf = (lds_ptr)(&sm.q[0][0]), rbuf = (lds_ptr)(&sm.row[0][0]);
-        auto stage = [&](int t, int slot) {
-            const int head = t / per_head, i = i0 + t % per_head * KW_ROWS, rows = imin(c.Nq - i, KW_ROWS);
-            const long row = (static_cast<long>(unit) * c.G + head) * c.Nq + i;
-            const BufRsrc rQ = make_rsrc(c.Q + row * D, rows * D), rM = make_rsrc(c.rows_out + row, rows * 8);
-            copy_pieces<PIECES>(rQ, qbuf + slot * QB + wave * PIECES * 1024, lo.gk, lo.gk, wave * PIECES * 1024);
-            if (wave < 2) lds_copy4(rM, rbuf + slot * 512 + 256 * wave, 4 * lane, 256 * wave);
+        const BufRsrc rQ = make_rsrc(c.Q + static_cast<long>(unit) * rows * D, rows * D), rM = make_rsrc(c.rows_out + static_cast<long>(unit) * rows, rows * 8);
+        auto stage = [&](int t, int slot) {                      // (rows past the last come as zeros)
+            const int tile = r0 + t * KW_ROWS;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int in = (wave * PIECES + i) * (1024 / D) + lane / (D / 16), row = tile + in;
+                // row = q G + g; the product with 2^32 / G, rounded up, is right or one too large
+                int q = c.G == 1 ? row : static_cast<int>(__umulhi(static_cast<unsigned>(row), c.G_inverse)), g_of = row - q * c.G;
+                if (g_of < 0) --q, g_of += c.G;
+                const unsigned from = row < rows ? static_cast<unsigned>(g_of * c.Nq + q) * D + (lo.gk & (D - 1)) : static_cast<unsigned>(NOTHING);
+                lds_copy16(rQ, qbuf + slot * QB + (wave * PIECES + i) * 1024, from, 0);
+            }
+            if (wave < 2) lds_copy4(rM, rbuf + slot * 512 + 256 * wave, 4 * lane, tile * 8 + 256 * wave);
         };
         v16i bias;
 #pragma unroll
@@ -386,11 +398,10 @@ __global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c,
         for (int t = t0; t < t1; ++t) {
             const int slot = (t - t0) & 1;
             if (t + 1 < t1) stage(t + 1, slot ^ 1);
-            const int i = i0 + t % per_head * KW_ROWS;
 #pragma unroll
             for (int q = 0; q < KW_ROWS / 32; ++q) {
-                const int p0 = shift + i + 32 * q;               // position of the first of these queries
-                if (p0 + 31 < jw || i + 32 * q >= c.Nq) continue;                // (wave-uniform) none sees any of the wavefront's keys
+                const int tile = r0 + t * KW_ROWS + 32 * q;      // the first of these rows
+                if (tile >= rows || tile + 31 < wave_first) continue;            // (wave-uniform) none sees any of the wavefront's keys
                 v4i qop[KS];
                 v4f row[4][2];
 #pragma unroll
@@ -399,7 +410,7 @@ __global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c,
                 for (int vq = 0; vq < 4; ++vq)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) row[vq][e] = *reinterpret_cast<LDS_AS const v4f *>(rbuf + slot * 512 + 256 * q + 64 * vq + 32 * g + 16 * e);
-                const bool masked = p0 < jw + 63 || i + 32 * q + 32 > c.Nq;
+                const bool masked = tile < wave_last || tile + 32 > rows;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     v16i acc = bias;
@@ -412,9 +423,8 @@ __global__ __launch_bounds__(256, 3) void key_weights_keys_kernel(WeightsCall c,
                         y[v] = __builtin_fmaf(__int_as_float(acc[v]) - ACC_BIAS_F, sk[h] * x4[2 * (v & 1) + 1], -x4[2 * (v & 1)]);
                     }
                     if (masked) {
-                        // query 32 q + k counts iff k >= first (it sees the key) and k < end
-                        const int first = jw + 32 * h + r - p0, end = c.Nq - i - 32 * q;
-                        const uint32_t seen = static_cast<uint32_t>(below(end) & ~below(first)) >> (4 * g);
+                        // from the first row that sees the lane's key to the last there is
+                        const uint32_t seen = static_cast<uint32_t>(below(rows - tile) & ~below(lane_first[h] - tile)) >> (4 * g);
 #pragma unroll
                         for (int v = 0; v < 16; ++v)
                             if (!(seen & (1u << (8 * (v >> 2) + (v & 3))))) y[v] = -INFINITY;
@@ -472,7 +482,7 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
         p.slices = 1;
     } else {
         p.rows = up(units * rows * 8);
-        const long groups = units * ((Nk + KW_KEYS - 1) / KW_KEYS), most = G * ((Nq + KW_ROWS - 1L) / KW_ROWS);
+        const long groups = units * ((Nk + KW_KEYS - 1) / KW_KEYS), most = (rows + KW_ROWS - 1) / KW_ROWS;
         long slices = (1024 + groups - 1) / groups;
         if (slices > most) slices = most;
         p.slices = static_cast<int>(slices < 1 ? 1 : slices > 64 ? 64 : slices);
@@ -517,7 +527,7 @@ int refuse_sizes(int B, int H, int Hkv, int Nq, int Nk, int d) {
     if (heads > (1L << 40) / N / d) return IFA_ERR_SHAPE;
     if (d != 64 && d != 128) return IFA_ERR_UNSUPPORTED;
     if (static_cast<long>(Nk) * d * 2 > 0x7ff00000L || heads * Nq > 1L << 26 || heads > 1L << 23) return IFA_ERR_UNSUPPORTED;
-    if (static_cast<long>(B) * Hkv * Nk > 1L << 30) return IFA_ERR_UNSUPPORTED;      // (a launch has less than 2^32 threads: two to a key)
+    if (static_cast<long>(H / Hkv) * Nq * d > 0x7ff00000L || static_cast<long>(B) * Hkv * Nk > 1L << 30) return IFA_ERR_UNSUPPORTED;      // (a launch has less than 2^32 threads: two to a key)
     return IFA_OK;
 }
 
@@ -616,7 +626,8 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
         if (lane == 63) wave_total[wave] = run;
         __syncthreads();
         uint32_t before = run - c0 - c1;
-        for (int w = 0; w < wave; ++w) before += wave_total[w];
+#pragma unroll
+        for (int w = 0; w < SEL_WAVES; ++w) before += w < wave ? wave_total[w] : 0;
         if (before < want && want <= before + c0) found[0] = b0, found[1] = want - before;
         else if (before + c0 < want && want <= before + c0 + c1) found[0] = b0 - 1, found[1] = want - before - c0;
         __syncthreads();
@@ -637,6 +648,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
         if (lane == 0) all[wave] = int2{n_more, n_equal};
         __syncthreads();
         int my_more = base, my_equal = equal_base;               // kept (without the equal ones) and equal ones in front of this wavefront's keys
+#pragma unroll
         for (int w = 0; w < SEL_WAVES; ++w) {
             const int2 x = all[w];
             if (w < wave) my_more += x.x, my_equal += x.y;
@@ -720,7 +732,7 @@ extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, con
     if (workspace_bytes < plan.bytes()) return IFA_ERR_WORKSPACE;
     WeightsCall c = {};
     c.Q = Q_i8, c.K = K_i8, c.sQ = s_Q, c.sK = s_K, c.W = W, c.lens = lens, c.out = W_out;
-    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.parts = plan.parts, c.slices = plan.slices;
+    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.G_inverse = static_cast<unsigned>(((1ull << 32) + c.G - 1) / c.G), c.parts = plan.parts, c.slices = plan.slices;
     char *const ws = static_cast<char *>(workspace);
     c.stats = reinterpret_cast<float2 *>(ws);
     c.rows_out = plan.stored ? nullptr : reinterpret_cast<float2 *>(ws + plan.stats);
@@ -761,6 +773,7 @@ extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void 
     auto select = [&](auto rounds) { hipLaunchKernelGGL((evict_select_kernel<decltype(rounds)::value>), dim3(static_cast<unsigned>(units)), dim3(SEL_THREADS), 0, st, c); };
     if (Nk <= 1 * SEL_ROUND) select(std::integral_constant<int, 1>{});
     else if (Nk <= 4 * SEL_ROUND) select(std::integral_constant<int, 4>{});
+    else if (Nk <= 8 * SEL_ROUND) select(std::integral_constant<int, 8>{});
     else select(std::integral_constant<int, 0>{});
     const int lanes = d / 16, per_block = 256 / lanes * MOVE_AT_ONCE, blocks = (keep + per_block - 1) / per_block;
     auto move = [&](auto vb) { hipLaunchKernelGGL((evict_move_kernel<decltype(vb)::value>), dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, lanes, blocks); };

@@ -36,6 +36,7 @@ WEIGHTS = [
     (1, 1, 2, 700, 900, 128, None),
     (2, 8, 2, 150, 1200, 128, (1200, 700)),              # tiles of 128 rows, the keys in parts
     (1, 20, 3, 80, 200, 64, (190,)),                     # ... in one
+    (3, 2, 7, 11, 700, 128, (700, 13, 5)),               # a few queries of many heads, an odd group
     (2, 1, 4, 1, 20000, 64, (20000, 19999)),             # many parts of stored scores
     (5, 1, 1, 31, 31, 128, (31, 30, 1, 0, 16)),
 ]
@@ -80,7 +81,8 @@ EVICTIONS = [
     (1, 3, 300, 128, 100, 60, 40, None),                 # nothing is chosen by weight
     (1, 1, 4097, 64, 4096, 0, 0, None),
     (1, 2, 260, 32, 37, 3, 2, (259,)),
-    (1, 1, 20000, 16, 300, 7, 1, (19999,)),              # weights read again in each pass
+    (1, 1, 40000, 16, 300, 7, 1, (39999,)),              # weights read again in each pass
+    (1, 2, 32768, 16, 30000, 0, 4, (31000,)),            # the most that stay in registers
     (2, 1, 16384, 48, 16000, 0, 0, None),
 ]
 
