@@ -263,7 +263,8 @@ int int_flash_attn_fwd_half_rect(const signed char *Q_i8, const signed char *K_i
  * memory, int32 [B]; null: Nk; values outside [0, Nk] count as the nearer end).  What lies at or beyond L_b is not looked at.
  *   Queries: Q_i8 [B, H, Nq, d], s_Q [B, H, Nq], H = G Hkv: query head h reads key head h / G.  The Nq queries of sequence b are its LAST
  * positions: query i stands at p = L_b - Nq + i and sees own keys j <= p.  A query at p < 0 (padding in front, an empty
- * sequence) sees no own key; one that sees no key at all gives zeros.
+ * sequence) sees no own key; one that sees no key at all gives zeros,
+ * whatever its codes and scale are.
  *   The weights are those of the half-INT8 variant, whatever V is: P~ = fp16(exp(S - m)), l the sum of the rounded weights, O = P~ V / l
  * (times s_V) with fp32 accumulation.  Unlike Algorithm 1's INT8 P they do not lie on the grid of a running maximum, so the result depends
  * on how the keys are shared out over the chip only by the rounding of a weight (2^-11 of it) and the order of fp32 additions.
@@ -298,7 +299,8 @@ int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8,
 /*
  * The softmax weight that each own key draws, added up over the queries and over the heads of its group -- what an eviction goes by:
  *   W_out[b, hk, j] = W[b, hk, j] + sum over i and over the heads h of group hk of exp(S_ij) / sum_j' exp(S_ij'),   j' over the keys that query i sees (j' <= p)
- * in fp32 (the weights are not rounded to fp16).  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W.
+ * in fp32 (the weights are not rounded to fp16).  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W
+ * (and must not overlap it otherwise).
  *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30, G Nq d <= 0x7ff00000.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
  * row and key where a key head has up to 16 query rows, else 4 a key and slice of the rows.
  */

@@ -101,7 +101,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
     v4i qf[KS];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = c.sQ[qrow] * LOG2E;
+    const float sq2 = shared || p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));    // landed before the loop
     v16i bias;
@@ -252,11 +252,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 // ---- many rows: tiles of 128 ----------------------------------------------------------------------------------------
 // Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered).  What bounds it is the vector unit: 32 keys of 32 rows are 12 matrix
 // instructions (384 cycles at d = 128), and of the vector instructions on each of their scores (subtract the start value, s_K, the maximum, s_Q and m, exp2, the conversion
-// in pairs, the sum in pairs) exp2 alone takes 16 cycles.  So nothing else is left to the vector unit:
-//   - the running maximum only moves when a block exceeds it by 2^8 (a row by itself: what a row gives does not depend on its neighbours), which an fp16 weight holds
-//     as well as a weight of 1, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made;
-//   - the weights are rounded toward zero, two to an instruction.  They are too small by 2^-11 on average, in O and in l alike; what is left of the quotient's error is
-//     within half a step (2^-11) of each weight, as with rounding to nearest.
+// in pairs, the sum in pairs) exp2 alone takes 16 cycles: 1111 vector cycles of the 2060 that 64 keys take a wavefront, 769 of the matrix unit (the chip runs it at 1.8 - 2.0 GHz).
+// So the running maximum only moves when a block exceeds it by 2^8 (a row by itself: what a row gives does not depend on its neighbours), which an fp16 weight holds as well
+// as a weight of 1, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made.
 constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
 template <int D, bool VI8> struct SmemTile {
     alignas(4096) int8_t k[2][TILE_KEYS * D];
@@ -326,8 +324,7 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
     const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
     h2 ph[2][8];
     auto weights = [&](int mt, int e) {
-        ph[mt][e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)),
-                                                                      __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e + 1], sq2, -m))));
+        ph[mt][e] = h2{(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e + 1], sq2, -m))};
         st.l = __builtin_amdgcn_fdot2(ph[mt][e], ones, st.l, false);
     };
     // the weights of the second 32 keys between the products of the first
@@ -446,7 +443,7 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     v4i qf[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = c.sQ[qrow] * LOG2E;
+    const float sq2 = p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;        // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
     v16i bias;

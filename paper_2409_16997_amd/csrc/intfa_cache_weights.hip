@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCa
     v4i qf[KS];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = c.sQ[qrow] * LOG2E;
+    const float sq2 = p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;        // (padding: whatever its scale holds)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));
     v16i bias;
@@ -728,6 +728,8 @@ extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, con
     if (!ifa_aligned16(Q_i8) || !ifa_aligned16(K_i8) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return IFA_ERR_UNSUPPORTED;
     for (const void *p : {static_cast<const void *>(s_Q), static_cast<const void *>(s_K), static_cast<const void *>(lens), static_cast<const void *>(W), static_cast<const void *>(W_out)})
         if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
+    const long n = static_cast<long>(B) * Hkv * Nk * 4;
+    if (W && W != W_out && overlap(W, n, W_out, n)) return IFA_ERR_UNSUPPORTED;      // (in place or apart, not shifted)
     const Plan plan = plan_of(B, Hkv, H / Hkv, Nq, Nk);
     if (workspace_bytes < plan.bytes()) return IFA_ERR_WORKSPACE;
     WeightsCall c = {};

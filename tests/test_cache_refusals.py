@@ -68,6 +68,7 @@ def test_key_weights(L):
     for bad in (dict(d=32), dict(q=ODD), dict(k=ODD), dict(ws=ODD), dict(w=ctypes.c_void_p(0x1002)), dict(o=ctypes.c_void_p(0x1002)), dict(Nk=0x7ff00000 // 256 + 1),
                 dict(Nq=1 << 25, Nk=1), dict(B=1 << 10, H=2, Nk=1 << 20, d=64)):
         assert weights(L, **bad) == -4, bad
+    assert weights(L, w=ctypes.c_void_p(0x1004)) == -4                     # W and W_out overlap, shifted
     need = L.ifa_key_weights_workspace_bytes(1, 4, 2, 1, 100, 128)
     assert need > 0 and weights(L, n=need - 1) == -6 and L.ifa_key_weights_workspace_bytes(1, 4, 2, 1, 100, 96) == -1
 

@@ -125,6 +125,19 @@ def test_what_no_query_of_a_prompt_sees_is_not_looked_at(ifa):
         check(window(ifa, s, 100, 70, (880,)), clean, tol)
 
 
+@pytest.mark.parametrize("Hkv,Nq", [(1, 9), (16, 200)])       # the kernel for 32 rows, tiles of 128
+def test_what_padding_queries_hold_does_not_matter(ifa, Hkv, Nq):
+    s = ref.problem(2, 2, Hkv, 2, Nq, 260, 64)
+    lens = (5, 0)
+    want, tol = ref.attention(s, torch.float16, lens, 40, 2)
+    for bad in (0.0, math.nan, math.inf):
+        s["sq"][0, :, :Nq - 5] = bad
+        s["sq"][1] = bad
+        got = window(ifa, s, 40, 2, lens)
+        check(got, want, tol)
+        assert bool((got[0, :, :Nq - 5] == 0).all()) and bool((got[1] == 0).all())
+
+
 def test_lengths_outside_the_buffer_count_as_the_nearer_end(ifa):
     s = ref.problem(4, 3, 1, 2, 2, 50, 64)
     a, b = window(ifa, s, 20, 2, (50, 0, 17)), window(ifa, s, 20, 2, (10 ** 9, -5, 17))

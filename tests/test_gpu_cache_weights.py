@@ -71,6 +71,17 @@ def test_weights_of_what_lies_behind_the_sequence(ifa):
         assert bool(((got - want - 0.25).abs() <= tol + 2.0 ** -23 * (want + 0.25)).all()) and bool((got[:, :, 333:] == 0.25).all())
 
 
+@pytest.mark.parametrize("Hkv,G,Nq", [(1, 1, 9), (1, 2, 30), (16, 2, 200)])   # stored scores, the kernel for 32 rows, tiles of 128
+def test_what_padding_queries_hold_does_not_matter(ifa, Hkv, G, Nq):
+    s = ref.problem(2, 1, Hkv, G, Nq, 260, 64)
+    want, tol = ref.key_weights(s, (5,))
+    for bad in (0.0, math.nan, math.inf):
+        s["sq"][:, :, :Nq - 5] = bad
+        t = ref.on_gpu(s)
+        got = ifa.key_weights(t["q8"], t["k8"], t["sq"], t["sk"], lens=dev_lens((5,))).cpu().double()
+        assert bool(((got - want).abs() <= tol).all())
+
+
 # B, Hkv, Nk, d, keep, recent, sinks, lens
 EVICTIONS = [
     (1, 1, 1, 64, 1, 0, 0, None),
