@@ -241,11 +241,11 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
     }
 }
 #endif
-template <int D, bool VI8, bool ALL, int ST, bool NT>
+template <int D, bool VI8, int ST, bool NT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Call c, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemFew<D, VI8, ST> sm;
-    few_rows_of_a_unit<D, VI8, ALL, ST, NT>(sm, c, blockIdx.x, units, row_tiles);
+    few_rows_of_a_unit<D, VI8, false, ST, NT>(sm, c, blockIdx.x, units, row_tiles);
 #endif
 }
 
@@ -636,30 +636,25 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv;
     float *const o = static_cast<float *>(workspace);
     float2 *const ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
-    auto run = [&](auto all, const Call &k, int n_units) {
-        constexpr bool ALL = decltype(all)::value;
-        const bool few = few_rows(ALL, n_units, k.rows);
-        const int tiles = static_cast<int>(row_tiles(few, k.rows));
-        if (!few) {
-            const long grid = static_cast<long>(n_units) * tiles * k.splits;
-            hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, ALL>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, k, n_units, tiles, head_group_for(true, 0, 0));
-            return;
-        }
-        const long grid = (static_cast<long>(n_units) * k.splits + 7) / 8 * 8 * tiles;
+    auto tiles = [&](auto all, const Call &k, int n_units) {
+        const int n = static_cast<int>(row_tiles(false, k.rows));
+        hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(static_cast<long>(n_units) * n * k.splits)), dim3(256), 0, st, k, n_units, n,
+                           head_group_for(true, 0, 0));
+    };
+    auto few = [&](const Call &k) {
+        const int n = static_cast<int>(row_tiles(true, k.rows));
+        const long grid = (static_cast<long>(units) * k.splits + 7) / 8 * 8 * n;
         auto launch_few = [&](auto stages, auto nt) {
-            hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, ALL, decltype(stages)::value, decltype(nt)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, n_units, tiles);
+            hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(stages)::value, decltype(nt)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, units, n);
         };
         constexpr std::integral_constant<int, 1> one{};
         constexpr std::integral_constant<int, 2> two{};
-        if constexpr (ALL) launch_few(one, std::false_type{});
-        else {
-            // with the non-temporal hint where what is read once does not stay in the caches anyway: 32 x 8 heads on 4096 keys 67 us against 76, 64 x 8 on 512 26 / 28; 4 x 8 on 4096 (50 MB) the same
-            const long keys = imin(k.Nk, imin(k.window, k.Nk - k.sinks) + k.sinks);
-            const bool once = tiles == 1 && n_units * keys * (D + V_ROW<D, VI8>) > 64L << 20;
-            // One workgroup to a CU copies two tiles ahead; more of them fit with one (64 x 8 heads on 512 keys 26 us, with two 27; 16 x 8 on 4096 in 256 workgroups 41 and 39)
-            if (grid > 256) once ? launch_few(one, std::true_type{}) : launch_few(one, std::false_type{});
-            else once ? launch_few(two, std::true_type{}) : launch_few(two, std::false_type{});
-        }
+        // with the non-temporal hint where what is read once does not stay in the caches anyway: 32 x 8 heads on 4096 keys 67 us against 76, 64 x 8 on 512 26 / 28; 4 x 8 on 4096 (50 MB) the same
+        const long keys = imin(k.Nk, imin(k.window, k.Nk - k.sinks) + k.sinks);
+        const bool once = n == 1 && units * keys * (D + V_ROW<D, VI8>) > 64L << 20;
+        // One workgroup to a CU copies two tiles ahead; more of them fit with one (64 x 8 heads on 512 keys 26 us, with two 27; 16 x 8 on 4096 in 256 workgroups 41 and 39)
+        if (grid > 256) once ? launch_few(one, std::true_type{}) : launch_few(one, std::false_type{});
+        else once ? launch_few(two, std::true_type{}) : launch_few(two, std::false_type{});
     };
     Call shared = {};
     if (plan.shared > 0) {
@@ -672,19 +667,20 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
     }
     c.splits = plan.own;
     if (plan.join()) c.part_o = o + plan.rows_shared * D, c.part_ml = ml + plan.rows_shared;
-    if (plan.shared > 0 && few_rows(false, units, c.rows)) {
-        const bool few = few_rows(true, c.Hkv, shared.rows);
-        const int shared_tiles = static_cast<int>(row_tiles(few, shared.rows)), own_tiles = static_cast<int>(row_tiles(true, c.rows));
-        const long blocks = few ? (static_cast<long>(c.Hkv) * shared.splits + 7) / 8 * 8 * shared_tiles : static_cast<long>(c.Hkv) * shared_tiles * shared.splits;
+    const bool own_few = few_rows(false, units, c.rows);
+    if (plan.shared > 0 && own_few) {
+        const bool shared_few = few_rows(true, c.Hkv, shared.rows);
+        const int shared_tiles = static_cast<int>(row_tiles(shared_few, shared.rows)), own_tiles = static_cast<int>(row_tiles(true, c.rows));
+        const long blocks = shared_few ? (static_cast<long>(c.Hkv) * shared.splits + 7) / 8 * 8 * shared_tiles : static_cast<long>(c.Hkv) * shared_tiles * shared.splits;
         const long grid = blocks + (static_cast<long>(units) * c.splits + 7) / 8 * 8 * own_tiles;
         auto both = [&](auto tile) {
             hipLaunchKernelGGL((cache_attention_both_kernel<D, VI8, decltype(tile)::value>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, shared, c, static_cast<int>(blocks), shared_tiles,
                                units, own_tiles, head_group_for(true, 0, 0));
         };
-        few ? both(std::false_type{}) : both(std::true_type{});
+        shared_few ? both(std::false_type{}) : both(std::true_type{});
     } else {
-        if (plan.shared > 0) run(std::true_type{}, shared, c.Hkv);
-        run(std::false_type{}, c, units);
+        if (plan.shared > 0) tiles(std::true_type{}, shared, c.Hkv);         // (more rows than own_few has: tiles)
+        own_few ? few(c) : tiles(std::false_type{}, c, units);
     }
     if (plan.join()) {
         const Parts parts = {o, c.part_o, ml, c.part_ml, plan.shared, plan.own};

@@ -192,3 +192,63 @@ def test_a_prefix_of_one_sequence_is_plain_attention(ifa):
     want, tol = ref.attention(whole, torch.float32, None, 10 ** 6)
     check(prefix(ifa, s, out_dtype=torch.float32), want, tol)
     check(window(ifa, whole, 10 ** 6, 0, out_dtype=torch.float32), want, tol)
+
+
+def test_calls_on_two_streams_at_once(ifa):
+    """Each call allocates a workspace of its own: calls that run side by side do not meet."""
+    s = [ref.on_gpu(ref.problem(20 + k, 4, 2, 4, 1, 3000, 128, Np=4000)) for k in range(2)]
+
+    def call(t):
+        return (ifa.int_flash_attn_fwd_window(t["q8"], t["k8"], t["v"], t["sq"], t["sk"], 2000, 4), ifa.key_weights(t["q8"], t["k8"], t["sq"], t["sk"]),
+                ifa.int_flash_attn_fwd_prefix(t["q8"], t["kp8"], t["vp"], t["k8"], t["v"], t["sq"], t["skp"], t["sk"]))
+
+    want = [call(t) for t in s]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in s], []
+    for _ in range(5):
+        for t, stream in zip(s, streams):
+            with torch.cuda.stream(stream):
+                got.append(call(t))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
+
+
+def test_refusals_of_the_binding(ifa):
+    t = ref.on_gpu(ref.problem(30, 2, 2, 2, 1, 3000, 64, Np=700))
+    q, k, v, sq, sk = t["q8"], t["k8"], t["v"], t["sq"], t["sk"]
+    lens = torch.tensor([5, 6], dtype=torch.int32, device="cuda")
+    win, pre = ifa.int_flash_attn_fwd_window, ifa.int_flash_attn_fwd_prefix
+
+    def refused(match, f, *a, **kw):
+        with pytest.raises(ifa.IntfaError, match=match):
+            f(*a, **kw)
+
+    refused("window is at least 1", win, q, k, v, sq, sk, 0)
+    refused("sinks at least 0", win, q, k, v, sq, sk, 4, -1)
+    refused("lens", win, q, k, v, sq, sk, 4, lens=lens.long())
+    refused("lens", win, q, k, v, sq, sk, 4, lens=lens[:1])
+    refused("lens", win, q, k, v, sq, sk, 4, lens=lens.cpu())
+    refused("V", win, q, k, v.float(), sq, sk, 4)
+    refused("V", win, q, k, v, sq, sk, 4, s_V=torch.ones(2, 2, device="cuda"))
+    refused("s_V", win, q, k, k, sq, sk, 4, s_V=torch.ones(2, device="cuda"))
+    refused("s_Q", win, q, k, v, sq[:, :2], sk, 4)
+    refused("do not agree", win, q, k.transpose(1, 2), v, sq, sk, 4)
+    refused("K_i8: expected a contiguous", win, q, torch.cat([k, k], -1)[..., ::2], v, sq, sk, 4)
+    refused("out", win, q, k, v, sq, sk, 4, out=torch.empty(2, 4, 1, 32, dtype=torch.float16, device="cuda"))
+    refused("unsupported dtype|out_dtype|dtype", win, q, k, v, sq, sk, 4, out_dtype=torch.int32)
+    refused("IFA_ERR_WORKSPACE", win, q, k, v, sq, sk, 2999, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    refused("uint8", win, q, k, v, sq, sk, 2999, workspace=torch.empty(1 << 22, dtype=torch.float32, device="cuda"))
+    refused("both .int8 V. or neither", pre, q, t["kp8"], t["vp"], k, v, sq, t["skp"], sk, s_Vp=torch.ones(2, device="cuda"))
+    refused("Vp", pre, q, t["kp8"], t["vp"][:, 1:], k, v, sq, t["skp"], sk)
+    refused("at least one key", pre, q, t["kp8"][:, :0], t["vp"][:, :0], k, v, sq, t["skp"][:, :0], sk)
+    refused("W", ifa.key_weights, q, k, sq, sk, W=torch.zeros(2, 2, 2999, device="cuda"))
+    W = torch.zeros(2 * 2 * 3000 + 4, device="cuda")
+    refused("IFA_ERR_UNSUPPORTED", ifa.key_weights, q, k, sq, sk, W=W[:-4].view(2, 2, 3000), out=W[4:].view(2, 2, 3000))
+    W = W[4:].view(2, 2, 3000)
+    refused("1 <= keep", ifa.evict_keys, k, sk, v, W, 3001)
+    refused("1 <= keep", ifa.evict_keys, k, sk, v, W, 10, recent=8, sinks=3)
+    refused("V", ifa.evict_keys, k, sk, v.bfloat16(), W, 10)
+    refused("out", ifa.evict_keys, k, sk, v, W, 10, out=(k,))
+    d32 = torch.zeros(1, 1, 1, 32, dtype=torch.int8, device="cuda")
+    refused("not supported", win, d32, d32, d32.half(), torch.ones(1, 1, 1, device="cuda"), torch.ones(1, 1, 1, device="cuda"), 4)
