@@ -79,8 +79,8 @@ _native = None
 _NATIVE_PATH = os.path.join(_HERE, "_intfa_host.so")
 # the functions of the C ABI that the module calls, in its order
 _NATIVE_CALLS = ("quantize_tokenwise_ex", "quantize_headwise_ex", "quantize_blockwise", "quantize_qkv", "quantize_qk", "int_flash_attn_fwd_rect", "int_flash_attn_fwd_vblock_rect",
-                 "int_flash_attn_fwd_half_rect", "int_flash_attn_fwd_splitk", "int_flash_attn_fwd_splitk_static", "ifa_block_cols", "ifa_window_workspace_bytes", "int_flash_attn_fwd_window", "ifa_prefix_workspace_bytes",
-                 "int_flash_attn_fwd_prefix", "ifa_key_weights_workspace_bytes", "key_weights", "evict_keys")
+                 "int_flash_attn_fwd_half_rect", "int_flash_attn_fwd_splitk", "int_flash_attn_fwd_splitk_static", "ifa_window_workspace_bytes", "int_flash_attn_fwd_window", "ifa_prefix_workspace_bytes",
+                 "int_flash_attn_fwd_prefix", "ifa_key_weights_workspace_bytes", "key_weights", "evict_keys", "ifa_block_cols")
 
 
 def _address(fn):

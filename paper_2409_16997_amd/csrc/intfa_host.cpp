@@ -32,7 +32,6 @@ struct Abi {
     decltype(&::int_flash_attn_fwd_half_rect) half;
     decltype(&::int_flash_attn_fwd_splitk) splitk;
     decltype(&::int_flash_attn_fwd_splitk_static) splitk_static;
-    decltype(&::ifa_block_cols) block_cols;
     decltype(&::ifa_window_workspace_bytes) window_bytes;
     decltype(&::int_flash_attn_fwd_window) window;
     decltype(&::ifa_prefix_workspace_bytes) prefix_bytes;
@@ -40,6 +39,7 @@ struct Abi {
     decltype(&::ifa_key_weights_workspace_bytes) weights_bytes;
     decltype(&::key_weights) weights;
     decltype(&::evict_keys) evict;
+    decltype(&::ifa_block_cols) block_cols;
 } abi;
 constexpr int ABI_FUNCTIONS = sizeof(Abi) / sizeof(void *);
 PyObject *check = nullptr;                                       // the binding's: check(status, name of the call) raises what such a status raises
