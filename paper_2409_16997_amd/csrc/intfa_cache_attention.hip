@@ -458,13 +458,14 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
         for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
     const float unit_of_o = VI8 ? (ALL ? c.sVp : c.sV)[unit] : 1.0f;
 
+    const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows copies only
     wait_all_memory();
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int slot = (t - t0) & 1, v0 = TILE_KEYS * t;
         if (t + 1 < t1) stage(t + 1, slot ^ 1);
         // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
-        const bool any = hi1 >= v0 && (hi0 - window < v0 + TILE_KEYS - 1 || v0 < sink);
+        const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + TILE_KEYS - 1 || v0 < sink);
         const bool clear = hi0 >= v0 + TILE_KEYS - 1 && (hi1 - window < v0 || v0 + TILE_KEYS <= sink);
         const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
         if (any) tile_block<D, VI8>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, clear, seen, g, bias, st);

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCa
     for (int t = t0; t < t1; ++t) {
         const int slot = (t - t0) & 1, j0 = TILE_KEYS * t;
         if (t + 1 < t1) stage(t + 1, slot ^ 1);
-        if (w1 >= j0) {                                          // (wave-uniform)
+        if (w1 >= j0 && row0 + 32 * wave < rows) {               // (wave-uniform)
             float a[2][16];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
