@@ -545,15 +545,16 @@ struct EvictCall {
 };
 constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64, SEL_ROUND = 4 * SEL_THREADS, BINS = 2048;
 
-// Larger weight, larger number; -0 is 0, a NaN is below everything
+// Larger weight, larger number; -0 is 0, a NaN is below everything.  Between 1 and 0xff800000 (+inf): 0 is left for places without a key, the largest number for keys that stay anyway.
 __device__ __forceinline__ uint32_t order_of(float w) {
-    if (w != w) return 0;
     const uint32_t u = __float_as_uint(w + 0.0f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return w != w ? 1u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t NO_KEY = 0, STAYS = 0xffffffffu;
 
 // The keys go by in rounds of 4096: wavefront w has 256 of them in a row, its lanes 64 at a time.  ROUNDS: of buffers of at most so many rounds the weights are read once and stay in
-// registers; 0: longer ones are read again each time (from the caches: 4 bytes a key).
+// registers; 0: longer ones are read again each time (from the caches: 4 bytes a key).  What bounds it is the vector unit: 16 keys a lane, each looked at four times (sinks and
+// recent keys as the largest numbers rather than as conditions of their own: 15.8 us for 128 heads of 16384 keys, 18.5 before).
 template <int ROUNDS>
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) {
     __shared__ uint32_t bins[BINS];
@@ -571,6 +572,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
     const float *const W = c.W + static_cast<long>(unit) * c.Nk;
     const int first = c.sinks, last = n - c.recent;              // the keys that are chosen from: [first, last)
     const int mine = wave * 256 + lane;                          // (of a round: and 64, 128, 192 further on)
+    auto number = [&](int j, float w) { return j >= n ? NO_KEY : j < first || j >= last ? STAYS : order_of(w); };
     uint32_t kept[ROUNDS > 0 ? ROUNDS : 1][4];
     if constexpr (ROUNDS > 0) {
         float w[ROUNDS][4];
@@ -584,15 +586,15 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) kept[i][e] = order_of(w[i][e]);
+            for (int e = 0; e < 4; ++e) kept[i][e] = number(i * SEL_ROUND + mine + 64 * e, w[i][e]);
     }
-    // f(round, e, key, order of its weight) for every place of a round; all of them, so that wavefronts stay together
+    // f(place of a round, the number there) for every place of every round; all of them, so that wavefronts stay together.  after(round)
     auto rounds = [&](auto f, auto after) {
         auto one = [&](int i, int slot) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = i * SEL_ROUND + mine + 64 * e;
-                f(e, j, ROUNDS > 0 ? kept[slot][e] : j < n ? order_of(W[j]) : 0u);
+                f(e, ROUNDS > 0 ? kept[slot][e] : number(j, j < n ? W[j] : 0.0f));
             }
             after(i);
         };
@@ -603,15 +605,15 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
         } else
             for (int i = 0; i * SEL_ROUND < n; ++i) one(i, 0);
     };
-    uint32_t want = c.keep - c.sinks - c.recent, prefix = 0, mask = 0;
-    const bool none = want == 0;
-    // 11 + 11 + 10 bits from the top: the digit in which the want-th largest lies
-    for (int pass = 0; pass < 3 && !none; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+    // The want-th largest weight, 11 + 11 + 10 bits from the top.  Keys that stay anyway and places without one are left out of the first count (the later ones leave them out by
+    // their bits): so many equal numbers would queue at one bin.
+    uint32_t want = c.keep - c.sinks - c.recent, prefix = 0;
+    auto digit = [&](auto above, auto shift_) {                  // among the numbers whose bits from `above` on are `prefix`
+        constexpr int ABOVE = decltype(above)::value, SHIFT = decltype(shift_)::value, WIDTH = ABOVE - SHIFT;
         for (int i = tid; i < BINS; i += SEL_THREADS) bins[i] = 0;
         __syncthreads();
-        rounds([&](int, int j, uint32_t u) {
-            if (j >= first && j < last && (u & mask) == prefix) atomicAdd(&bins[(u >> shift) & ((1u << width) - 1)], 1u);
+        rounds([&](int, uint32_t u) {
+            if (ABOVE == 32 ? u + 1 > 1 : u >> (ABOVE & 31) == prefix) atomicAdd(&bins[u >> SHIFT & ((1u << WIDTH) - 1)], 1u);
         }, [](int) {});
         __syncthreads();
         // from the top bin down: thread t has bins 2047 - 2 t and the one below
@@ -631,18 +633,21 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
         if (before < want && want <= before + c0) found[0] = b0, found[1] = want - before;
         else if (before + c0 < want && want <= before + c0 + c1) found[0] = b0 - 1, found[1] = want - before - c0;
         __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= ((1u << width) - 1) << shift;
+        prefix = prefix << WIDTH | found[0];
         want = found[1];
-    }
-    // `prefix` is the order of the last weight that stays, `want` how many of those equal to it do: the first ones
+    };
+    if (want) {
+        digit(std::integral_constant<int, 32>{}, std::integral_constant<int, 21>{});
+        digit(std::integral_constant<int, 21>{}, std::integral_constant<int, 10>{});
+        digit(std::integral_constant<int, 10>{}, std::integral_constant<int, 0>{});
+    } else prefix = STAYS - 1;                                   // none by its weight
+    // `prefix` is the number of the last key that stays, `want` how many of those equal to it do: the first ones
     int base = 0, equal_base = 0, n_more = 0, n_equal = 0;
-    uint64_t more[4], equal[4];                                  // ballots
-    rounds([&](int e, int j, uint32_t u) {
-        const bool middle = j >= first && j < last && !none;
-        more[e] = __ballot(j < n && (j < first || j >= last || (middle && u > prefix)));
-        equal[e] = __ballot(middle && u == prefix);
-        n_more += __popcll(more[e]), n_equal += __popcll(equal[e]);
+    bool more[4], equal[4];
+    auto in_front = [](uint64_t ballot) { return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(ballot >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(ballot), 0))); };
+    rounds([&](int e, uint32_t u) {
+        more[e] = u > prefix, equal[e] = u == prefix;
+        n_more += __popcll(__ballot(more[e])), n_equal += __popcll(__ballot(equal[e]));
     }, [&](int i) {
         int2 *const all = counts[i & 1];
         if (lane == 0) all[wave] = int2{n_more, n_equal};
@@ -654,13 +659,13 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(EvictCall c) 
             if (w < wave) my_more += x.x, my_equal += x.y;
             base += x.x, equal_base += x.y;
         }
-        const uint64_t in_front = (1ull << lane) - 1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int rank = my_equal + __popcll(equal[e] & in_front);
-            const bool stays = (more[e] >> lane & 1) || ((equal[e] >> lane & 1) && rank < static_cast<int>(want));
-            if (stays) index[my_more + __popcll(more[e] & in_front) + imin(rank, static_cast<int>(want))] = i * SEL_ROUND + mine + 64 * e;
-            my_more += __popcll(more[e]), my_equal += __popcll(equal[e]);
+            const uint64_t bm = __ballot(more[e]), be = __ballot(equal[e]);
+            const int rank = my_equal + in_front(be);
+            if (more[e] || (equal[e] && rank < static_cast<int>(want)))
+                index[my_more + in_front(bm) + imin(rank, static_cast<int>(want))] = i * SEL_ROUND + mine + 64 * e;
+            my_more += __popcll(bm), my_equal += __popcll(be);
         }
         n_more = n_equal = 0;
     });
