@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, lo
 }
 
 // ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
-constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128)
+constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128) and the products
 __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, int units, int blocks, bool whole) {
     __shared__ float2 st[STORED_ROWS];
     const int unit = blockIdx.x / blocks, j = (blockIdx.x % blocks * 256 + threadIdx.x) * 4, rows = c.G * c.Nq;
@@ -471,9 +471,14 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     Plan p = {};
     p.stored = rows <= STORED_ROWS;
-    p.few = rows <= 32 || units * ((rows + 31) / 32) <= 128;
-    long parts = p.few ? 1024 / (units * ((rows + 31) / 32)) : 1024 / (units * ((rows + TILE_ROWS - 1) / TILE_ROWS));
-    if (parts > Nk / 512) parts = Nk / 512;
+    // The kernel for 32 rows up to 48 of its tiles, then tiles of 128 (8 key heads on 8192 keys, 32 rows / 128, us: 128 rows 19.5 / 20.6, 256 rows 26.0 / 24.2, 512 rows 34.8 / 30.9).
+    const long few_tiles = units * ((rows + 31) / 32), tiles = units * ((rows + TILE_ROWS - 1) / TILE_ROWS);
+    p.few = rows <= 32 || few_tiles <= 48;
+    // As many parts as there are places for 4 workgroups a CU (16 x 8 heads on up to 16384 keys 41.3 us, for 2 46.2; 32 x 800 rows on 8192 117.9 and 125.2), of at least 512 keys each, or 256 where few
+    // rows have to be joined (8 heads, 24 rows on 4096 keys 10.9 and 13.2; 64 rows on 8192 16.7 and 15.2).
+    long parts = 1024 / (p.few ? few_tiles : tiles);
+    const long least = rows <= 32 ? 256 : 512;
+    if (parts > Nk / least) parts = Nk / least;
     p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
     p.stats = p.parts > 1 || p.stored ? up(units * rows * p.parts * 8) : 0;
     p.stride = (Nk + 31L) / 32 * 32;
@@ -483,7 +488,7 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
     } else {
         p.rows = up(units * rows * 8);
         const long groups = units * ((Nk + KW_KEYS - 1) / KW_KEYS), most = (rows + KW_ROWS - 1) / KW_ROWS;
-        long slices = (1024 + groups - 1) / groups;
+        long slices = (1024 + groups - 1) / groups;              // four workgroups a CU here, too
         if (slices > most) slices = most;
         p.slices = static_cast<int>(slices < 1 ? 1 : slices > 64 ? 64 : slices);
         p.sums = p.slices > 1 ? up(units * Nk * 4L * p.slices) : 0;
