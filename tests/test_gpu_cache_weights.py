@@ -185,3 +185,29 @@ def test_graph_replays(ifa):
         eager = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(captured, eager))
+
+
+def test_offsets_beyond_32_bits(ifa):
+    """The last of 36 heads of 2^20 keys (4.8 GB of K, which is V, too): what it gives is what its last keys give in a cache of their own."""
+    H, N, d = 36, 1 << 20, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k8 = torch.randint(-127, 128, (1, H, N, d), dtype=torch.int8, device="cuda", generator=g)
+    sk = (torch.rand((1, H, N), device="cuda", generator=g) + 0.5) * 0.01
+    sv = torch.full((1, H), 0.01, device="cuda")
+    for Nq in (1, 400):                                  # the kernel for 32 rows, tiles of 128
+        q8 = torch.randint(-127, 128, (1, H, Nq, d), dtype=torch.int8, device="cuda", generator=g)
+        sq = (torch.rand((1, H, Nq), device="cuda", generator=g) + 0.5) * 3e-3
+        got = ifa.int_flash_attn_fwd_window(q8, k8, k8, sq, sk, 100, s_V=sv)
+        own = {"q8": q8[:, -1:], "sq": sq[:, -1:], "k8": k8[:, -1:, N - 600:], "sk": sk[:, -1:, N - 600:], "v": k8[:, -1:, N - 600:], "sv": sv[:, -1:]}
+        want, tol = ref.attention({k: x.cpu() for k, x in own.items()}, torch.float16, None, 100)
+        assert bool(((got[:, -1:].cpu().double() - want).abs() <= tol).all())
+    q8, sq = q8[:, :, :1].contiguous(), sq[:, :, :1].contiguous()
+    W = ifa.key_weights(q8, k8, sq, sk)
+    alone = ifa.key_weights(q8[:, -1:].contiguous(), k8[:, -1:], sq[:, -1:].contiguous(), sk[:, -1:].contiguous())
+    # each is off by less than 2 (8 max |S| 2^-24 + 2^-22) + 2^-22 + 2^-19 of itself (see cache_reference), max |S| < 40: 4.1e-5
+    assert bool(((W[:, -1:] - alone).abs() <= 1e-4 * alone).all()) and abs(W[:, -1].double().sum().item() - 1) < 1e-4
+    out = ifa.evict_keys(k8, sk, k8, W, 500, 20, 4)
+    index = out[4][0, -1].long()
+    assert torch.equal(out[0][0, -1], k8[0, -1, index]) and torch.equal(out[2][0, -1], k8[0, -1, index]) and torch.equal(out[1][0, -1], sk[0, -1, index])
+    assert index[:4].tolist() == [0, 1, 2, 3] and index[-1].item() == N - 1 and bool((index[1:] > index[:-1]).all())
+    assert torch.equal(index[4:-20], W[0, -1, 4:N - 20].topk(476).indices.sort().values + 4)
