@@ -384,10 +384,13 @@ __device__ __forceinline__ void store_rows(lds_ptr stage, int lane, Val val, At 
 }
 #endif
 
+// What a tile walks: the own keys through a window; the shared keys, for rows of the whole batch; or the shared keys and then the own ones of its sequence.
+enum Walk { OWN, SHARED, SHARED_AND_OWN };
 #if defined(__HIP_DEVICE_COMPILE__)
-template <int D, bool VI8, bool ALL>
+template <int D, bool VI8, Walk WALK>
 __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call &c, int block, int units, int row_tiles, int head_group) {
     constexpr int DT = D / 32, KB = TILE_KEYS * D, VB = TILE_KEYS * V_ROW<D, VI8>, KP = KB / 4096, VP = VB / 4096;
+    constexpr bool ALL = WALK == SHARED, FRONT = WALK == SHARED_AND_OWN;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
@@ -401,7 +404,8 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     // The two runs one after the other, cut into blocks of 64 with no seam: key v of them is key v for v < lenA, else key v + gap.  All of it lies in front of key pos1 + 1.
     const Runs runs(false, 0, window, ALL ? 0 : c.sinks, pos0, pos1);
     const int lenA = runs.lenA, gap = runs.lo - lenA, keys = lenA + runs.lenB;
-    const int blocks = (keys + TILE_KEYS - 1) / TILE_KEYS, per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
+    const int front = FRONT ? (c.Np + TILE_KEYS - 1) / TILE_KEYS : 0;            // blocks of shared keys in front
+    const int blocks = front + (keys + TILE_KEYS - 1) / TILE_KEYS, per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
     // a row at p sees key v iff v <= p - gap and (v > p - gap - window or v < sink); one at p < 0 none
     const int p = position(row), hi = p < 0 ? -1 : p - gap, sink = imax(lenA, (ALL ? 0 : c.sinks) - gap);
     const int w0 = position(imin(row0 + 32 * wave, last_row)), w1 = position(imin(row0 + 32 * wave + 31, last_row));      // of the wavefront's first and last row
@@ -412,11 +416,21 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     const long first_key = static_cast<long>(unit) * (ALL ? c.Np : c.Nk);
     const int seen_end = imax(0, pos1 + 1);
     const BufRsrc rK = make_rsrc(K + first_key * D, seen_end * D), rV = make_rsrc(V + first_key * V_ROW<D, VI8>, seen_end * V_ROW<D, VI8>), rS = make_rsrc(sK + first_key, seen_end * 4);
+    const long front_key = FRONT ? static_cast<long>(unit % c.Hkv) * c.Np : 0;
+    const BufRsrc fK = FRONT ? make_rsrc(c.Kp + front_key * D, c.Np * D) : rK,
+                  fV = FRONT ? make_rsrc(static_cast<const int8_t *>(c.Vp) + front_key * V_ROW<D, VI8>, c.Np * V_ROW<D, VI8>) : rV, fS = FRONT ? make_rsrc(c.sKp + front_key, c.Np * 4) : rS;
     const Lane<D, VI8> lo(lane);
     const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]);
     auto stage = [&](int t, int slot) {                          // a quarter of the block to each wavefront
         const lds_ptr kl = kbuf + slot * KB + wave * KP * 1024, vl = vbuf + slot * VB + wave * VP * 1024, sl = skbuf + slot * 256;
-        int v0 = TILE_KEYS * t;
+        if (FRONT && t < front) {
+            const int f0 = TILE_KEYS * t;
+            copy_pieces<KP>(fK, kl, lo.gk, lo.gk, f0 * D + wave * KP * 1024);
+            copy_pieces<VP>(fV, vl, lo.gv[0], lo.gv[1], f0 * V_ROW<D, VI8> + wave * VP * 1024);
+            if (wave == 3) lds_copy4(fS, sl, 4 * lane, f0 * 4);
+            return;
+        }
+        int v0 = TILE_KEYS * (t - front);
         if (v0 < lenA && v0 + TILE_KEYS > lenA) {                // the block with the seam: row by row
             constexpr int K_ROWS = 1024 / D, V_ROWS = 1024 / V_ROW<D, VI8>;
 #pragma unroll
@@ -443,7 +457,7 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     v4i qf[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;        // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
+    const float sq2 = FRONT || p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
     v16i bias;
@@ -456,18 +470,27 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
-    const float unit_of_o = VI8 ? (ALL ? c.sVp : c.sV)[unit] : 1.0f;
+    float unit_of_o = !VI8 ? 1.0f : FRONT && t0 < front ? c.sVp[unit % c.Hkv] : (ALL ? c.sVp : c.sV)[unit];
 
     const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows copies only
     wait_all_memory();
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-        const int slot = (t - t0) & 1, v0 = TILE_KEYS * t;
+        const int slot = (t - t0) & 1, v0 = TILE_KEYS * (t - front);
         if (t + 1 < t1) stage(t + 1, slot ^ 1);
+        if (VI8 && FRONT && t == front && t > t0) {              // from the shared keys' scale of V to the own ones', once
+            const float own = c.sV[unit], f = unit_of_o / own;
+            unit_of_o = own;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) st.o[dt][v] *= f;
+        }
+        const bool in_front = FRONT && t < front;
         // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
-        const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + TILE_KEYS - 1 || v0 < sink);
-        const bool clear = hi0 >= v0 + TILE_KEYS - 1 && (hi1 - window < v0 || v0 + TILE_KEYS <= sink);
-        const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
+        const bool any = alive && (in_front || (hi1 >= v0 && (hi0 - window < v0 + TILE_KEYS - 1 || v0 < sink)));
+        const bool clear = in_front ? TILE_KEYS * (t + 1) <= c.Np : hi0 >= v0 + TILE_KEYS - 1 && (hi1 - window < v0 || v0 + TILE_KEYS <= sink);
+        const uint64_t seen = clear ? 0 : in_front ? below(c.Np - TILE_KEYS * t) : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
         if (any) tile_block<D, VI8>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, lo, qf, sq2, clear, seen, g, bias, st);
         wait_all_memory();                                       // my part of the next block has landed
         __syncthreads();                                         // everyone's has, and this one's place is free
@@ -496,11 +519,11 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     else store(__hip_bfloat16{});
 }
 #endif
-template <int D, bool VI8, bool ALL>
+template <int D, bool VI8, Walk WALK>
 __global__ __launch_bounds__(256, 2) void cache_attention_tile_kernel(Call c, int units, int row_tiles, int head_group) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemTile<D, VI8> sm;
-    tile_of_a_unit<D, VI8, ALL>(sm, c, blockIdx.x, units, row_tiles, head_group);
+    tile_of_a_unit<D, VI8, WALK>(sm, c, blockIdx.x, units, row_tiles, head_group);
 #endif
 }
 
@@ -515,7 +538,7 @@ __global__ __launch_bounds__(256, 2) void cache_attention_both_kernel(Call share
         SmemFew<D, VI8, 1> few;
     } sm;
     if (static_cast<int>(blockIdx.x) >= blocks) few_rows_of_a_unit<D, VI8, false, 1, false>(sm.few, own, blockIdx.x - blocks, own_units, own_tiles);
-    else if constexpr (TILE) tile_of_a_unit<D, VI8, true>(sm.tile, shared, blockIdx.x, shared.Hkv, shared_tiles, head_group);
+    else if constexpr (TILE) tile_of_a_unit<D, VI8, SHARED>(sm.tile, shared, blockIdx.x, shared.Hkv, shared_tiles, head_group);
     else few_rows_of_a_unit<D, VI8, true, 1, false>(sm.few, shared, blockIdx.x, shared.Hkv, shared_tiles);
 #endif
 }
@@ -623,12 +646,16 @@ Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sink
     const long span = static_cast<long>(window) + imin(Nq, TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
     const bool few = few_rows(false, units, rows);
     p.own = parts_for(few ? 256 : 512, units * row_tiles(few, rows), keys, few ? 128 : 256);
-    // Few keys: every sequence reads the shared ones, too (2 sequences on 300 + 40 keys 6.2 us, with a launch for the parts 7.4; on 600 + 100 12.1 and 9.1)
-    if (Np > 0 && !(few && static_cast<long>(Np) + Nk < 512)) {
-        const long all = rows * B;
+    // Few keys: every sequence reads the shared ones, too (2 sequences on 300 + 40 keys 6.2 us, with a launch for the parts 7.4; on 600 + 100 12.1 and 9.1).  So it does with many rows of
+    // its own, unless tiles of the batch's rows on the shared keys are so many fewer that it pays for the parts: 8 x 8 heads, 4 x 512 queries on 2048 + 512 keys 143 us, with parts 184;
+    // 64 x 8 heads, 8 x 10 queries on 4000 + 50 (64 tiles a head for 40: 2400 keys a tile) 106 and 117; 6 x 8 heads, 4 x 40 queries on 32000 + 50 (12 for 8: 16000) 169 and 136.
+    if (Np > 0) {
+        const long all = rows * B, all_tiles = row_tiles(false, all);
+        const bool parts = few ? static_cast<long>(Np) + Nk >= 512 : (B * row_tiles(false, rows) - all_tiles) * Np > 6000 * all_tiles;
         // (own keys in the same launch: a place on every CU is left to them; 64 sequences x 8 heads on 8192 + 512 keys 28.5 us, with 384 places 34, with 512 38)
-        p.shared = parts_for(few ? 256 : 512, Hkv * row_tiles(few_rows(true, Hkv, all), all), Np, 256);
+        if (parts) p.shared = parts_for(few ? 256 : 512, Hkv * row_tiles(few_rows(true, Hkv, all), all), Np, 256);
         p.rows_shared = Hkv * all * p.shared;
+        if (!few && !parts) p.own = parts_for(512, units * row_tiles(false, rows), keys + Np, 256);
     }
     p.rows_own = p.join() ? units * rows * p.own : 0;
     return p;
@@ -639,9 +666,9 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv;
     float *const o = static_cast<float *>(workspace);
     float2 *const ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
-    auto tiles = [&](auto all, const Call &k, int n_units) {
+    auto tiles = [&](auto walk, const Call &k, int n_units) {
         const int n = static_cast<int>(row_tiles(false, k.rows));
-        hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(all)::value>), dim3(static_cast<unsigned>(static_cast<long>(n_units) * n * k.splits)), dim3(256), 0, st, k, n_units, n,
+        hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(walk)::value>), dim3(static_cast<unsigned>(static_cast<long>(n_units) * n * k.splits)), dim3(256), 0, st, k, n_units, n,
                            head_group_for(true, 0, 0));
     };
     auto few = [&](const Call &k) {
@@ -681,9 +708,11 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
                                units, own_tiles, head_group_for(true, 0, 0));
         };
         shared_few ? both(std::false_type{}) : both(std::true_type{});
-    } else {
-        if (plan.shared > 0) tiles(std::true_type{}, shared, c.Hkv);         // (more rows than own_few has: tiles)
-        own_few ? few(c) : tiles(std::false_type{}, c, units);
+    } else if (own_few) few(c);
+    else if (c.Kp) tiles(std::integral_constant<Walk, SHARED_AND_OWN>{}, c, units);
+    else {
+        if (plan.shared > 0) tiles(std::integral_constant<Walk, SHARED>{}, shared, c.Hkv);       // (more rows than few_rows() has)
+        tiles(std::integral_constant<Walk, OWN>{}, c, units);
     }
     if (plan.join()) {
         const Parts parts = {o, c.part_o, ml, c.part_ml, plan.shared, plan.own};

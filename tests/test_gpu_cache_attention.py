@@ -85,6 +85,8 @@ PREFIXES = [
     (33, 2, 1, 1, 1500, 9, 128, None),
     (4, 4, 4, 80, 600, 300, 64, (300, 0, 81, 200)),      # prompts behind a prefix: tiles of 128 rows for both
     (3, 8, 2, 100, 70, 100, 128, (100, 99, 1)),
+    (2, 4, 3, 200, 1500, 70, 64, (0, 69)),               # ... the keys of both in parts
+    (9, 8, 2, 20, 7000, 30, 64, None),                   # ... the shared ones for the whole batch
 ]
 
 
