@@ -35,6 +35,10 @@ __device__ __forceinline__ long row_of(const Call &c, bool all, int unit, int ro
     return (static_cast<long>(b * c.Hkv + hk) * c.G + g) * c.Nq + i;
 }
 
+// INT8 V: o is in units of one scale.  Own V whose scale is 0, or vanishes beside the shared one's so that the ratio of the two could leave the range of fp32 (|o| < 2^46), is
+// taken as the zeros it is then: its keys have their weights, its values are not read and o stays in the shared keys' units.
+__device__ __forceinline__ bool counts_as_zero(float own, float shared) { return fabsf(own) <= fabsf(shared) * 0x1p-64f; }
+
 // ---- 32 rows against many keys: every wavefront for itself -------------------------------------------------------
 // The four wavefronts of a workgroup hold the same 32 rows and take every fourth tile of 32 keys each, with an online softmax of their own; they meet
 // once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
@@ -82,6 +86,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
     const BufRsrc rKB = ALL ? rKA : make_rsrc(c.K + kB * D, runs.lenB * D), rVB = ALL ? rVA : make_rsrc(vB + kB * V_ROW<D, VI8>, runs.lenB * V_ROW<D, VI8>),
                   rSB = ALL ? rSA : make_rsrc(c.sK + kB, runs.lenB * 4);
     const float unitA = VI8 ? (shared ? c.sVp[hk] : c.sV[unit]) : 1.0f, unitB = VI8 && !ALL ? c.sV[unit] : unitA;
+    const bool zeros = VI8 && !ALL && counts_as_zero(unitB, unitA);
 
     const Lane<D, VI8> lo(lane);
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]);
@@ -90,7 +95,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
         const int j0 = 32 * (inA ? t : t - tilesA);
         const bool real = t < t1;
         copy_pieces<K_PIECES<D>, NT>(pick(inA, rKA, rKB), kbuf + slot * KB, lo.gk, lo.gk, real ? j0 * D : NOTHING);
-        copy_pieces<V_PIECES<D, VI8>, NT>(pick(inA, rVA, rVB), vbuf + slot * VB, lo.gv[0], lo.gv[1], real ? j0 * V_ROW<D, VI8> : NOTHING);
+        copy_pieces<V_PIECES<D, VI8>, NT>(pick(inA, rVA, rVB), vbuf + slot * VB, lo.gv[0], lo.gv[1], real && (inA || !zeros) ? j0 * V_ROW<D, VI8> : NOTHING);
         if (g == 0) lds_copy4(pick(inA, rSA, rSB), skbuf + slot * 128, 4 * r, real ? j0 * 4 : NOTHING);
     };
     const int first = t0 + wave;
@@ -175,7 +180,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
             psum = __builtin_amdgcn_fdot2(ph[e], ones, psum, false);
         }
         l = __builtin_fmaf(l, alpha, psum);
-        if (VI8 && !inA && t - FEW_WAVES < tilesA) {             // from the shared keys' scale of V to the own ones', once
+        if (VI8 && !inA && !zeros && unit_of_o != unitB) {       // from the shared keys' scale of V to the own ones', once
             alpha *= unit_of_o / unitB;
             unit_of_o = unitB;
         }
@@ -419,6 +424,8 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     const long front_key = FRONT ? static_cast<long>(unit % c.Hkv) * c.Np : 0;
     const BufRsrc fK = FRONT ? make_rsrc(c.Kp + front_key * D, c.Np * D) : rK,
                   fV = FRONT ? make_rsrc(static_cast<const int8_t *>(c.Vp) + front_key * V_ROW<D, VI8>, c.Np * V_ROW<D, VI8>) : rV, fS = FRONT ? make_rsrc(c.sKp + front_key, c.Np * 4) : rS;
+    const float unit_own = VI8 ? (ALL ? c.sVp : c.sV)[unit] : 1.0f, unit_front = VI8 && FRONT ? c.sVp[unit % c.Hkv] : unit_own;
+    const bool zeros = VI8 && FRONT && counts_as_zero(unit_own, unit_front);
     const Lane<D, VI8> lo(lane);
     const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]);
     auto stage = [&](int t, int slot) {                          // a quarter of the block to each wavefront
@@ -448,7 +455,7 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
         }
         if (v0 >= lenA) v0 += gap;
         copy_pieces<KP>(rK, kl, lo.gk, lo.gk, v0 * D + wave * KP * 1024);
-        copy_pieces<VP>(rV, vl, lo.gv[0], lo.gv[1], v0 * V_ROW<D, VI8> + wave * VP * 1024);
+        copy_pieces<VP>(rV, vl, lo.gv[0], lo.gv[1], zeros ? NOTHING : v0 * V_ROW<D, VI8> + wave * VP * 1024);
         if (wave == 3) lds_copy4(rS, sl, 4 * lane, v0 * 4);
     };
     if (t0 < t1) stage(t0, 0);
@@ -470,7 +477,7 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
-    float unit_of_o = !VI8 ? 1.0f : FRONT && t0 < front ? c.sVp[unit % c.Hkv] : (ALL ? c.sVp : c.sV)[unit];
+    float unit_of_o = t0 < front ? unit_front : unit_own;
 
     const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows copies only
     wait_all_memory();
@@ -478,9 +485,9 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     for (int t = t0; t < t1; ++t) {
         const int slot = (t - t0) & 1, v0 = TILE_KEYS * (t - front);
         if (t + 1 < t1) stage(t + 1, slot ^ 1);
-        if (VI8 && FRONT && t == front && t > t0) {              // from the shared keys' scale of V to the own ones', once
-            const float own = c.sV[unit], f = unit_of_o / own;
-            unit_of_o = own;
+        if (VI8 && FRONT && t == front && t > t0 && !zeros) {    // from the shared keys' scale of V to the own ones', once
+            const float f = unit_of_o / unit_own;
+            unit_of_o = unit_own;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

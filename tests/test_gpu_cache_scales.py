@@ -1,0 +1,95 @@
+"""Scales at the edge of their range in the calls on a quantized cache, on every way through the kernels, against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import cache_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ifa():
+    import paper_2409_16997_amd as ifa
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return ifa
+
+
+def dev_lens(lens):
+    return None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+def window(ifa, s, w, sinks, lens=None, **kw):
+    t = ref.on_gpu(s)
+    return ifa.int_flash_attn_fwd_window(t["q8"], t["k8"], t["v"], t["sq"], t["sk"], w, sinks, s_V=t["sv"], lens=dev_lens(lens), **kw)
+
+
+def prefix(ifa, s, lens=None, **kw):
+    t = ref.on_gpu(s)
+    return ifa.int_flash_attn_fwd_prefix(t["q8"], t["kp8"], t["vp"], t["k8"], t["v"], t["sq"], t["skp"], t["sk"], s_Vp=t["svp"], s_V=t["sv"], lens=dev_lens(lens), **kw)
+
+
+def check(got, want, tol):
+    got = got.cpu().double()
+    assert bool(torch.isfinite(got).all()), "not finite"
+    off = (got - want).abs()
+    assert bool((off <= tol).all()), f"off by up to {(off / tol.clamp_min(1e-300)).max().item():.3f} of the tolerance"
+
+
+# B, Hkv, G, Nq, Nk, d, window, sinks, lens
+WINDOWS = {
+    "32 rows": (2, 2, 4, 1, 300, 128, 64, 4, (300, 257)),
+    "32 rows, in parts": (1, 1, 8, 2, 5000, 64, 4096, 4, None),
+    "tiles": (1, 16, 3, 170, 333, 128, 70, 64, (331,)),
+    "tiles, in parts": (1, 8, 4, 140, 2600, 64, 2000, 5, None),
+}
+# B, Hkv, G, Nq, Np, Nk, d, lens
+PREFIXES = {
+    "32 rows": (2, 2, 1, 1, 300, 40, 64, (40, 7)),
+    "both, 32 rows": (3, 1, 4, 1, 700, 65, 128, (65, 0, 1)),
+    "both, tiles": (40, 1, 4, 1, 2000, 200, 64, None),
+    "shared tiles, own tiles": (9, 8, 2, 20, 7000, 30, 64, (30, 0, 1, 19, 20, 21, 30, 5, 30)),
+    "tiles of both": (3, 8, 2, 100, 70, 100, 128, (100, 99, 1)),
+    "tiles of both, in parts": (2, 4, 3, 200, 1000, 300, 64, (300, 0)),
+}
+
+
+@pytest.mark.parametrize("name", WINDOWS)
+def test_window_with_values_of_no_scale(ifa, name):
+    """s_V = 0 in some heads, and in all: zeros."""
+    B, Hkv, G, Nq, Nk, d, w, sinks, lens = WINDOWS[name]
+    s = ref.problem(41, B, Hkv, G, Nq, Nk, d, v="int8")
+    for zero in (slice(0, None, 2), slice(None)):
+        s["sv"][:, zero] = 0.0
+        want, tol = ref.attention(s, torch.float32, lens, w, sinks)
+        check(window(ifa, s, w, sinks, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("which", ["one sequence's", "all own", "shared", "all"])
+@pytest.mark.parametrize("name", PREFIXES)
+def test_prefix_with_values_of_no_scale(ifa, name, which):
+    B, Hkv, G, Nq, Np, Nk, d, lens = PREFIXES[name]
+    s = ref.problem(42, B, Hkv, G, Nq, Nk, d, Np=Np, v="int8")
+    if which == "one sequence's":
+        s["sv"][0] = 0.0
+    if which in ("all own", "all"):
+        s["sv"][:] = 0.0
+    if which in ("shared", "all"):
+        s["svp"][:] = 0.0
+    want, tol = ref.attention(s, torch.float32, lens)
+    check(prefix(ifa, s, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("own,shared", [(1e-36, 1.0), (1e-30, 1.0), (1e-12, 100.0), (1.0, 1e-30), (100.0, 1e-12)])
+@pytest.mark.parametrize("name", PREFIXES)
+def test_prefix_with_scales_far_apart(ifa, name, own, shared):
+    """Own and shared V, one of which next to vanishes beside the other.  (Where a scale that is 2^-64 of the other counts as 0, that is 2^-57 of the values beside it: far inside the
+    tolerance, which allows 2^-25 of them.)"""
+    B, Hkv, G, Nq, Np, Nk, d, lens = PREFIXES[name]
+    s = ref.problem(43, B, Hkv, G, Nq, Nk, d, Np=Np, v="int8")
+    s["sv"] *= own
+    s["svp"] *= shared
+    want, tol = ref.attention(s, torch.float32, lens)
+    check(prefix(ifa, s, lens, out_dtype=torch.float32), want, tol)
