@@ -510,7 +510,8 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
         const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows;
         const int n = c.rows;
         float *const po = c.part_o + pr * D;
-        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * unit_of_o; },
+        const float u = st.m2 == -INFINITY ? 0.0f : unit_of_o;   // (a part without keys of its row: zeros, whatever the scale that it did not use is)
+        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * u; },
                              [&](int k) { return first + k < n ? reinterpret_cast<char *>(po + static_cast<long>(first + k) * D) : nullptr; });
         if (g == 0 && first + r < n) c.part_ml[pr + first + r] = float2{st.m2, l};
         return;

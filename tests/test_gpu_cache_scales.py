@@ -93,3 +93,30 @@ def test_prefix_with_scales_far_apart(ifa, name, own, shared):
     s["svp"] *= shared
     want, tol = ref.attention(s, torch.float32, lens)
     check(prefix(ifa, s, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("v", ["int8", "fp16"])
+@pytest.mark.parametrize("name", list(PREFIXES) + ["tiles, many own parts"])
+def test_what_an_empty_sequence_holds_does_not_matter(ifa, name, v, bad):
+    """A cache slot of a batch that has no keys yet, behind a prefix: whatever lies in its s_V, V and s_K, its queries get what the shared keys give."""
+    B, Hkv, G, Nq, Np, Nk, d, _ = dict(PREFIXES, **{"tiles, many own parts": (3, 1, 2, 600, 4000, 2100, 64, None)})[name]
+    lens = [Nk if b % 2 else 0 for b in range(B)]
+    s = ref.problem(44, B, Hkv, G, Nq, Nk, d, Np=Np, v=v)
+    want, tol = ref.attention(s, torch.float32, lens)
+    for b in range(0, B, 2):
+        s["sk"][b] = bad
+        if v == "int8":
+            s["sv"][b] = bad
+        else:
+            s["v"][b] = bad
+    check(prefix(ifa, s, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("name", WINDOWS)
+def test_what_an_empty_sequence_of_a_window_holds_does_not_matter(ifa, name):
+    B, Hkv, G, Nq, Nk, d, w, sinks, _ = WINDOWS[name]
+    s = ref.problem(45, B, Hkv, G, Nq, Nk, d, v="int8")
+    s["sv"][:], s["sk"][:] = math.nan, math.nan
+    got = window(ifa, s, w, sinks, [0] * B, out_dtype=torch.float32)
+    assert bool((got == 0).all())
