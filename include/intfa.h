@@ -265,7 +265,8 @@ int int_flash_attn_fwd_half_rect(const signed char *Q_i8, const signed char *K_i
  * positions: query i stands at p = L_b - Nq + i and sees own keys j <= p.  A query at p < 0 (padding in front, an empty
  * sequence) sees no own key; one that sees no key at all gives zeros,
  * whatever its codes and scale are.
- *   s_V and s_Vp may be 0: such values are zeros, their keys keep their weights.  (Where both kinds of keys meet, an own s_V of at most 2^-64 of the shared one counts as 0, too.)
+ *   Scales: s_Q >= 0; a query whose s_Q is 0 scores 0 with every key, i.e. all that it sees weigh the same.  s_K may be any finite number.
+ * s_V and s_Vp may be 0: such values are zeros, their keys keep their weights.  (Where both kinds of keys meet, an own s_V of at most 2^-64 of the shared one counts as 0, too.)
  *   The weights are those of the half-INT8 variant, whatever V is: P~ = fp16(exp(S - m)), l the sum of the rounded weights, O = P~ V / l
  * (times s_V) with fp32 accumulation.  Unlike Algorithm 1's INT8 P they do not lie on the grid of a running maximum, so the result depends
  * on how the keys are shared out over the chip only by the rounding of a weight (2^-11 of it) and the order of fp32 additions.

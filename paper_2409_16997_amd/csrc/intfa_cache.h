@@ -145,6 +145,16 @@ constexpr int NOTHING = 0x7fff0000;
 __device__ __forceinline__ BufRsrc pick(bool a, const BufRsrc &x, const BufRsrc &y) {
     return {{a ? x.w[0] : y.w[0], a ? x.w[1] : y.w[1], a ? x.w[2] : y.w[2], x.w[3]}};
 }
+// s_Q log2(e) of a live query.  One whose scale is 0 scores 0 with every key: its codes become 0 and its scale 1, so that the -inf of masked scores, to which the scale comes last,
+// is never multiplied by 0.
+template <int KS> __device__ __forceinline__ float query_scale(float sq, v4i (&codes)[KS]) {
+    if (sq == 0.0f) {
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) codes[kk] = v4i{0, 0, 0, 0};
+        sq = 1.0f;
+    }
+    return sq * LOG2E;
+}
 // Copies into LDS are assembly that the compiler does not see write memory: nothing is read across this.
 __device__ __forceinline__ void memory_fence_of_the_compiler() { asm volatile("" ::: "memory"); }
 

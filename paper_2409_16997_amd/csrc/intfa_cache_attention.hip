@@ -106,7 +106,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
     v4i qf[KS];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = shared || p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
+    const float sq2 = shared || p >= 0 ? query_scale(c.sQ[qrow], qf) : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));    // landed before the loop
     v16i bias;
@@ -464,7 +464,7 @@ __device__ __forceinline__ void tile_of_a_unit(SmemTile<D, VI8> &sm, const Call 
     v4i qf[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = FRONT || p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
+    const float sq2 = FRONT || p >= 0 ? query_scale(c.sQ[qrow], qf) : 1.0f;       // (padding: whatever its scale holds, 0 and NaN too, its row is zeros)
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
     v16i bias;

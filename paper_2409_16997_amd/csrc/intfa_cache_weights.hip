@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 4) void key_weights_row_tiles_kernel(WeightsCa
     v4i qf[KS];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = p >= 0 ? c.sQ[qrow] * LOG2E : 1.0f;        // (padding: whatever its scale holds)
+    const float sq2 = p >= 0 ? query_scale(c.sQ[qrow], qf) : 1.0f;        // (padding: whatever its scale holds)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[kk]));
     v16i bias;

@@ -120,3 +120,59 @@ def test_what_an_empty_sequence_of_a_window_holds_does_not_matter(ifa, name):
     s["sv"][:], s["sk"][:] = math.nan, math.nan
     got = window(ifa, s, w, sinks, [0] * B, out_dtype=torch.float32)
     assert bool((got == 0).all())
+
+
+def queries_without_a_scale(s):
+    """Every third query row's s_Q 0, the next a subnormal number."""
+    flat = s["sq"].view(-1)
+    flat[::3] = 0.0
+    flat[1::3] = 1e-42
+    return s
+
+
+@pytest.mark.parametrize("name", WINDOWS)
+def test_window_with_queries_of_no_scale(ifa, name):
+    """s_Q = 0: every score is 0, so all keys that the query sees weigh the same."""
+    B, Hkv, G, Nq, Nk, d, w, sinks, lens = WINDOWS[name]
+    s = queries_without_a_scale(ref.problem(46, B, Hkv, G, Nq, Nk, d))
+    want, tol = ref.attention(s, torch.float32, lens, w, sinks)
+    check(window(ifa, s, w, sinks, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("name", PREFIXES)
+def test_prefix_with_queries_of_no_scale(ifa, name):
+    B, Hkv, G, Nq, Np, Nk, d, lens = PREFIXES[name]
+    s = queries_without_a_scale(ref.problem(47, B, Hkv, G, Nq, Nk, d, Np=Np))
+    want, tol = ref.attention(s, torch.float32, lens)
+    check(prefix(ifa, s, lens, out_dtype=torch.float32), want, tol)
+
+
+# B, Hkv, G, Nq, Nk, d, lens
+WEIGHTS = {
+    "stored scores": (2, 2, 4, 2, 700, 64, (700, 1)),
+    "32 rows": (1, 2, 3, 40, 300, 128, (299,)),
+    "tiles": (1, 20, 3, 80, 200, 64, (190,)),
+    "tiles, in parts": (2, 8, 2, 150, 1200, 128, (1200, 700)),
+}
+
+
+@pytest.mark.parametrize("name", WEIGHTS)
+def test_key_weights_with_queries_of_no_scale(ifa, name):
+    B, Hkv, G, Nq, Nk, d, lens = WEIGHTS[name]
+    s = queries_without_a_scale(ref.problem(48, B, Hkv, G, Nq, Nk, d))
+    want, tol = ref.key_weights(s, lens)
+    t = ref.on_gpu(s)
+    check(ifa.key_weights(t["q8"], t["k8"], t["sq"], t["sk"], lens=dev_lens(lens)), want, tol)
+
+
+@pytest.mark.parametrize("name", WEIGHTS)
+def test_keys_of_no_scale(ifa, name):
+    """s_K = 0: such keys score 0 with every query."""
+    B, Hkv, G, Nq, Nk, d, lens = WEIGHTS[name]
+    s = ref.problem(49, B, Hkv, G, Nq, Nk, d)
+    s["sk"].view(-1)[::3] = 0.0
+    want, tol = ref.key_weights(s, lens)
+    t = ref.on_gpu(s)
+    check(ifa.key_weights(t["q8"], t["k8"], t["sq"], t["sk"], lens=dev_lens(lens)), want, tol)
+    want, tol = ref.attention(s, torch.float32, lens, 100, 3)
+    check(window(ifa, s, 100, 3, lens, out_dtype=torch.float32), want, tol)
