@@ -267,9 +267,10 @@ int int_flash_attn_fwd_half_rect(const signed char *Q_i8, const signed char *K_i
  * whatever its codes and scale are.
  *   Scales: s_Q >= 0; a query whose s_Q is 0 scores 0 with every key, i.e. all that it sees weigh the same.  s_K may be any finite number.
  * s_V and s_Vp may be 0: such values are zeros, their keys keep their weights.  (Where both kinds of keys meet, an own s_V of at most 2^-64 of the shared one counts as 0, too.)
- *   The weights are those of the half-INT8 variant, whatever V is: P~ = fp16(exp(S - m)), l the sum of the rounded weights, O = P~ V / l
+ *   The weights are fp16 like those of the half-INT8 variant, whatever V is: P~ = fp16(exp(S - m)), l the sum of the rounded weights, O = P~ V / l
  * (times s_V) with fp32 accumulation.  Unlike Algorithm 1's INT8 P they do not lie on the grid of a running maximum, so the result depends
- * on how the keys are shared out over the chip only by the rounding of a weight (2^-11 of it) and the order of fp32 additions.
+ * on how the keys are shared out over the chip only by the rounding of a weight and the order of fp32 additions.  A weight is rounded by at most 2^-11 of itself, or by 2^-40 (where a
+ * tile of 128 rows is worked on together: 2^-32) of the largest weight of its row so far if that is more: smaller ones than that may count as 0.
  * Supported: d in {64, 128}; H a multiple of Hkv; 2 Nk d and 2 Np d <= 0x7ff00000; B H <= 2^23, B H Nq <= 2^26.
  *   Workspaces: device memory, 256-byte aligned, owned by the caller, contents undefined before and after, not to be shared by calls
  * that may overlap (two streams, two captured graphs that may replay at once).  The ..._workspace_bytes functions return the bytes needed (0: none, the pointer may be null), -1 for

@@ -1,11 +1,13 @@
 // Attention over a quantized cache for gfx950: with a sliding window and sinks, and over keys that a batch shares.
 //
 //     S = s_Q s_K (Q K^T)        v_mfma_i32_32x32x32_i8, exact in int32, fp32 scales
-//     P~ = fp16(exp(S - m))      m the running maximum; l = the sum of the rounded weights in fp32
+//     P~ = fp16(exp(S - m))      m 15 (in tiles of 128 rows 7 to 15) log2 units below the running maximum; l = the sum of the rounded weights in fp32
 //     O = P~ V / l               v_mfma_f32_32x32x16_f16, fp32 accumulation; INT8 V enters as fp16 (exactly) and its scale meets O
 //
-// The weights are those of the half-INT8 variant, for INT8 V too: rounded relative to themselves (2^-11) rather than on the grid of a running maximum,
-// they do not depend on where a sequence is cut, so its keys may be shared out over workgroups and the parts joined with e^{m_part - m}.
+// The weights are fp16 like those of the half-INT8 variant, for INT8 V too: rounded relative to themselves (2^-11) rather than on the grid of a running maximum, they hardly
+// depend on where a sequence is cut, so its keys may be shared out over workgroups and the parts joined with e^{m_part - m}.  What ends that is the lower end of fp16: below 2^-14 a weight is
+// rounded by 2^-25, whatever it is.  With the largest weight near the upper end rather than at 1 those 2^-25 are 2^-40 of it (tiles: 2^-32 at worst), so that a long rest of small weights
+// counts: with 1 as the largest weight what 16384 keys give 18 nats below the first was 25 % off (tiles, 9000 keys: 100 %), like this .01 % (.9 %), in the same time.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_bf16.h>
@@ -44,6 +46,7 @@ __device__ __forceinline__ bool counts_as_zero(float own, float shared) { return
 // once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
 // asks for the one that goes into its place before it computes.  What bounds it is memory: 32 sequences x 8 heads on 4096 keys of d = 128 in 66.5 us, 6.1 TB/s.
 constexpr int FEW_WAVES = 4;
+constexpr float FEW_BELOW = 15.0f;                               // the largest weight is 2^15
 template <int D, bool VI8, int ST> struct SmemFew {
     static constexpr int KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
     union {
@@ -114,7 +117,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
     for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I;
     asm volatile("" : "+v"(bias));
 
-    float m2 = -INFINITY, l = 0.0f, unit_of_o = first < tilesA ? unitA : unitB;
+    float m2 = -INFINITY, l = 0.0f, unit_of_o = first < tilesA ? unitA : unitB;      // m2: what the weights refer to, FEW_BELOW under the maximum
     v16f o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -167,7 +170,7 @@ __device__ __forceinline__ void few_rows_of_a_unit(SmemFew<D, VI8, ST> &sm, cons
 #pragma unroll
         for (int v = 0; v < 16; ++v) tmax = fmaxf(tmax, a[v]);
         tmax = pair_max(tmax);
-        const float m_new = fmaxf(m2, tmax * sq2);
+        const float m_new = fmaxf(m2, __builtin_fmaf(tmax, sq2, -FEW_BELOW));
         const float m_at = m_new == -INFINITY ? 0.0f : m_new;    // a row that has seen nothing yet: weights of 0, no NaN
         float alpha = __builtin_amdgcn_exp2f(m2 - m_at);         // exp2(-inf) = 0
         m2 = m_new;
@@ -258,8 +261,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 // Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered).  What bounds it is the vector unit: 32 keys of 32 rows are 12 matrix
 // instructions (384 cycles at d = 128), and of the vector instructions on each of their scores (subtract the start value, s_K, the maximum, s_Q and m, exp2, the conversion
 // in pairs, the sum in pairs) exp2 alone takes 16 cycles: 1111 vector cycles of the 2060 that 64 keys take a wavefront, 769 of the matrix unit (the chip runs it at 1.8 - 2.0 GHz).
-// So the running maximum only moves when a block exceeds it by 2^8 (a row by itself: what a row gives does not depend on its neighbours), which an fp16 weight holds as well
-// as a weight of 1, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made.
+// So the number that the weights refer to, 2^7 under the maximum when it was taken, only moves when a block exceeds that maximum by 2^8 (a row by itself: what a row gives does not depend on
+// its neighbours), which fp16 weights of up to 2^15 hold, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made.
 constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
 template <int D, bool VI8> struct SmemTile {
     alignas(4096) int8_t k[2][TILE_KEYS * D];
@@ -269,10 +272,10 @@ template <int D, bool VI8> struct SmemTile {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 template <int D> struct RowState {
-    float m2, l;                                                 // m2: the maximum that the weights refer to, log2 units
+    float m2, l;                                                 // m2: what the weights refer to, log2 units
     v16f o[D / 32];
 };
-constexpr float SLACK = 8.0f;
+constexpr float SLACK = 8.0f, TILE_BELOW = 7.0f;                 // (below a maximum that may be exceeded: weights of up to 2^15)
 
 // 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.  (One body for both, with a branch around
 // the mask alone: two bodies and o would be moved from one's registers to the other's at every block.)
@@ -313,7 +316,7 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
 #pragma unroll
         for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
     __builtin_amdgcn_sched_barrier(0);
-    const float top = pair_max(bmax) * sq2;
+    const float top = __builtin_fmaf(pair_max(bmax), sq2, -TILE_BELOW);
     const bool moves = top > st.m2 + SLACK;                      // (st.m2 = -inf: whenever a key counts)
     if (__any(moves)) {
         const float m_new = moves ? top : st.m2;
@@ -328,9 +331,10 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
     const float m = st.m2 == -INFINITY ? 0.0f : st.m2; // a row that has seen nothing yet: weights of 0, no NaN
     const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
     h2 ph[2][8];
+    float sum = 0.0f;                                            // of the block: small weights do not meet l one by one
     auto weights = [&](int mt, int e) {
         ph[mt][e] = h2{(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e], sq2, -m)), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][2 * e + 1], sq2, -m))};
-        st.l = __builtin_amdgcn_fdot2(ph[mt][e], ones, st.l, false);
+        sum = __builtin_amdgcn_fdot2(ph[mt][e], ones, sum, false);
     };
     // the weights of the second 32 keys between the products of the first
     h8 vop[DT][2];
@@ -356,6 +360,7 @@ __device__ __forceinline__ void tile_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, c
                 for (int q = 0; q < 8 / DT; ++q) weights(1, dt * (8 / DT) + q);
             }
         }
+    st.l += sum;
     __builtin_amdgcn_s_setprio(0);
 }
 
