@@ -317,7 +317,7 @@ int key_weights(const signed char *Q_i8, const signed char *K_i8, const float *s
  * W (of equal ones the first; a NaN is below everything) stay, in their order; with L_b <= keep all do.
  *   K_out [B, Hkv, keep, d], s_K_out, W_out [B, Hkv, keep], V_out [B, Hkv, keep, d] (V of v_bytes = 1 or 2 bytes an element): the rows that stay, then zeros
  *   index [B, Hkv, keep] int32: which key each was, then -1;  lens_out [B] int32: min(L_b, keep)
- * s_V of an INT8 V stays as it is.  1 <= keep <= Nk, sinks + recent <= keep; d a multiple of 16 up to 1024.  Nothing is evicted in place: outputs that overlap an input or each
+ * s_V of an INT8 V stays as it is.  1 <= keep <= Nk, sinks + recent <= keep; d a multiple of 16 up to 1024, Nk < 2^31 - 8192, B Hkv < 2^22, B Hkv keep d <= 2^35.  Nothing is evicted in place: outputs that overlap an input or each
  * other are refused (IFA_ERR_UNSUPPORTED).  Two launches, no workspace.
  */
 int evict_keys(const signed char *K_i8, const float *s_K, const void *V, int v_bytes, const float *W, const int *lens,

@@ -763,7 +763,7 @@ extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void 
     const long units = static_cast<long>(B) * Hkv;
     if (keep > Nk || static_cast<long>(recent) + sinks > keep || units > (1L << 40) / Nk / d) return IFA_ERR_SHAPE;
     if (v_bytes != 1 && v_bytes != 2) return IFA_ERR_DTYPE;
-    if ((d & 15) || d > 1024 || Nk > 0x7fffffff - 8192 || units > 1L << 22 || units * keep > (1L << 35) / d) return IFA_ERR_UNSUPPORTED;
+    if ((d & 15) || d > 1024 || Nk > 0x7fffffff - 8192 || units >= 1L << 22 || units * keep > (1L << 35) / d) return IFA_ERR_UNSUPPORTED;      // (a launch has less than 2^32 threads: 1024 to a head)
     for (const void *p : {static_cast<const void *>(K_i8), V, static_cast<const void *>(K_out), static_cast<const void *>(V_out)})
         if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
     for (const void *p : {static_cast<const void *>(s_K), static_cast<const void *>(W), static_cast<const void *>(lens), static_cast<const void *>(s_K_out),
