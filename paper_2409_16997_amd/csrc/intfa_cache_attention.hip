@@ -18,6 +18,7 @@
 #include "intfa_internal.h"
 #include "intfa_device.h"
 #include "intfa_cache.h"
+#include "intfa_cache_plan.h"
 
 namespace {
 
@@ -263,7 +264,6 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 // in pairs, the sum in pairs) exp2 alone takes 16 cycles: 1111 vector cycles of the 2060 that 64 keys take a wavefront, 769 of the matrix unit (the chip runs it at 1.8 - 2.0 GHz).
 // So the number that the weights refer to, 2^7 under the maximum when it was taken, only moves when a block exceeds that maximum by 2^8 (a row by itself: what a row gives does not depend on
 // its neighbours), which fp16 weights of up to 2^15 hold, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made.
-constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
 template <int D, bool VI8> struct SmemTile {
     alignas(4096) int8_t k[2][TILE_KEYS * D];
     alignas(4096) int8_t v[2][TILE_KEYS * V_ROW<D, VI8>];
@@ -631,51 +631,8 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(Call c, Parts
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
-// How a call is carried out: in how many parts the shared keys and the own keys of a unit are taken, each part leaving 4 (d + 2) bytes a row.
-struct Plan {
-    int shared, own;                       // parts of the shared keys taken for the whole batch (0: every sequence reads them), and of the own keys
-    long rows_shared, rows_own;            // rows of parts: all units x parts x rows
-    bool join() const { return shared > 0 || own > 1; }
-    long bytes(int d) const { return (rows_shared + rows_own) * (4L * d + 8); }
-};
-constexpr int MOST_PARTS = 64;
-
-long row_tiles(bool few, long rows) { return few ? (rows + 31) / 32 : (rows + TILE_ROWS - 1) / TILE_ROWS; }
-// The kernel for 32 rows, whose wavefronts share the keys out among themselves, or tiles of 128.  Own keys: 32 rows as long as that leaves half of the CUs without one (us, 32 rows / 128, 8 key heads,
-// groups of 4, window 4096: 64 queries 20.8 / 22.6, 256 queries 41.6 / 34.7; 2 x 4 heads of d = 64, 300 queries, window 1000: 9.9 / 12.8).  Shared keys: the tiles read them once for
-// 128 rows of the batch (64 sequences x 4 rows on 8192 keys 43 / 30 in all).
-bool few_rows(bool all, long units, long rows) { return rows <= 32 || (!all && units * ((rows + 31) / 32) <= 128); }
-// Parts where there is less than a workgroup for each of `places`, as many as there are, of at least `least` keys each.  Under 512 keys the second launch that joins them costs more than it
-// gains (one sequence on 261 keys 6.2 us whole, 7.5 in two; 16 x 8 heads on 4096 of up to 16384 keys 39 in two parts each, 44 in four; one x 8 on 4096 12 in 32, 13 in 16).
-int parts_for(long places, long groups, long keys, long least) {
-    long parts = keys < 512 ? 1 : places / groups;
-    if (parts > keys / least) parts = keys / least;
-    return static_cast<int>(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
-}
-
-Plan plan_of(int B, int Hkv, int G, int Nq, int Np, int Nk, int window, int sinks) {
-    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
-    Plan p = {};
-    const long span = static_cast<long>(window) + imin(Nq, TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
-    const bool few = few_rows(false, units, rows);
-    p.own = parts_for(few ? 256 : 512, units * row_tiles(few, rows), keys, few ? 128 : 256);
-    // Few keys: every sequence reads the shared ones, too (2 sequences on 300 + 40 keys 6.2 us, with a launch for the parts 7.4; on 600 + 100 12.1 and 9.1).  So it does with many rows of
-    // its own, unless tiles of the batch's rows on the shared keys are so many fewer that it pays for the parts: 8 x 8 heads, 4 x 512 queries on 2048 + 512 keys 143 us, with parts 184;
-    // 64 x 8 heads, 8 x 10 queries on 4000 + 50 (64 tiles a head for 40: 2400 keys a tile) 106 and 117; 6 x 8 heads, 4 x 40 queries on 32000 + 50 (12 for 8: 16000) 169 and 136.
-    if (Np > 0) {
-        const long all = rows * B, all_tiles = row_tiles(false, all);
-        const bool parts = few ? static_cast<long>(Np) + Nk >= 512 : (B * row_tiles(false, rows) - all_tiles) * Np > 6000 * all_tiles;
-        // (own keys in the same launch: a place on every CU is left to them; 64 sequences x 8 heads on 8192 + 512 keys 28.5 us, with 384 places 34, with 512 38)
-        if (parts) p.shared = parts_for(few ? 256 : 512, Hkv * row_tiles(few_rows(true, Hkv, all), all), Np, 256);
-        p.rows_shared = Hkv * all * p.shared;
-        if (!few && !parts) p.own = parts_for(512, units * row_tiles(false, rows), keys + Np, 256);
-    }
-    p.rows_own = p.join() ? units * rows * p.own : 0;
-    return p;
-}
-
 template <int D, bool VI8>
-int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
+int launch(Call c, const AttentionPlan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv;
     float *const o = static_cast<float *>(workspace);
     float2 *const ml = reinterpret_cast<float2 *>(o + (plan.rows_shared + plan.rows_own) * D);
@@ -684,48 +641,39 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
         hipLaunchKernelGGL((cache_attention_tile_kernel<D, VI8, decltype(walk)::value>), dim3(static_cast<unsigned>(static_cast<long>(n_units) * n * k.splits)), dim3(256), 0, st, k, n_units, n,
                            head_group_for(true, 0, 0));
     };
-    auto few = [&](const Call &k) {
-        const int n = static_cast<int>(row_tiles(true, k.rows));
-        const long grid = (static_cast<long>(units) * k.splits + 7) / 8 * 8 * n;
-        auto launch_few = [&](auto stages, auto nt) {
-            hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(stages)::value, decltype(nt)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * FEW_WAVES), 0, st, k, units, n);
-        };
-        constexpr std::integral_constant<int, 1> one{};
-        constexpr std::integral_constant<int, 2> two{};
-        // with the non-temporal hint where what is read once does not stay in the caches anyway: 32 x 8 heads on 4096 keys 67 us against 76, 64 x 8 on 512 26 / 28; 4 x 8 on 4096 (50 MB) the same
-        const long keys = imin(k.Nk, imin(k.window, k.Nk - k.sinks) + k.sinks);
-        const bool once = n == 1 && units * keys * (D + V_ROW<D, VI8>) > 64L << 20;
-        // One workgroup to a CU copies two tiles ahead; more of them fit with one (64 x 8 heads on 512 keys 26 us, with two 27; 16 x 8 on 4096 in 256 workgroups 41 and 39)
-        if (grid > 256) once ? launch_few(one, std::true_type{}) : launch_few(one, std::false_type{});
-        else once ? launch_few(two, std::true_type{}) : launch_few(two, std::false_type{});
-    };
-    Call shared = {};
+    Call shared = c;                                             // the shared keys for the rows of the whole batch, if they are taken so
     if (plan.shared > 0) {
-        Call k = c;
-        k.rows = c.rows * c.B;
-        k.splits = plan.shared;
-        k.part_o = o, k.part_ml = ml;
+        shared.rows = c.rows * c.B;
+        shared.splits = plan.shared;
+        shared.part_o = o, shared.part_ml = ml;
         c.Kp = nullptr, c.Np = 0;                                // the own keys alone
-        shared = k;
     }
     c.splits = plan.own;
     if (plan.join()) c.part_o = o + plan.rows_shared * D, c.part_ml = ml + plan.rows_shared;
-    const bool own_few = few_rows(false, units, c.rows);
-    if (plan.shared > 0 && own_few) {
-        const bool shared_few = few_rows(true, c.Hkv, shared.rows);
-        const int shared_tiles = static_cast<int>(row_tiles(shared_few, shared.rows)), own_tiles = static_cast<int>(row_tiles(true, c.rows));
-        const long blocks = shared_few ? (static_cast<long>(c.Hkv) * shared.splits + 7) / 8 * 8 * shared_tiles : static_cast<long>(c.Hkv) * shared_tiles * shared.splits;
-        const long grid = blocks + (static_cast<long>(units) * c.splits + 7) / 8 * 8 * own_tiles;
-        auto both = [&](auto tile) {
-            hipLaunchKernelGGL((cache_attention_both_kernel<D, VI8, decltype(tile)::value>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, shared, c, static_cast<int>(blocks), shared_tiles,
-                               units, own_tiles, head_group_for(true, 0, 0));
-        };
-        shared_few ? both(std::false_type{}) : both(std::true_type{});
-    } else if (own_few) few(c);
-    else if (c.Kp) tiles(std::integral_constant<Walk, SHARED_AND_OWN>{}, c, units);
-    else {
-        if (plan.shared > 0) tiles(std::integral_constant<Walk, SHARED>{}, shared, c.Hkv);       // (more rows than few_rows() has)
-        tiles(std::integral_constant<Walk, OWN>{}, c, units);
+    const int own_tiles = static_cast<int>(row_tiles(true, c.rows));
+    const long own_grid = few_grid(units, c.splits, c.rows);
+    auto few = [&](auto ahead, auto once) {
+        hipLaunchKernelGGL((cache_attention_few_kernel<D, VI8, decltype(ahead)::value, decltype(once)::value>), dim3(static_cast<unsigned>(own_grid)), dim3(64 * FEW_WAVES), 0, st, c, units, own_tiles);
+    };
+    auto both = [&](auto tile) {
+        constexpr bool TILE = decltype(tile)::value;
+        const int n = static_cast<int>(row_tiles(!TILE, shared.rows));
+        const long blocks = TILE ? static_cast<long>(c.Hkv) * n * shared.splits : few_grid(c.Hkv, shared.splits, shared.rows);
+        hipLaunchKernelGGL((cache_attention_both_kernel<D, VI8, TILE>), dim3(static_cast<unsigned>(blocks + own_grid)), dim3(256), 0, st, shared, c, static_cast<int>(blocks), n, units, own_tiles,
+                           head_group_for(true, 0, 0));
+    };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    switch (plan.way) {
+    case WAY_FEW:
+        if (plan.ahead == 1) plan.once ? few(one, std::true_type{}) : few(one, std::false_type{});
+        else plan.once ? few(two, std::true_type{}) : few(two, std::false_type{});
+        break;
+    case WAY_BOTH_FEW: both(std::false_type{}); break;
+    case WAY_BOTH_TILE: both(std::true_type{}); break;
+    case WAY_TILE_APART: tiles(std::integral_constant<Walk, SHARED>{}, shared, c.Hkv); [[fallthrough]];
+    case WAY_TILE: tiles(std::integral_constant<Walk, OWN>{}, c, units); break;
+    case WAY_TILE_FRONT: tiles(std::integral_constant<Walk, SHARED_AND_OWN>{}, c, units); break;
     }
     if (plan.join()) {
         const Parts parts = {o, c.part_o, ml, c.part_ml, plan.shared, plan.own};
@@ -741,7 +689,7 @@ int launch(Call c, const Plan &plan, void *workspace, hipStream_t st) {
 }
 
 // The argument rules that both entry points share
-int refuse(const Call &c, int d, const void *workspace, long workspace_bytes, const Plan &plan) {
+int refuse(const Call &c, int d, const void *workspace, long workspace_bytes, const AttentionPlan &plan) {
     const bool prefix = c.Np > 0;
     if (!c.Q || !c.K || !c.V || !c.sQ || !c.sK || !c.O || (prefix && (!c.Kp || !c.Vp || !c.sKp || !c.sVp != !c.sV))) return IFA_ERR_NULL;
     if (c.o_dtype < IFA_F32 || c.o_dtype > IFA_BF16) return IFA_ERR_DTYPE;
@@ -769,10 +717,10 @@ int refuse_sizes(int B, int H, int Hkv, int Nq, int Np, int Nk, int d) {
 }
 
 int entry(const Call &c, int d, void *workspace, long workspace_bytes, void *hip_stream) {
-    const Plan plan = plan_of(c.B, c.Hkv, c.G, c.Nq, c.Np, c.Nk, c.window, c.sinks);
+    const bool i8 = c.sV != nullptr;
+    const AttentionPlan plan = attention_plan(c.B, c.Hkv, c.G, c.Nq, c.Np, c.Nk, c.window, c.sinks, i8 ? 2 * d : 3 * d);
     if (const int rc = refuse(c, d, workspace, workspace_bytes, plan)) return rc;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const bool i8 = c.sV != nullptr;
     if (d == 128) return i8 ? launch<128, true>(c, plan, workspace, st) : launch<128, false>(c, plan, workspace, st);
     return i8 ? launch<64, true>(c, plan, workspace, st) : launch<64, false>(c, plan, workspace, st);
 }
@@ -781,7 +729,7 @@ int entry(const Call &c, int d, void *workspace, long workspace_bytes, void *hip
 
 extern "C" long ifa_window_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks) {
     if (refuse_sizes(B, H, Hkv, Nq, 0, Nk, d) || window <= 0 || sinks < 0) return -1;
-    return plan_of(B, Hkv, H / Hkv, Nq, 0, Nk, imin(window, Nk), imin(sinks, Nk)).bytes(d);
+    return attention_plan(B, Hkv, H / Hkv, Nq, 0, Nk, imin(window, Nk), imin(sinks, Nk), d).bytes(d);
 }
 
 extern "C" int int_flash_attn_fwd_window(const signed char *Q_i8, const signed char *K_i8, const void *V, const float *s_Q, const float *s_K,
@@ -798,7 +746,7 @@ extern "C" int int_flash_attn_fwd_window(const signed char *Q_i8, const signed c
 
 extern "C" long ifa_prefix_workspace_bytes(int B, int H, int Hkv, int Nq, int Np, int Nk, int d) {
     if (refuse_sizes(B, H, Hkv, Nq, Np, Nk, d) || Np <= 0) return -1;
-    return plan_of(B, Hkv, H / Hkv, Nq, Np, Nk, Nk, 0).bytes(d);
+    return attention_plan(B, Hkv, H / Hkv, Nq, Np, Nk, Nk, 0, d).bytes(d);
 }
 
 extern "C" int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8, const void *Vp, const signed char *K_i8, const void *V,

@@ -12,6 +12,7 @@
 #include "intfa_internal.h"
 #include "intfa_device.h"
 #include "intfa_cache.h"
+#include "intfa_cache_plan.h"
 
 namespace {
 
@@ -156,7 +157,6 @@ __global__ __launch_bounds__(64 * KW_WAVES) void key_weights_rows_kernel(Weights
 // ---- the same for tiles of 128 rows, which share the keys, 64 at a time, through LDS ------------------------------------------------
 // A score costs the vector unit a subtraction, s_K, half a maximum, s_Q and m, exp2 (16 cycles) and an addition, four times the 8 cycles of its products.  The maximum that
 // a sum refers to moves only when a block exceeds it by 2^8, a row by itself.
-constexpr int TILE_ROWS = 128, TILE_KEYS = 64;
 template <int D> struct SmemRowTile {
     alignas(4096) int8_t k[2][TILE_KEYS * D];
     alignas(256) float sk[2][TILE_KEYS];
@@ -280,7 +280,6 @@ __global__ __launch_bounds__(256) void key_weights_join_kernel(WeightsCall c, lo
 }
 
 // ---- second pass, from stored scores: four keys to a thread ------------------------------------------------------------------------------
-constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128) and the products
 __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, int units, int blocks, bool whole) {
     __shared__ float2 st[STORED_ROWS];
     const int unit = blockIdx.x / blocks, j = (blockIdx.x % blocks * 256 + threadIdx.x) * 4, rows = c.G * c.Nq;
@@ -333,7 +332,6 @@ __global__ __launch_bounds__(256) void key_weights_stored_kernel(WeightsCall c, 
 // The rows go by in tiles of 64 through LDS, shared by the four wavefronts of 64 keys (two operands of K in registers, so that what is read of the rows counts
 // twice); a slice of them per workgroup.  They are packed like everywhere, row (i, g) with g fastest: a row is a copy from a place of its own, and a few queries of many heads fill a tile.  The vector unit's part of a score: s_Q s_K, the subtraction of the start value, their product less the row's maximum + log2(sum), exp2 and the
 // addition.  (Maximum and log2 in one number: it rounds by 2^-24 of itself, as scores do, and the rows' errors do not add up.)
-constexpr int KW_ROWS = 64, KW_KEYS = 256;
 template <int D> struct SmemKeys {
     alignas(4096) int8_t q[2][KW_ROWS * D];
     alignas(256) float2 row[2][KW_ROWS];
@@ -459,52 +457,13 @@ __global__ __launch_bounds__(256) void key_weights_add_kernel(WeightsCall c, lon
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
-struct Plan {
-    int parts, slices;
-    bool stored, few;
-    long stats, rows, scores, sums;        // bytes
-    long stride;                           // of a row of scores
-    long bytes() const { return stats + rows + scores + sums; }
-};
-long up(long n) { return (n + 255) / 256 * 256; }
-Plan plan_of(int B, int Hkv, int G, int Nq, int Nk) {
-    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
-    Plan p = {};
-    p.stored = rows <= STORED_ROWS;
-    // The kernel for 32 rows up to 48 of its tiles, then tiles of 128 (8 key heads on 8192 keys, 32 rows / 128, us: 128 rows 19.5 / 20.6, 256 rows 26.0 / 24.2, 512 rows 34.8 / 30.9).
-    const long few_tiles = units * ((rows + 31) / 32), tiles = units * ((rows + TILE_ROWS - 1) / TILE_ROWS);
-    p.few = rows <= 32 || few_tiles <= 48;
-    // As many parts as there are places for 4 workgroups a CU (16 x 8 heads on up to 16384 keys 41.3 us, for 2 46.2; 32 x 800 rows on 8192 117.9 and 125.2), of at least 512 keys each, or 256 where few
-    // rows have to be joined (8 heads, 24 rows on 4096 keys 10.9 and 13.2; 64 rows on 8192 16.7 and 15.2).
-    long parts = 1024 / (p.few ? few_tiles : tiles);
-    const long least = rows <= 32 ? 256 : 512;
-    if (parts > Nk / least) parts = Nk / least;
-    p.parts = static_cast<int>(parts < 1 ? 1 : parts > 64 ? 64 : parts);
-    p.stats = p.parts > 1 || p.stored ? up(units * rows * p.parts * 8) : 0;
-    p.stride = (Nk + 31L) / 32 * 32;
-    if (p.stored) {
-        p.scores = up(units * rows * p.stride * 4);
-        p.slices = 1;
-    } else {
-        p.rows = up(units * rows * 8);
-        const long groups = units * ((Nk + KW_KEYS - 1) / KW_KEYS), most = (rows + KW_ROWS - 1) / KW_ROWS;
-        long slices = (1024 + groups - 1) / groups;              // four workgroups a CU here, too
-        if (slices > most) slices = most;
-        p.slices = static_cast<int>(slices < 1 ? 1 : slices > 64 ? 64 : slices);
-        p.sums = p.slices > 1 ? up(units * Nk * 4L * p.slices) : 0;
-    }
-    return p;
-}
-
-template <int D> int launch(WeightsCall c, const Plan &plan, hipStream_t st) {
+template <int D> int launch(WeightsCall c, const WeightsPlan &plan, hipStream_t st) {
     const int units = c.B * c.Hkv, unit_rows = c.G * c.Nq;
     const long rows = static_cast<long>(units) * unit_rows;
     if (plan.few) {
         const int row_tiles = (unit_rows + 31) / 32;
         const long grid = (static_cast<long>(units) * c.parts + 7) / 8 * 8 * row_tiles;
-        // with the non-temporal hint where K is read once and does not stay in the caches anyway (16 x 8 heads on up to 16384 keys 45.0 us against 47.4)
-        const bool once = plan.stored && static_cast<long>(units) * c.Nk * D > 64L << 20;
-        if (once) hipLaunchKernelGGL((key_weights_rows_kernel<D, true>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
+        if (plan.once) hipLaunchKernelGGL((key_weights_rows_kernel<D, true>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
         else hipLaunchKernelGGL((key_weights_rows_kernel<D, false>), dim3(static_cast<unsigned>(grid)), dim3(64 * KW_WAVES), 0, st, c, units, row_tiles);
     } else {
         const int row_tiles = (unit_rows + TILE_ROWS - 1) / TILE_ROWS;
@@ -548,7 +507,7 @@ struct EvictCall {
     float *sK_out, *W_out;
     int *index, *lens_out;
 };
-constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64, SEL_ROUND = 4 * SEL_THREADS, BINS = 2048;
+constexpr int SEL_WAVES = SEL_THREADS / 64, BINS = 2048;
 
 // Larger weight, larger number; -0 is 0, a NaN is below everything.  Between 1 and 0xff800000 (+inf): 0 is left for places without a key, the largest number for keys that stay anyway.
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -728,7 +687,7 @@ bool overlap(const void *a, long na, const void *b, long nb) {
 
 extern "C" long ifa_key_weights_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d) {
     if (refuse_sizes(B, H, Hkv, Nq, Nk, d)) return -1;
-    return plan_of(B, Hkv, H / Hkv, Nq, Nk).bytes();
+    return weights_plan(B, Hkv, H / Hkv, Nq, Nk, d).bytes();
 }
 
 extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, const float *s_Q, const float *s_K, const int *lens, const float *W,
@@ -740,7 +699,7 @@ extern "C" int key_weights(const signed char *Q_i8, const signed char *K_i8, con
         if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
     const long n = static_cast<long>(B) * Hkv * Nk * 4;
     if (W && W != W_out && overlap(W, n, W_out, n)) return IFA_ERR_UNSUPPORTED;      // (in place or apart, not shifted)
-    const Plan plan = plan_of(B, Hkv, H / Hkv, Nq, Nk);
+    const WeightsPlan plan = weights_plan(B, Hkv, H / Hkv, Nq, Nk, d);
     if (workspace_bytes < plan.bytes()) return IFA_ERR_WORKSPACE;
     WeightsCall c = {};
     c.Q = Q_i8, c.K = K_i8, c.sQ = s_Q, c.sK = s_K, c.W = W, c.lens = lens, c.out = W_out;
@@ -783,10 +742,12 @@ extern "C" int evict_keys(const signed char *K_i8, const float *s_K, const void 
                    K_out, static_cast<int8_t *>(V_out), s_K_out, W_out, index, lens_out};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto select = [&](auto rounds) { hipLaunchKernelGGL((evict_select_kernel<decltype(rounds)::value>), dim3(static_cast<unsigned>(units)), dim3(SEL_THREADS), 0, st, c); };
-    if (Nk <= 1 * SEL_ROUND) select(std::integral_constant<int, 1>{});
-    else if (Nk <= 4 * SEL_ROUND) select(std::integral_constant<int, 4>{});
-    else if (Nk <= 8 * SEL_ROUND) select(std::integral_constant<int, 8>{});
-    else select(std::integral_constant<int, 0>{});
+    switch (evict_rounds(Nk)) {
+    case 1: select(std::integral_constant<int, 1>{}); break;
+    case 4: select(std::integral_constant<int, 4>{}); break;
+    case 8: select(std::integral_constant<int, 8>{}); break;
+    default: select(std::integral_constant<int, 0>{});
+    }
     const int lanes = d / 16, per_block = 256 / lanes * MOVE_AT_ONCE, blocks = (keep + per_block - 1) / per_block;
     auto move = [&](auto vb) { hipLaunchKernelGGL((evict_move_kernel<decltype(vb)::value>), dim3(static_cast<unsigned>(units) * blocks), dim3(256), 0, st, c, lanes, blocks); };
     if (v_bytes == 1) move(std::integral_constant<int, 1>{});
