@@ -302,7 +302,8 @@ int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8,
 /*
  * The softmax weight that each own key draws, added up over the queries and over the heads of its group -- what an eviction goes by:
  *   W_out[b, hk, j] = W[b, hk, j] + sum over i and over the heads h of group hk of exp(S_ij) / sum_j' exp(S_ij'),   j' over the keys that query i sees (j' <= p)
- * in fp32 (the weights are not rounded to fp16).  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W
+ * in fp32 (the weights are not rounded to fp16).  That is causal attention over the own keys, without a window or shared keys: after a call with either, these are not the weights
+ * which that call gave.  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W
  * (and must not overlap it otherwise).
  *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30, G Nq d <= 0x7ff00000.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
  * row and key where a key head has up to 16 query rows, else 4 a key and slice of the rows.
@@ -317,6 +318,7 @@ int key_weights(const signed char *Q_i8, const signed char *K_i8, const float *s
  * W (of equal ones the first; a NaN is below everything) stay, in their order; with L_b <= keep all do.
  *   K_out [B, Hkv, keep, d], s_K_out, W_out [B, Hkv, keep], V_out [B, Hkv, keep, d] (V of v_bytes = 1 or 2 bytes an element): the rows that stay, then zeros
  *   index [B, Hkv, keep] int32: which key each was, then -1;  lens_out [B] int32: min(L_b, keep)
+ * The outputs hold `keep` keys a head and no room behind them: a sequence that goes on is copied into larger buffers, its next key at lens_out[b].
  * s_V of an INT8 V stays as it is.  1 <= keep <= Nk, sinks + recent <= keep; d a multiple of 16 up to 1024, Nk < 2^31 - 8192, B Hkv < 2^22, B Hkv keep d <= 2^35.  Nothing is evicted in place: outputs that overlap an input or each
  * other are refused (IFA_ERR_UNSUPPORTED).  Two launches, no workspace.
  */

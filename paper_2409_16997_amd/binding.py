@@ -491,7 +491,8 @@ def key_weights_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: i
 def key_weights(Q_i8, K_i8, s_Q, s_K, W=None, lens=None, out=None, workspace=None):
     """The softmax weight that each key of a cache draws, summed over the queries and the heads of its group, added to W [B, Hkv, Nk]
     (None: zeros): fp32 [B, Hkv, Nk], into `out` if given (which may be W).  int8 Q [B, H, Nq, d], K [B, Hkv, Nk, d] with token-level scales; the queries
-    are the last Nq positions of the lens[b] keys of their sequence and see the keys up to their own."""
+    are the last Nq positions of the lens[b] keys of their sequence and see the keys up to their own: the weights of causal attention, without a
+    window or a prefix."""
     r = (_native or _load_native()).weights(Q_i8, K_i8, s_Q, s_K, W, lens, out, workspace)
     if r is not None:
         return out if out is not None else r
@@ -513,6 +514,7 @@ def evict_keys(K_i8, s_K, V, W, keep, recent=0, sinks=0, lens=None, out=None):
     """The cache K_i8, V [B, Hkv, Nk, d] (V fp16 or int8), s_K, W [B, Hkv, Nk] cut down to `keep` keys a head: the first `sinks` of the lens[b]
     keys, the last `recent` and those of the largest W between them (of equal ones the first), in their order.  Returns (K_i8, s_K, V, W
     [B, Hkv, keep, ...], index [B, Hkv, keep] int32, lens [B] int32); past min(lens[b], keep) keys index is -1 and the rest zero.
+    They hold `keep` keys and no more: pad them (torch.nn.functional.pad) for a sequence that goes on, its next key at lens[b].
     out: optional tuple of those six tensors to write into, which overlap neither the inputs nor each other."""
     if out is None:
         r = (_native or _load_native()).evict(K_i8, s_K, V, W, keep, recent, sinks, lens)
