@@ -94,9 +94,12 @@ static inline WeightsPlan weights_plan(int B, int Hkv, int G, int Nq, int Nk, in
     auto up = [](long n) { return (n + 255) / 256 * 256; };
     WeightsPlan p = {};
     p.stored = rows <= STORED_ROWS;
-    // The kernel for 32 rows up to 48 of its tiles, then tiles of 128 (8 key heads on 8192 keys, 32 rows / 128, us: 128 rows 19.5 / 20.6, 256 rows 26.0 / 24.2, 512 rows 34.8 / 30.9).
+    // The kernel for 32 rows for up to 512 of its tiles of up to 400 K keys in all, then tiles of 128, which read K a quarter as often and take longer to start and to end.  32 rows / 128, us, in all, d = 128 unless
+    // stated (key heads x rows x keys): 8 x 400 x 1024 16.0 / 20.3, 32 x 128 x 1024 16.6 / 19.0, 8 x 200 x 4096 19.6 / 21.0, 128 x 64 x 1024 19.4 / 20.3, 128 x 128 x 512 16.8 / 19.4, 12 x 100 x 8192 25.4 / 26.6;
+    // 8 x 200 x 8192 26.8 / 25.2, 16 x 256 x 4096 26.6 / 25.3, 64 x 200 x 1024 26.4 / 25.8, 128 x 128 x 2048 34.9 / 30.7, 16 x 100 x 16384 36.5 / 32.2, 256 x 200 x 256 24.1 / 21.1; d = 64, 32 x 512 x 512 14.2 / 17.1,
+    // 16 x 512 x 2048 21.0 / 21.9, 8 x 384 x 16384 36.3 / 33.2.  Within .4 % of the faster one over 414 calls of 64 to 16384 keys, 9 % off at worst.
     const long few_tiles = units * ((rows + 31) / 32), tiles = units * ((rows + TILE_ROWS - 1) / TILE_ROWS);
-    p.few = rows <= 32 || few_tiles <= 48;
+    p.few = rows <= 32 || (few_tiles <= 512 && few_tiles * Nk <= 400 << 10);
     // with the non-temporal hint where K is read once and does not stay in the caches anyway (16 x 8 heads on up to 16384 keys 45.0 us against 47.4)
     p.once = p.few && p.stored && units * Nk * d > 64L << 20;
     // As many parts as there are places for 4 workgroups a CU (16 x 8 heads on up to 16384 keys 41.3 us, for 2 46.2; 32 x 800 rows on 8192 117.9 and 125.2), of at least 512 keys each, or 256 where few

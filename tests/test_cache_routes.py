@@ -1,8 +1,11 @@
 """Which kernels the GPU tests of the calls on a quantized cache reach, by the library's own rules."""
+import pytest
+
 import cache_routes
 import test_gpu_cache_attention as attention_tests
 import test_gpu_cache_far_weights as far_tests
 import test_gpu_cache_scales as scale_tests
+import test_gpu_cache_weight_tiles as tile_tests
 import test_gpu_cache_weights as weights_tests
 
 
@@ -39,11 +42,21 @@ def test_the_padding_and_hidden_keys_reach_both_kernels():
 
 
 def test_the_key_weights_reach_every_kernel():
-    plans = [weights(c) for c in weights_tests.WEIGHTS]
+    plans = [weights(c) for c in weights_tests.WEIGHTS + tile_tests.WEIGHTS]
     assert {(p["few"], p["stored"], p["parts"] > 1) for p in plans} == {(True, True, False), (True, True, True), (True, False, False), (True, False, True), (False, False, False), (False, False, True)}
     assert {p["slices"] > 1 for p in plans if not p["stored"]} == {False, True}
-    of_padding = [cache_routes.weights(1, Hkv, G, Nq, 260, 64) for Hkv, G, Nq in ((1, 1, 9), (1, 2, 30), (16, 2, 200))]
+    assert not any(weights(c)["few"] for c in tile_tests.WEIGHTS)
+    of_padding = [cache_routes.weights(1, Hkv, G, Nq, 260, 64) for Hkv, G, Nq in ((1, 1, 9), (1, 2, 30))] + [cache_routes.weights(*tile_tests.PADDED)]
     assert [(p["few"], p["stored"]) for p in of_padding] == [(True, True), (True, False), (False, False)]
+
+
+# First passes on the faster side of the line between 32 rows and tiles of 128, where the other one takes at least 5 % longer
+@pytest.mark.parametrize("heads,rows,Nk,d,few", [
+    (8, 400, 1024, 128, True), (32, 128, 1024, 128, True), (16, 512, 1024, 128, True), (128, 64, 512, 128, True), (8, 200, 4096, 128, True), (128, 128, 256, 64, True), (4, 100, 8192, 64, True),
+    (8, 200, 8192, 128, False), (16, 256, 4096, 128, False), (128, 128, 2048, 128, False), (16, 100, 16384, 128, False), (256, 200, 256, 128, False), (8, 384, 16384, 64, False),
+    (32, 512, 2048, 64, False), (256, 512, 2048, 64, False)])
+def test_first_passes_on_the_faster_side(heads, rows, Nk, d, few):
+    assert cache_routes.weights(1, heads, 1, rows, Nk, d)["few"] == few
 
 
 def test_the_evictions_reach_every_form():

@@ -151,8 +151,8 @@ def test_prefix_with_queries_of_no_scale(ifa, name):
 WEIGHTS = {
     "stored scores": (2, 2, 4, 2, 700, 64, (700, 1)),
     "32 rows": (1, 2, 3, 40, 300, 128, (299,)),
-    "tiles": (1, 20, 3, 80, 200, 64, (190,)),
-    "tiles, in parts": (2, 8, 2, 150, 1200, 128, (1200, 700)),
+    "tiles": (3, 88, 2, 32, 70, 64, (70, 3, 40)),
+    "tiles, in parts": (2, 24, 2, 128, 1100, 128, (1100, 700)),
 }
 
 
