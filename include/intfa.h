@@ -306,7 +306,7 @@ int int_flash_attn_fwd_prefix(const signed char *Q_i8, const signed char *Kp_i8,
  * which that call gave.  W null: zeros.  Keys that nobody sees, those at or beyond L_b among them, keep W.  W_out may be W
  * (and must not overlap it otherwise).
  *   Equal calls give equal results, bit for bit (no floating point atomics).  B Hkv Nk <= 2^30, G Nq d <= 0x7ff00000.  The workspace is always needed: 8 bytes a query row and part of the keys, and 4 a query
- * row and key where a key head has up to 16 query rows, else 4 a key and slice of the rows.
+ * row and key where a key head has up to 16 (d = 64: 12) query rows, else 4 a key and slice of the rows.
  */
 long ifa_key_weights_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d);
 

@@ -79,7 +79,11 @@ static inline AttentionPlan attention_plan(int B, int Hkv, int G, int Nq, int Np
 }
 
 // ---- key weights ---------------------------------------------------------------------------------------------------
-constexpr int STORED_ROWS = 16;                                  // most rows whose scores are stored: 8 bytes a row and key out and in, 128 for K again (d = 128) and the products
+// Most rows whose scores are stored, 8 bytes a row and key out and in, rather than K read and multiplied again, d bytes a key.  Stored / again, us, d = 128: 16 sequences x 8 heads x 16384 keys, 8 rows
+// 77 / 120, 16 rows 101 / 120; 1 x 8 x 4096, 16 rows 10.3 / 11.0; 32 x 8 x 2000 30.4 / 34.6.  d = 64: 16 x 8 x 16384, 9 rows 63 / 71, 12 rows 73 / 72, 16 rows 86 / 72; 4 x 8 x 8192 17.4 / 18.5, 19.3 / 18.6, 21.3 / 18.7;
+// 16 x 8 x 4096 19.7 / 24.1, 21.2 / 23.9, 23.4 / 24.2.
+constexpr int STORED_ROWS = 16;
+static inline int stored_rows(int d) { return d == 64 ? 12 : STORED_ROWS; }
 constexpr int KW_ROWS = 64, KW_KEYS = 256;                       // of a workgroup of the second pass that computes them again
 
 struct WeightsPlan {
@@ -93,7 +97,7 @@ static inline WeightsPlan weights_plan(int B, int Hkv, int G, int Nq, int Nk, in
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     auto up = [](long n) { return (n + 255) / 256 * 256; };
     WeightsPlan p = {};
-    p.stored = rows <= STORED_ROWS;
+    p.stored = rows <= stored_rows(d);
     // The kernel for 32 rows for up to 512 of its tiles of up to 400 K keys in all, then tiles of 128, which read K a quarter as often and take longer to start and to end.  32 rows / 128, us, in all, d = 128 unless
     // stated (key heads x rows x keys): 8 x 400 x 1024 16.0 / 20.3, 32 x 128 x 1024 16.6 / 19.0, 8 x 200 x 4096 19.6 / 21.0, 128 x 64 x 1024 19.4 / 20.3, 128 x 128 x 512 16.8 / 19.4, 12 x 100 x 8192 25.4 / 26.6;
     // 8 x 200 x 8192 26.8 / 25.2, 16 x 256 x 4096 26.6 / 25.3, 64 x 200 x 1024 26.4 / 25.8, 128 x 128 x 2048 34.9 / 30.7, 16 x 100 x 16384 36.5 / 32.2, 256 x 200 x 256 24.1 / 21.1; d = 64, 32 x 512 x 512 14.2 / 17.1,

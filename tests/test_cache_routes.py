@@ -50,6 +50,11 @@ def test_the_key_weights_reach_every_kernel():
     assert [(p["few"], p["stored"]) for p in of_padding] == [(True, True), (True, False), (False, False)]
 
 
+def test_where_scores_are_stored():
+    for d, most in ((64, 12), (128, 16)):
+        assert [cache_routes.weights(4, 8, rows, 1, 8192, d)["stored"] for rows in (1, most, most + 1)] == [True, True, False]
+
+
 # First passes on the faster side of the line between 32 rows and tiles of 128, where the other one takes at least 5 % longer
 @pytest.mark.parametrize("heads,rows,Nk,d,few", [
     (8, 400, 1024, 128, True), (32, 128, 1024, 128, True), (16, 512, 1024, 128, True), (128, 64, 512, 128, True), (8, 200, 4096, 128, True), (128, 128, 256, 64, True), (4, 100, 8192, 64, True),

@@ -69,6 +69,19 @@ def test_window(ifa, name, d, v):
         assert bool((off <= tol).all()), f"sequence {b}, head {hk}: off by up to {(off / tol.clamp_min(1e-300)).max().item():.3f} of the tolerance"
 
 
+@pytest.mark.parametrize("d,rows,stored", [(64, 12, True), (64, 13, False), (128, 16, True), (128, 17, False)])
+def test_key_weights_on_both_sides_of_the_stored_scores(ifa, d, rows, stored):
+    assert cache_routes.weights(2, 2, rows, 1, 700, d)["stored"] == stored
+    for G, Nq in ((rows, 1), (1, rows)):
+        lens = (700, rows - 1)
+        s = ref.problem(55, 2, 2, G, Nq, 700, d)
+        want, tol = ref.key_weights(s, lens)
+        t = ref.on_gpu(s)
+        got = ifa.key_weights(t["q8"], t["k8"], t["sq"], t["sk"], lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+        off = (got.cpu().double() - want).abs()
+        assert bool((off <= tol).all()), f"off by up to {(off / tol).max().item():.3f} of the tolerance"
+
+
 @pytest.mark.parametrize("d,Nk", [(128, 8300), (64, 16700)])
 def test_key_weights_past_the_caches(ifa, d, Nk):
     B, Hkv, G, lens = 2, 32, 4, (Nk, Nk // 3)
