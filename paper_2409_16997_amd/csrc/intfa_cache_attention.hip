@@ -40,14 +40,14 @@ __device__ __forceinline__ long row_of(const Call &c, bool all, int unit, int ro
 
 // INT8 V: o is in units of one scale.  Own V whose scale is 0, or vanishes beside the shared one's so that the ratio of the two could leave the range of fp32 (|o| < 2^46), is
 // taken as the zeros it is then: its keys have their weights, its values are not read and o stays in the shared keys' units.
-__device__ __forceinline__ bool counts_as_zero(float own, float shared) { return fabsf(own) <= fabsf(shared) * 0x1p-64f; }
+[[maybe_unused]] __device__ __forceinline__ bool counts_as_zero(float own, float shared) { return fabsf(own) <= fabsf(shared) * 0x1p-64f; }
 
 // ---- 32 rows against many keys: every wavefront for itself -------------------------------------------------------
 // The four wavefronts of a workgroup hold the same 32 rows and take every fourth tile of 32 keys each, with an online softmax of their own; they meet
 // once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
 // asks for the one that goes into its place before it computes.  What bounds it is memory: 32 sequences x 8 heads on 4096 keys of d = 128 in 66.5 us, 6.1 TB/s.
 constexpr int FEW_WAVES = 4;
-constexpr float FEW_BELOW = 15.0f;                               // the largest weight is 2^15
+[[maybe_unused]] constexpr float FEW_BELOW = 15.0f;                               // the largest weight is 2^15
 template <int D, bool VI8, int ST> struct SmemFew {
     static constexpr int KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
     union {
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cache_attention_few_kernel(Cal
 // ---- many rows: tiles of 128 ----------------------------------------------------------------------------------------
 // Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered).  What bounds it is the vector unit: 32 keys of 32 rows are 12 matrix
 // instructions (384 cycles at d = 128), and of the vector instructions on each of their scores (subtract the start value, s_K, the maximum, s_Q and m, exp2, the conversion
-// in pairs, the sum in pairs) exp2 alone takes 16 cycles: 1111 vector cycles of the 2060 that 64 keys take a wavefront, 769 of the matrix unit (the chip runs it at 1.8 - 2.0 GHz).
+// in pairs, the sum in pairs) exp2 alone takes 16 cycles: 1116 vector cycles of the 2004 that 64 keys take a wavefront, 768 of the matrix unit (the chip runs it at 1.8 - 2.0 GHz).
 // So the number that the weights refer to, 2^7 under the maximum when it was taken, only moves when a block exceeds that maximum by 2^8 (a row by itself: what a row gives does not depend on
 // its neighbours), which fp16 weights of up to 2^15 hold, and only then are o and l rescaled: 64 multiplications a block that are hardly ever made.
 template <int D, bool VI8> struct SmemTile {
