@@ -47,7 +47,7 @@ __device__ __forceinline__ long row_of(const Call &c, bool all, int unit, int ro
 // once, at the end.  So the loop has no barrier: a wavefront copies its tile into LDS, ST tiles ahead, takes the operands of a tile to registers and
 // asks for the one that goes into its place before it computes.  What bounds it is memory: 32 sequences x 8 heads on 4096 keys of d = 128 in 66.5 us, 6.1 TB/s.
 constexpr int FEW_WAVES = 4;
-[[maybe_unused]] constexpr float FEW_BELOW = 15.0f;                               // the largest weight is 2^15
+[[maybe_unused]] constexpr float FEW_BELOW = 15.0f;              // the largest weight is 2^15
 template <int D, bool VI8, int ST> struct SmemFew {
     static constexpr int KB = 32 * D, VB = 32 * V_ROW<D, VI8>;
     union {
