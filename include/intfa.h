@@ -326,6 +326,42 @@ int evict_keys(const signed char *K_i8, const float *s_K, const void *V, int v_b
                int B, int Hkv, int Nk, int d, int keep, int recent, int sinks,
                signed char *K_out, float *s_K_out, void *V_out, float *W_out, int *index, int *lens_out, void *hip_stream);
 
+/*
+ * ---- Writing the cache, and a cache in 4 bits -----------------------------------------------------------------------
+ * How K and V are held:
+ *   IFA_CACHE_I8_F16  K int8 [B, Hkv, Nk, d] with s_K [B, Hkv, Nk]; V fp16 [B, Hkv, Nk, d], no s_V
+ *   IFA_CACHE_I8      V int8, too, with s_V [B, Hkv], which the program has from a calibration.  (These two: the cache of the calls above.)
+ *   IFA_CACHE_I4      K and V [B, Hkv, Nk, d / 2] bytes, s_K and s_V [B, Hkv, Nk].  Byte j of a row holds channel j in its low four bits and channel j + d / 2 in the
+ *                     high ones, each as code + 8.  The quantizers write codes -7 .. 7; a cache from elsewhere may hold -8, too.
+ * lens, and which slots tokens have, as above: the Nn tokens (queries) of sequence b are its LAST positions, token i stands at p = L_b - Nn + i, with lens[b] the length
+ * that includes them, so that one lens serves the call that writes a step's keys and the one that attends to them.
+ */
+typedef enum { IFA_CACHE_I8_F16 = 0, IFA_CACHE_I8 = 1, IFA_CACHE_I4 = 2 } ifa_cache_held;
+
+/*
+ * New tokens into the cache, K and V quantized on the way, in one launch.
+ *   K, V   activations of x_dtype, element (b, h, i, c) of K at K[b K_stride_b + h K_stride_h + i K_stride_n + c] (in elements; V likewise): [B, Hkv, Nn, d], or [B, Nn, Hkv, d] as a
+ *          projection leaves them, or a part of a wider tensor.  Rows start at multiples of 16 bytes.  A stride of 0 (one row for many tokens or heads) is fine.
+ *   K      in 8 bits by the rule of quantize_tokenwise, in 4 bits by the same with 7 in the place of 127: q = rint(x * (7 / a)), s = a / 7, a = max|x| of the row; a row with a < 2^-118 counts as
+ *          zeros (scale 1, codes 0).  hadamard non-zero: of the row rotated as in quantize_tokenwise_hadamard; a query for it is quantized so, too.
+ *   V      rounded to fp16; or q = clamp(rint(x * (1 / s_V)), -127, 127) by the given scale (0: codes 0); or in 4 bits as K (never rotated).
+ *   s_V    null; or [B, Hkv], read; or [B, Hkv, Nk], written.
+ * Tokens at p < 0 (padding in front) are not written, nothing else of the cache is changed.  fp32 with round-half-to-even, bit-exact against that definition.  NaN/Inf are outside the contract.
+ * Supported: d in {64, 128}; B Hkv Nn <= 2^29.  The cache's arrays overlap neither the tokens, nor lens, nor each other (else IFA_ERR_UNSUPPORTED).
+ */
+int append_keys(const void *K, const void *V, int x_dtype, long K_stride_b, long K_stride_h, long K_stride_n, long V_stride_b, long V_stride_h, long V_stride_n,
+                const int *lens, int B, int Hkv, int Nn, int Nk, int d, int held, int hadamard, void *K_c, float *s_K, void *V_c, float *s_V, void *hip_stream);
+
+/*
+ * The cache back as values, K and V [B, Hkv, count, d] of x_dtype: code times scale (fp32, rounded once), and then to x_dtype.
+ *   first      row i is the key at first + i (0 <= first <= Nk), or with first = -1 the one at L_b - count + i: where append_keys puts `count` tokens.  Rows that lie in front of key 0 or at or
+ *              beyond L_b are zeros.
+ *   hadamard   non-zero: K is rotated back (H_d x / d, fp32 butterflies)
+ * Supported: d in {64, 128}; B Hkv count <= 2^29.  K and V overlap neither the cache, nor lens, nor each other.
+ */
+int read_keys(const void *K_c, const float *s_K, const void *V_c, const float *s_V, const int *lens, int B, int Hkv, int Nk, int d, int held, int hadamard,
+              long first, int count, void *K, void *V, int x_dtype, void *hip_stream);
+
 /* Key-block size of the half-INT8 kernel for (d, causal); 0 if that pair is unsupported. */
 int ifa_block_cols_half(int d, int causal);
 

@@ -44,6 +44,8 @@ SIGNATURES = {
     "ifa_key_weights_workspace_bytes": (_l, [_i] * 6),
     "key_weights": (_i, [_vp] * 6 + [_i] * 6 + [_vp, _vp, _l, _vp]),
     "evict_keys": (_i, [_vp] * 3 + [_i] + [_vp] * 2 + [_i] * 7 + [_vp] * 7),
+    "append_keys": (_i, [_vp] * 2 + [_i] + [_l] * 6 + [_vp] + [_i] * 7 + [_vp] * 5),
+    "read_keys": (_i, [_vp] * 5 + [_i] * 6 + [_l, _i] + [_vp] * 2 + [_i, _vp]),
     "ifa_block_cols_half": (_i, [_i, _i]),
     "ifa_debug_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
@@ -541,6 +543,80 @@ def evict_keys(K_i8, s_K, V, W, keep, recent=0, sinks=0, lens=None, out=None):
     to = [_operand(x, f"out[{i}]", (t,), s, dev) for i, (x, t, s) in enumerate(zip(out, (torch.int8, torch.float32, V.dtype, torch.float32, torch.int32, torch.int32),
                                                                                   (rows + (d,), rows, rows + (d,), rows, rows, (B,))))]
     _check(lib().evict_keys(at[0], at[1], at[2], V.element_size(), at[3], ln, B, Hkv, Nk, d, keep, recent, sinks, *to, _stream()), "evict_keys")
+    return tuple(out)
+
+
+# ---- writing the cache, and a cache in 4 bits
+
+IFA_CACHE_I8_F16, IFA_CACHE_I8, IFA_CACHE_I4 = 0, 1, 2
+
+
+def _held(K_c, s_K, V_c, s_V, lens, dev):
+    """(how the cache is held, its sizes B, Hkv, Nk, d, addresses of K, s_K, V, s_V and lens)."""
+    import torch
+    if getattr(K_c, "dim", int)() != 4 or K_c.numel() == 0:
+        raise IntfaError("the cache's K is [B, Hkv, Nk, d], or [B, Hkv, Nk, d / 2] in 4 bits, and not empty")
+    B, Hkv, Nk, d = K_c.shape
+    u8, i8, f32 = (torch.uint8,), (torch.int8,), (torch.float32,)
+    four = K_c.dtype is torch.uint8
+    if not four and s_V is None:
+        held, vtype, svshape = IFA_CACHE_I8_F16, (torch.float16,), None
+    else:
+        held, vtype, svshape = (IFA_CACHE_I4, u8, (B, Hkv, Nk)) if four else (IFA_CACHE_I8, i8, (B, Hkv))
+    at = (_operand(K_c, "K_c", u8 if four else i8, K_c.shape, dev), _operand(s_K, "s_K", f32, (B, Hkv, Nk), dev), _operand(V_c, "V_c", vtype, K_c.shape, dev),
+          None if svshape is None else _operand(s_V, "s_V", f32, svshape, dev), None if lens is None else _operand(lens, "lens", (torch.int32,), (B,), dev))
+    return held, (B, Hkv, Nk, 2 * d if four else d), at
+
+
+def _tokens(X, what, dtype, shape, dev):
+    """(address, strides) of activations [B, Hkv, Nn, d] whose rows are contiguous."""
+    import torch
+    if not isinstance(X, torch.Tensor) or not X.is_cuda or X.layout is not torch.strided or X.is_neg() or X.is_conj():
+        raise IntfaError(f"{what}: expected a tensor in GPU memory")
+    if X.dtype is not dtype or tuple(X.shape) != shape:
+        raise IntfaError(f"{what}: expected {tuple(shape)} of {dtype}, got {tuple(X.shape)} of {X.dtype}")
+    if X.stride(3) != 1:
+        raise IntfaError(f"{what}: the channels of a row are adjacent in memory")
+    if X.device.index != dev:
+        raise IntfaError(f"{what} is on {X.device}, the current device is cuda:{dev}")
+    return X.data_ptr(), X.stride()[:3]
+
+
+def append_keys(K, V, K_c, s_K, V_c, s_V=None, lens=None, hadamard=False):
+    """New tokens K, V [B, Hkv, Nn, d] fp32/fp16/bf16 (any strides of b, h and n) quantized into a cache: int8 K_c [B, Hkv, Nk, d] with V_c fp16, or int8 by the
+    given s_V [B, Hkv]; or uint8 K_c, V_c [B, Hkv, Nk, d / 2] in 4 bits with s_V [B, Hkv, Nk]; s_K [B, Hkv, Nk].  lens[b] keys (int32 [B]; None: Nk) count the new ones, which are the last
+    Nn: token i goes to lens[b] - Nn + i, and nowhere if that is below 0.  hadamard=True rotates K as quantize_tokenwise does.  The cache is changed in place."""
+    import torch
+    dev = torch.cuda.current_device()
+    held, (B, Hkv, Nk, d), at = _held(K_c, s_K, V_c, s_V, lens, dev)
+    if getattr(K, "dim", int)() != 4 or K.shape[2] == 0:
+        raise IntfaError("K is [B, Hkv, Nn, d] with at least one token")
+    Nn = K.shape[2]
+    (k, ks), (v, vs) = _tokens(K, "K", K.dtype, (B, Hkv, Nn, d), dev), _tokens(V, "V", K.dtype, (B, Hkv, Nn, d), dev)
+    _check(lib().append_keys(k, v, _dtype_enum(K), *ks, *vs, at[4], B, Hkv, Nn, Nk, d, held, int(bool(hadamard)), *at[:4], _stream()), "append_keys")
+
+
+def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=False, out_dtype=None, out=None):
+    """A run of the cache (as append_keys has it) back as values: (K, V) [B, Hkv, count, d], fp16 unless out_dtype/out says otherwise.  Row i is the key at first + i, or with first=None at
+    lens[b] - count + i; rows in front of key 0 or behind the last one are zeros.  count: None for all from `first` on.  hadamard=True rotates K back.
+    out: optional tuple of the two tensors to write into."""
+    import torch
+    dev = torch.cuda.current_device()
+    held, (B, Hkv, Nk, d), at = _held(K_c, s_K, V_c, s_V, lens, dev)
+    first = -1 if first is None else int(first)
+    if first == -1 and count is None:
+        count = Nk
+    count = Nk - first if count is None else int(count)
+    if first < -1 or first > Nk or count < 1:
+        raise IntfaError(f"{count} keys from {first} on of {Nk}")
+    shape = (B, Hkv, count, d)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=out_dtype or torch.float16, device=K_c.device) for _ in range(2))
+    elif len(out) != 2:
+        raise IntfaError("out: K, V")
+    types = (torch.float16, torch.bfloat16, torch.float32) if out_dtype is None else (out_dtype,)
+    to = _operand(out[0], "out[0]", types, shape, dev), _operand(out[1], "out[1]", (out[0].dtype,), shape, dev)
+    _check(lib().read_keys(*at, B, Hkv, Nk, d, held, int(bool(hadamard)), first, count, *to, _dtype_enum(out[0]), _stream()), "read_keys")
     return tuple(out)
 
 
