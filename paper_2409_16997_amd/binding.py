@@ -46,6 +46,8 @@ SIGNATURES = {
     "evict_keys": (_i, [_vp] * 3 + [_i] + [_vp] * 2 + [_i] * 7 + [_vp] * 7),
     "append_keys": (_i, [_vp] * 2 + [_i] + [_l] * 6 + [_vp] + [_i] * 7 + [_vp] * 5),
     "read_keys": (_i, [_vp] * 5 + [_i] * 6 + [_l, _i] + [_vp] * 2 + [_i, _vp]),
+    "ifa_int4_workspace_bytes": (_l, [_i] * 8),
+    "int_flash_attn_fwd_int4": (_i, [_vp] * 7 + [_i] * 8 + [_vp, _i, _vp, _l, _vp]),
     "ifa_block_cols_half": (_i, [_i, _i]),
     "ifa_debug_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
@@ -618,6 +620,40 @@ def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=
     to = _operand(out[0], "out[0]", types, shape, dev), _operand(out[1], "out[1]", (out[0].dtype,), shape, dev)
     _check(lib().read_keys(*at, B, Hkv, Nk, d, held, int(bool(hadamard)), first, count, *to, _dtype_enum(out[0]), _stream()), "read_keys")
     return tuple(out)
+
+
+def int4_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: int, window=None, sinks: int = 0) -> int:
+    """Bytes of workspace int_flash_attn_fwd_int4 needs for this shape (0: none; -1: sizes that it refuses)."""
+    window = 0x7fffffff if window is None else min(int(window), 0x7fffffff)
+    return int(lib().ifa_int4_workspace_bytes(int(B), int(H), int(Hkv), int(Nq), int(Nk), int(d), window, min(int(sinks), 0x7fffffff)))
+
+
+def int_flash_attn_fwd_int4(Q_i8, K_i4, V_i4, s_Q, s_K, s_V, window=None, sinks=0, lens=None, out_dtype=None, out=None, workspace=None):
+    """Attention over a cache in 4 bits, as append_keys writes it: int8 Q [B, H, Nq, d] (H a multiple of Hkv) with s_Q [B, H, Nq], uint8 K, V [B, Hkv, Nk, d / 2] with s_K, s_V [B, Hkv, Nk].
+    Queries, lens, window (None: every key up to the query's own) and sinks as in int_flash_attn_fwd_window.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).
+    `workspace`: a uint8 device tensor of int4_workspace_bytes(...) bytes (allocated here if not given)."""
+    import torch
+    if getattr(Q_i8, "dim", int)() != 4 or getattr(K_i4, "dim", int)() != 4:
+        raise IntfaError("Q [B, H, Nq, d] and K [B, Hkv, Nk, d / 2] are 4-dimensional")
+    B, H, Nq, d = Q_i8.shape
+    Hkv, Nk = K_i4.shape[1:3]
+    if min(B, H, Nq, d, Hkv, Nk) == 0 or K_i4.shape[0] != B or 2 * K_i4.shape[3] != d or H % Hkv:
+        raise IntfaError(f"Q {tuple(Q_i8.shape)} and K {tuple(K_i4.shape)} in 4 bits do not agree (H is a multiple of Hkv, nothing is empty)")
+    dev = torch.cuda.current_device()
+    u8, f32 = (torch.uint8,), (torch.float32,)
+    at = [_operand(Q_i8, "Q_i8", (torch.int8,), (B, H, Nq, d), dev), _operand(K_i4, "K_i4", u8, (B, Hkv, Nk, d // 2), dev), _operand(V_i4, "V_i4", u8, (B, Hkv, Nk, d // 2), dev),
+          _operand(s_Q, "s_Q", f32, (B, H, Nq), dev), _operand(s_K, "s_K", f32, (B, Hkv, Nk), dev), _operand(s_V, "s_V", f32, (B, Hkv, Nk), dev),
+          None if lens is None else _operand(lens, "lens", (torch.int32,), (B,), dev)]
+    if out is None:
+        out = torch.empty_like(Q_i8, dtype=out_dtype or torch.float16)
+    else:
+        _operand(out, "out", (torch.float16, torch.bfloat16, torch.float32) if out_dtype is None else (out_dtype,), (B, H, Nq, d), dev)
+    window, sinks = 0x7fffffff if window is None else min(int(window), 0x7fffffff), min(int(sinks), 0x7fffffff)
+    if window < 1 or sinks < 0:
+        raise IntfaError("window is at least 1, sinks at least 0")
+    ws, n, _keep = _workspace(workspace, int4_workspace_bytes(B, H, Hkv, Nq, Nk, d, window, sinks), dev)
+    _check(lib().int_flash_attn_fwd_int4(*at, B, H, Hkv, Nq, Nk, d, window, sinks, out.data_ptr(), _dtype_enum(out), ws, n, _stream()), "int_flash_attn_fwd_int4")
+    return out
 
 
 def debug_fwd(Q_i8, K_i8, V_i8, s_Q, s_K, s_V, causal=False, P_in=None, fill=-1):

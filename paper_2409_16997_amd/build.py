@@ -9,7 +9,7 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libintfa.so")
 SOURCES = ["intfa_attention.hip", "intfa_attention_fewq.hip", "intfa_attention_half.hip", "intfa_quantize.hip", "intfa_cache_attention.hip",
-           "intfa_cache_weights.hip", "intfa_append.hip"]
+           "intfa_cache_weights.hip", "intfa_append.hip", "intfa_cache_int4.hip"]
 
 # Packed-fp32 instructions are switched off on purpose (the flag is a device-side feature; the host
 # pass warns that it does not know it, which is harmless).  No fast-math: the quantizer is bit-exact.

@@ -1,0 +1,630 @@
+// Attention over a cache held in 4 bits for gfx950: K and V as codes u - 8, u = 0 .. 15, with one fp32 scale a token and head, window and sinks as for the cache in 8 bits.
+//
+//     S = s_Q s_K (sum q u - 8 sum q)       v_mfma_i32_16x16x64_i8 (32x32x32 in tiles), exact in int32: the accumulator starts at -8 sum q
+//     p = exp(S - M),  w~ = fp16(p s_V)     M per row: 15 (tiles: 7 to 15) log2 units below a bound of log2(p s_V), so that |w~| <= 2^15; l = sum p in fp32
+//     O = sum w~ (u - 8) / l                v_mfma_f32_16x16x32_f16 (32x32x16 in tiles), fp32 accumulation
+//
+// The scale of a token joins its weight, one multiplication a score, where applied to V it would be one a code.  Then the weights' range is that of p s_V: M follows log2 of the
+// largest |s_V| of the keys at hand, and what fp16 cuts off is small beside the largest summand that could be there.  Scales are expected below 2^64; below 2^-64 they count as that for M alone.
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_bf16.h>
+#include <stdint.h>
+#include <type_traits>
+
+#include "intfa.h"
+#include "intfa_internal.h"
+#include "intfa_device.h"
+#include "intfa_cache.h"
+#include "intfa_cache_plan.h"
+#include "intfa_cache_rows.h"
+
+namespace {
+
+using namespace ifa_cache;
+
+constexpr int KEYS4 = 64;                  // keys of a tile
+template <int D> constexpr int ROW4 = D / 2;                 // bytes of a row of codes,
+template <int D> constexpr int TILE4 = KEYS4 * D / 2;        // and of a tile's K or V
+constexpr int WAVES4 = 4;
+[[maybe_unused]] constexpr float LEAST_SCALE = 0x1p-64f;
+[[maybe_unused]] constexpr float FEW4_BELOW = 15.0f, TILE4_BELOW = 7.0f, SLACK4 = 8.0f;     // the largest weight is 2^15; in tiles 2^7, and 2^15 until M moves
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// 16-byte chunks of a row are exchanged by the row so that what is read at once spreads over the banks.  K is read a row to a lane; V transposed, rows 4 q .. 4 q + 3 and those 16
+// further (kernel for few rows), or 8 further (tiles), at once.
+template <int D> __device__ __forceinline__ int k4_slot(int row) { return D == 128 ? (row >> 1) & 3 : (row >> 2) & 1; }
+template <int D> __device__ __forceinline__ int v4_slot_few(int row) { return D == 128 ? (((row >> 1) ^ (row >> 2)) & 1) | (row >> 3 & 2) : row >> 4 & 1; }
+template <int D> __device__ __forceinline__ int v4_slot_tile(int row) { return D == 128 ? (row >> 1 & 1) | (row >> 2 & 2) : row >> 3 & 1; }
+
+constexpr uint32_t LOW4 = 0x0f0f0f0fu;
+
+// 8 keys of a column of bytes (dwords of keys 0 - 3 and 4 - 7) as fp16 operands of the low and of the high channel; keys in the order 0, 2, 1, 3, 4, 6, 5, 7.  u in bits 0 - 3 of a half with the
+// exponent of 1024 above it is 1024 + u, u in bits 4 - 7 with that of 64 is 64 + u; what is taken off leaves u - 8 exactly.  (u alone, as a subnormal number, would save the subtraction, but the matrix
+// unit aligns such operands by their exponent: sums of them were off by 2^-14 and, in bits 4 - 7, 2^-18.)
+__device__ __forceinline__ h2 low_codes(uint32_t w) { return __builtin_bit_cast(h2, (w & 0x000f000fu) | 0x64006400u) - h2{(_Float16)1032.0f, (_Float16)1032.0f}; }
+__device__ __forceinline__ h2 high_codes(uint32_t w) { return __builtin_bit_cast(h2, (w & 0x00f000f0u) | 0x54005400u) - h2{(_Float16)72.0f, (_Float16)72.0f}; }
+__device__ __forceinline__ void values_of(const v2i &w, h8 &low, h8 &high) {
+    const uint32_t a = static_cast<uint32_t>(w[0]), b = static_cast<uint32_t>(w[1]), a8 = a >> 8, b8 = b >> 8;
+    const h2 l0 = low_codes(a), l1 = low_codes(a8), l2 = low_codes(b), l3 = low_codes(b8), h0 = high_codes(a), h1 = high_codes(a8), h2_ = high_codes(b), h3 = high_codes(b8);
+    low = h8{l0[0], l0[1], l1[0], l1[1], l2[0], l2[1], l3[0], l3[1]};
+    high = h8{h0[0], h0[1], h1[0], h1[1], h2_[0], h2_[1], h3[0], h3[1]};
+}
+__device__ __forceinline__ int high_nibbles(int w) { return static_cast<int>(static_cast<uint32_t>(w) >> 4 & LOW4); }
+__device__ __forceinline__ int low_nibbles(int w) { return w & static_cast<int>(LOW4); }
+
+__device__ __forceinline__ float swap16_max(float x) {           // with the lane 16 apart
+    const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+// the largest of 64 lanes, in all of them
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xf, 0xf, true)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, true)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xf, 0xf, true)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xf, 0xf, true)));
+    return pair_max(swap16_max(x));
+}
+// log2 of a bound of |s_V| over the tile, from this lane's key
+__device__ __forceinline__ float scale_bound(float sv) { return __builtin_amdgcn_logf(fmaxf(wave_max(fabsf(sv)), LEAST_SCALE)); }
+#endif
+
+// ---- up to 16 RT rows against many keys: every wavefront for itself ----------------------------------------------------
+// As in the kernel for 8 bits, the four wavefronts of a workgroup hold the same rows, take every fourth tile of keys, without a barrier in the loop, and meet once at the end.  A matrix
+// instruction has 16 query columns, so that a decode step's few rows leave fewer of them idle, and all of a lane's softmax work is for keys of its 16 bytes of K.
+template <int D, int RT, int ST> struct SmemFew4 {
+    union {
+        struct {
+            alignas(4096) int8_t k[WAVES4][ST][TILE4<D>];
+            alignas(4096) int8_t v[WAVES4][ST][TILE4<D>];
+            alignas(256) float sk[WAVES4][ST][KEYS4], sv[WAVES4][ST][KEYS4];
+        };
+        float o[WAVES4][16 * RT][64];                            // when the loop is over: 64 columns at a time
+    };
+    float2 ml[WAVES4][16 * RT];
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+template <int D, int RT, int ST, bool NT>
+__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, const Call &c, int block, int units, int row_tiles) {
+    constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, KS = D / 64, CT = D / 32, ROWS = 16 * RT;
+    constexpr int PER_TILE = 2 * PIECES + 2;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // the row tiles of one share of the keys run 8 apart: on one XCD
+    const int in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), tile_of_rows = in8 >> 3;
+    const int unit = share / c.splits, split = share % c.splits;
+    if (unit >= units) return;
+    const int row0 = ROWS * tile_of_rows, last_row = imin(row0 + ROWS - 1, c.rows - 1);
+    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
+    auto position = [&](int row) { return L - c.Nq + row / c.G; };
+    const int p0 = position(row0), p1 = position(last_row);
+    const Runs runs(false, 0, c.window, c.sinks, p0, p1);
+    const int tilesA = (runs.lenA + KEYS4 - 1) / KEYS4, tiles = tilesA + (runs.lenB + KEYS4 - 1) / KEYS4;
+    const int per = (tiles + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(tiles, t0 + per);
+
+    const long kA = static_cast<long>(unit) * c.Nk, kB = kA + runs.lo;
+    const int8_t *const V = static_cast<const int8_t *>(c.V);
+    const BufRsrc rKA = make_rsrc(c.K + kA * ROW, runs.lenA * ROW), rVA = make_rsrc(V + kA * ROW, runs.lenA * ROW), rSKA = make_rsrc(c.sK + kA, runs.lenA * 4), rSVA = make_rsrc(c.sV + kA, runs.lenA * 4);
+    const BufRsrc rKB = make_rsrc(c.K + kB * ROW, runs.lenB * ROW), rVB = make_rsrc(V + kB * ROW, runs.lenB * ROW), rSKB = make_rsrc(c.sK + kB, runs.lenB * 4), rSVB = make_rsrc(c.sV + kB, runs.lenB * 4);
+
+    constexpr int CH = ROW / 16;
+    const int crow = lane / CH, cslot = lane % CH;               // of a copied piece; an odd one is 16 (d = 64: 32) rows further
+    const unsigned gk = crow * ROW + 16 * (cslot ^ k4_slot<D>(crow));
+    const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot_few<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot_few<D>(crow + 1024 / ROW));
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]), svbuf = (lds_ptr)(&sm.sv[wave][0][0]);
+    auto stage = [&](int t, int slot) {                          // (a tile past the last costs as many copies, of nothing)
+        const bool inA = t < tilesA;
+        const int j0 = KEYS4 * (inA ? t : t - tilesA);
+        const bool real = t < t1;
+        copy_pieces<PIECES, NT>(pick(inA, rKA, rKB), kbuf + slot * TB, gk, gk, real ? j0 * ROW : NOTHING);
+        copy_pieces<PIECES, NT>(pick(inA, rVA, rVB), vbuf + slot * TB, gv0, gv1, real ? j0 * ROW : NOTHING);
+        lds_copy4(pick(inA, rSKA, rSKB), skbuf + slot * 256, 4 * lane, real ? j0 * 4 : NOTHING);
+        lds_copy4(pick(inA, rSVA, rSVB), svbuf + slot * 256, 4 * lane, real ? j0 * 4 : NOTHING);
+    };
+    const int first = t0 + wave;
+#pragma unroll
+    for (int s = 0; s < ST; ++s) stage(first + s * WAVES4, s);
+
+    // where this lane reads K (key r of 16; the 16 bytes, at d = 64 8 bytes, of quarter q) and V (row i / 2 of the 8 that are transposed, half i & 1 of 16 columns)
+    const unsigned k0 = D == 128 ? r * ROW + 16 * (q ^ k4_slot<D>(r)) : r * ROW + 16 * ((q >> 1) ^ k4_slot<D>(r)) + 8 * (q & 1);
+    const int vkey = 4 * q + (r >> 1 & 3) + 16 * (r >> 3);
+    const unsigned v0 = vkey * ROW + 16 * v4_slot_few<D>(vkey) + 8 * (r & 1);
+
+    v4i qf[RT][KS], bias[RT];
+    float sq2[RT];
+    int p[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = imin(row0 + 16 * rt + r, c.rows - 1);
+        p[rt] = position(row);
+        const int8_t *const at = c.Q + row_of(c, false, unit, row) * D;
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[rt][s] = *reinterpret_cast<const v4i *>(at + 64 * s + 16 * q);
+        } else {                                                 // channels in the order in which 8 bytes of K hold them: 8 low ones, then the 8 that are 32 further
+            const v2i a = *reinterpret_cast<const v2i *>(at + 8 * q), b = *reinterpret_cast<const v2i *>(at + 32 + 8 * q);
+            qf[rt][0] = v4i{a[0], a[1], b[0], b[1]};
+        }
+        sq2[rt] = p[rt] >= 0 ? query_scale(c.sQ[row_of(c, false, unit, row)], qf[rt]) : 1.0f;        // (padding: whatever its scale holds, its row is zeros)
+        v4i sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(v4i{0x01010101, 0x01010101, 0x01010101, 0x01010101}, qf[rt][s], sum, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[rt][i] = ACC_BIAS_I - 8 * sum[i];
+    }
+
+    float m2[RT], l[RT];                                         // m2: M
+    v4f o[RT][2][CT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m2[rt] = -INFINITY, l[rt] = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[rt][h][ct] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    int slot = 0;
+    for (int t = first; t < t1; t += WAVES4) {
+        wait_vmcnt<PER_TILE *(ST - 1)>();                        // this tile has landed
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        v4i kw[4];                                               // 16 keys each: the bytes of this lane (d = 64: two dwords)
+        v2i vw[2][CT];                                           // 32 keys each
+        v4f skv[4], svv[4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const lds_ptr at = lds_xor(kbuf + slot * TB + 16 * kb * ROW, 0, k0);
+            if constexpr (D == 128) kw[kb] = *reinterpret_cast<LDS_AS const v4i *>(at);
+            else {
+                const v2i x = *reinterpret_cast<LDS_AS const v2i *>(at);
+                kw[kb] = v4i{x[0], x[1], 0, 0};
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            skv[kb] = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 256 + 16 * q + 64 * kb);
+            svv[kb] = *reinterpret_cast<LDS_AS const v4f *>(svbuf + slot * 256 + 16 * q + 64 * kb);
+        }
+        const float sv_here = *reinterpret_cast<LDS_AS const float *>(svbuf + slot * 256 + 4 * lane);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) vw[h][ct] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_AS v2i *>(lds_xor(vbuf + slot * TB + 32 * h * ROW, 16 * ct, v0)));
+        wait_lds();
+        __builtin_amdgcn_sched_barrier(0);
+        memory_fence_of_the_compiler();
+        stage(t + ST * WAVES4, slot);                            // into the place this tile has left
+        __builtin_amdgcn_sched_barrier(0);
+        slot = slot == ST - 1 ? 0 : slot + 1;
+
+        const float below = FEW4_BELOW - scale_bound(sv_here);
+        v4i kop[4][KS];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            if constexpr (D == 128) {
+                kop[kb][0] = v4i{low_nibbles(kw[kb][0]), low_nibbles(kw[kb][1]), low_nibbles(kw[kb][2]), low_nibbles(kw[kb][3])};
+                kop[kb][KS - 1] = v4i{high_nibbles(kw[kb][0]), high_nibbles(kw[kb][1]), high_nibbles(kw[kb][2]), high_nibbles(kw[kb][3])};
+            } else kop[kb][0] = v4i{low_nibbles(kw[kb][0]), low_nibbles(kw[kb][1]), high_nibbles(kw[kb][0]), high_nibbles(kw[kb][1])};
+        }
+        const bool inA = t < tilesA;
+        const int j0 = KEYS4 * (inA ? t : t - tilesA);
+        // whether all rows see all 64 keys (wave-uniform)
+        const bool clear = p0 >= 0 && (inA ? j0 + KEYS4 <= runs.lenA : j0 + KEYS4 - 1 <= p0 - runs.lo && (j0 > p1 - runs.lo - c.window || j0 + KEYS4 - 1 < c.sinks - runs.lo));
+        h8 pb[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float a[16], tmax = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                v4i acc = bias[rt];
+#pragma unroll
+                for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(kop[kb][s], qf[rt][s], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[4 * kb + i] = (__int_as_float(acc[i]) - ACC_BIAS_F) * skv[kb][i];
+            }
+            if (!clear) {
+                const int hi = (inA ? (p[rt] >= 0 ? runs.lenA - 1 : -1) : p[rt] - runs.lo) - j0;
+                const int from = inA ? 0 : p[rt] - runs.lo - c.window + 1 - j0, sink = inA ? 0 : c.sinks - runs.lo - j0;
+                const uint64_t seen = keys_seen(hi, from, sink) >> (4 * q);
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(static_cast<uint32_t>(seen >> (32 * (kb >> 1))) & (1u << (16 * (kb & 1) + i)))) a[4 * kb + i] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, a[e]);
+            tmax = pair_max(swap16_max(tmax));
+            const float m_new = fmaxf(m2[rt], __builtin_fmaf(tmax, sq2[rt], -below));
+            const float m_at = m_new == -INFINITY ? 0.0f : m_new;    // a row that has seen nothing yet: weights of 0, no NaN
+            const float alpha = __builtin_amdgcn_exp2f(m2[rt] - m_at);   // exp2(-inf) = 0
+            m2[rt] = m_new;
+            float psum = 0.0f;
+            h2 w[8];                                             // keys 0, 2 and 1, 3 of each four: the order of values_of
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[4 * kb + i], sq2[rt], -m_at));
+                    psum += e;
+                    x[i] = e * svv[kb][i];
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w[2 * kb + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
+            }
+            l[rt] = __builtin_fmaf(l[rt], alpha, psum);
+            if (__any(alpha != 1.0f)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) o[rt][h][ct] *= alpha;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) pb[rt][h] = h8{w[4 * h][0], w[4 * h][1], w[4 * h + 1][0], w[4 * h + 1][1], w[4 * h + 2][0], w[4 * h + 2][1], w[4 * h + 3][0], w[4 * h + 3][1]};
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                h8 low, high;
+                values_of(vw[h][ct], low, high);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    o[rt][0][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(low, pb[rt][h], o[rt][0][ct], 0, 0, 0);
+                    o[rt][1][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(high, pb[rt][h], o[rt][1][ct], 0, 0, 0);
+                }
+            }
+    }
+    wait_all_memory();                                           // requests past the last tile
+    __syncthreads();                                             // every wavefront is done with its buffers: o may lie there
+
+    // ---- the four meet
+    float f[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += swap32(l[rt]);
+        l[rt] += __shfl_xor(l[rt], 16);
+        if (q == 0) sm.ml[wave][16 * rt + r] = float2{m2[rt], l[rt]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float m_all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES4; ++w) m_all = fmaxf(m_all, sm.ml[w][16 * rt + r].x);
+        f[rt] = m2[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2[rt] - m_all);
+    }
+    const int valid = last_row - row0 + 1;
+    for (int half = 0; half < D / 64; ++half) {
+        if (half) __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (D == 64 || h == half) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
+                        const int chunk = ((D == 64 ? 8 * h : 0) + 4 * ct + q) ^ r;
+                        *reinterpret_cast<v4f *>(&sm.o[wave][16 * rt + r][4 * chunk]) = o[rt][h][ct] * f[rt];
+                    }
+                }
+        __syncthreads();
+        for (int at = tid; at < valid * 16; at += 64 * WAVES4) {
+            const int rr = at / 16, cc = at % 16;
+            float m = -INFINITY, ls = 0.0f;
+            v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < WAVES4; ++w) m = fmaxf(m, sm.ml[w][rr].x);
+#pragma unroll
+            for (int w = 0; w < WAVES4; ++w) {
+                const float2 x = sm.ml[w][rr];
+                ls += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - m);
+                s += *reinterpret_cast<const v4f *>(&sm.o[w][rr][4 * (cc ^ (rr & 15))]);
+            }
+            if (c.part_o) {
+                const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows + row0 + rr;
+                *reinterpret_cast<v4f *>(c.part_o + pr * D + 64 * half + 4 * cc) = s;
+                if (cc == 0 && half == 0) c.part_ml[pr] = float2{m, ls};
+            } else {
+                const float i = ls > 0.0f ? 1.0f / ls : 0.0f;    // a row that sees nothing: zeros
+                store4(c.O, c.o_dtype, row_of(c, false, unit, row0 + rr) * D + 64 * half + 4 * cc, s[0] * i, s[1] * i, s[2] * i, s[3] * i);
+            }
+        }
+    }
+}
+#endif
+template <int D, int RT, int ST, bool NT>
+__global__ __launch_bounds__(64 * WAVES4, 2) void int4_few_kernel(Call c, int units, int row_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemFew4<D, RT, ST> sm;
+    few4_rows_of_a_unit<D, RT, ST, NT>(sm, c, blockIdx.x, units, row_tiles);
+#endif
+}
+
+// ---- many rows: tiles of 128 ------------------------------------------------------------------------------------------
+// Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered), where they stay in 4 bits; each wavefront unpacks its operands.
+template <int D> struct SmemTile4 {
+    union {
+        struct {
+            alignas(4096) int8_t k[2][TILE4<D>];
+            alignas(4096) int8_t v[2][TILE4<D>];
+            alignas(256) float sk[2][KEYS4], sv[2][KEYS4];
+        };
+        int8_t out[4][64 * D];
+    };
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+template <int D> struct RowState4 {
+    float m2, l;                                                 // m2: M
+    v16f o[D / 32];
+};
+
+// 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.
+template <int D>
+__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, int lane, unsigned k0, unsigned v0, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
+                                            const v16i &bias, RowState4<D> &st) {
+    constexpr int ROW = ROW4<D>, KS = D / 32, HALF = D / 64, DT = D / 32;
+    const int g = lane >> 5;
+    float a[2][16];
+    const float below = TILE4_BELOW - scale_bound(*reinterpret_cast<LDS_AS const float *>(sv + 4 * lane));
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+        v16i acc = bias;
+#pragma unroll
+        for (int x = 0; x < HALF; ++x) {
+            const v4i w = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(ks + 32 * mt * ROW, 32 * x, k0));
+            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{low_nibbles(w[0]), low_nibbles(w[1]), low_nibbles(w[2]), low_nibbles(w[3])}, qf[x], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{high_nibbles(w[0]), high_nibbles(w[1]), high_nibbles(w[2]), high_nibbles(w[3])}, qf[x + KS / 2], acc, 0, 0, 0);
+        }
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) {
+            const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(sk + 16 * g + 128 * mt + 32 * vq);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[4 * vq + e]) - ACC_BIAS_F) * skv[e];
+        }
+    }
+    if (!clear) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * (v >> 2) + (v & 3))))) a[mt][v] = -INFINITY;
+    }
+    float bmax = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
+    const float top = __builtin_fmaf(pair_max(bmax), sq2, -below);
+    const bool moves = top > st.m2 + SLACK4;                     // (st.m2 = -inf: whenever a key counts)
+    if (__any(moves)) {
+        const float m_new = moves ? top : st.m2;
+        const float alpha = moves ? __builtin_amdgcn_exp2f(st.m2 - m_new) : 1.0f;
+        st.m2 = m_new;
+        st.l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) st.o[dt][v] *= alpha;
+    }
+    const float m = st.m2 == -INFINITY ? 0.0f : st.m2;           // a row that has seen nothing yet: weights of 0, no NaN
+    float psum = 0.0f;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+        h2 w[8];
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq) {
+            const v4f svv = *reinterpret_cast<LDS_AS const v4f *>(sv + 16 * g + 128 * mt + 32 * vq);
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][4 * vq + i], sq2, -m));
+                psum += e;
+                x[i] = e * svv[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[2 * vq + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {                            // 16 keys each
+            const h8 pb = {w[4 * s][0], w[4 * s][1], w[4 * s + 1][0], w[4 * s + 1][1], w[4 * s + 2][0], w[4 * s + 2][1], w[4 * s + 3][0], w[4 * s + 3][1]};
+#pragma unroll
+            for (int x = 0; x < HALF; ++x) {
+                h8 low, high;
+                values_of(__builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_AS v2i *>(lds_xor(vs, 32 * x, v0) + (32 * mt + 16 * s) * ROW)), low, high);
+                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(low, pb, st.o[x], 0, 0, 0);
+                st.o[x + HALF] = __builtin_amdgcn_mfma_f32_32x32x16_f16(high, pb, st.o[x + HALF], 0, 0, 0);
+            }
+        }
+    }
+    st.l += psum;
+}
+
+template <int D>
+__device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c, int block, int units, int row_tiles, int head_group) {
+    constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, DT = D / 32, CH = ROW / 16, PIECE_ROWS = 1024 / ROW;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
+    map_workgroup(block, units, row_tiles * c.splits, head_group, true, unit, ord);
+    const int rt = row_tiles - 1 - ord / c.splits, split = ord % c.splits;
+    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk), window = c.window;
+    const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), row = imin(row0 + 32 * wave + r, last_row);
+    auto position = [&](int i) { return L - c.Nq + i / c.G; };
+    const int pos0 = position(row0), pos1 = position(last_row);
+    // The two runs one after the other, cut into blocks of 64 with no seam: key v of them is key v for v < lenA, else key v + gap.  All of it lies in front of key pos1 + 1.
+    const Runs runs(false, 0, window, c.sinks, pos0, pos1);
+    const int lenA = runs.lenA, gap = runs.lo - lenA, keys = lenA + runs.lenB;
+    const int blocks = (keys + KEYS4 - 1) / KEYS4, per = (blocks + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(blocks, t0 + per);
+    // a row at p sees key v iff v <= p - gap and (v > p - gap - window or v < sink); one at p < 0 none
+    const int p = position(row), hi = p < 0 ? -1 : p - gap, sink = imax(lenA, c.sinks - gap);
+    const int w0 = position(imin(row0 + 32 * wave, last_row)), w1 = position(imin(row0 + 32 * wave + 31, last_row));      // of the wavefront's first and last row
+    const int hi0 = w0 < 0 ? -1 : w0 - gap, hi1 = w1 < 0 ? -1 : w1 - gap;
+
+    const long first_key = static_cast<long>(unit) * c.Nk;
+    const int seen_end = imax(0, pos1 + 1);
+    const BufRsrc rK = make_rsrc(c.K + first_key * ROW, seen_end * ROW), rV = make_rsrc(static_cast<const int8_t *>(c.V) + first_key * ROW, seen_end * ROW), rSK = make_rsrc(c.sK + first_key, seen_end * 4),
+                  rSV = make_rsrc(c.sV + first_key, seen_end * 4);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]), svbuf = (lds_ptr)(&sm.sv[0][0]);
+    const int crow = lane / CH, cslot = lane % CH;
+    auto stage = [&](int t, int slot) {                          // K and V: pieces of 1 KB, shared out over the wavefronts; scales by the last two
+        const int v0 = KEYS4 * t;
+        const bool seam = v0 < lenA && v0 + KEYS4 > lenA;        // the block with the seam: row by row
+        const int shift = v0 >= lenA ? gap : 0;
+        auto copy = [&](const BufRsrc &from, lds_ptr to, int piece, int chunk) {
+            const int in = piece * PIECE_ROWS + crow;
+            lds_copy16(from, to + slot * TB + 1024 * piece, in * ROW + 16 * chunk + (seam && v0 + in >= lenA ? gap * ROW : 0), (v0 + shift) * ROW);
+        };
+        if (D == 128 || wave < 2) copy(rK, kbuf, wave & (PIECES - 1), cslot ^ k4_slot<D>((wave & (PIECES - 1)) * PIECE_ROWS + crow));
+        if (D == 128 || wave >= 2) copy(rV, vbuf, wave & (PIECES - 1), cslot ^ v4_slot_tile<D>((wave & (PIECES - 1)) * PIECE_ROWS + crow));
+        if (wave >= 2) lds_copy4(pick(wave == 2, rSK, rSV), (wave == 2 ? skbuf : svbuf) + slot * 256, 4 * (lane + (seam && v0 + lane >= lenA ? gap : 0)), (v0 + shift) * 4);
+    };
+    if (t0 < t1) stage(t0, 0);
+
+    const long qrow = row_of(c, false, unit, row);
+    v4i qf[DT];
+#pragma unroll
+    for (int kk = 0; kk < DT; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
+    const float sq2 = p >= 0 ? query_scale(c.sQ[qrow], qf) : 1.0f;                // (padding: whatever its scale holds, its row is zeros)
+    v16i bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = 0;
+#pragma unroll
+    for (int kk = 0; kk < DT; ++kk) bias = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{0x01010101, 0x01010101, 0x01010101, 0x01010101}, qf[kk], bias, 0, 0, 0);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I - 8 * bias[v];
+    asm volatile("" : "+v"(bias));
+    const unsigned k0 = r * ROW + 16 * (g ^ k4_slot<D>(r));      // chunk 2 x + g at k0 ^ 32 x
+    const int i16 = lane & 15, G = lane >> 4, vkey = 8 * (i16 >> 3) + 4 * g + (i16 >> 1 & 3);
+    const unsigned vo = vkey * ROW + 16 * ((G & 1) ^ v4_slot_tile<D>(vkey)) + 8 * (i16 & 1);    // columns 32 x .. at vo ^ 32 x
+    RowState4<D> st;
+    st.m2 = -INFINITY, st.l = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
+
+    const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows copies only
+    wait_all_memory();
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int slot = (t - t0) & 1, v0 = KEYS4 * t;
+        if (t + 1 < t1) stage(t + 1, slot ^ 1);
+        // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
+        const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + KEYS4 - 1 || v0 < sink);
+        const bool clear = hi0 >= v0 + KEYS4 - 1 && (hi1 - window < v0 || v0 + KEYS4 <= sink);
+        const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
+        memory_fence_of_the_compiler();
+        if (any) tile4_block<D>(kbuf + slot * TB, vbuf + slot * TB, skbuf + slot * 256, svbuf + slot * 256, lane, k0, vo, qf, sq2, clear, seen, bias, st);
+        wait_all_memory();                                       // my part of the next block has landed
+        __syncthreads();                                         // everyone's has, and this one's place is free
+    }
+
+    const float l = st.l + swap32(st.l);
+    const lds_ptr stage_out = (lds_ptr)(&sm) + wave * (64 * D);
+    const int first = row0 + 32 * wave;
+    if (c.part_o) {
+        const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows;
+        float *const po = c.part_o + pr * D;
+        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v]; },
+                             [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(po + static_cast<long>(first + k) * D) : nullptr; });
+        if (g == 0 && first + r < c.rows) c.part_ml[pr + first + r] = float2{st.m2, l};
+        return;
+    }
+    const float f = l > 0.0f ? 1.0f / l : 0.0f;                  // a row that sees nothing: zeros
+    auto store = [&](auto type) {
+        using OutT = decltype(type);
+        store_rows<D, OutT>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * f; },
+                            [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(static_cast<OutT *>(c.O) + row_of(c, false, unit, first + k) * D) : nullptr; });
+    };
+    if (c.o_dtype == IFA_F32) store(float{});
+    else if (c.o_dtype == IFA_F16) store(__half{});
+    else store(__hip_bfloat16{});
+}
+#endif
+template <int D>
+__global__ __launch_bounds__(256, 2) void int4_tile_kernel(Call c, int units, int row_tiles, int head_group) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ SmemTile4<D> sm;
+    tile4_of_a_unit<D>(sm, c, blockIdx.x, units, row_tiles, head_group);
+#endif
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+template <int D>
+int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
+    const int units = c.B * c.Hkv;
+    c.splits = plan.parts;
+    if (plan.parts > 1) {
+        c.part_o = static_cast<float *>(workspace);
+        c.part_ml = reinterpret_cast<float2 *>(c.part_o + static_cast<long>(units) * plan.parts * c.rows * D);
+    }
+    const int row_tiles = static_cast<int>(plan.row_tiles);
+    auto few = [&](auto rt, auto once) {
+        const long grid = (static_cast<long>(units) * plan.parts + 7) / 8 * 8 * row_tiles;
+        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, 1, decltype(once)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * WAVES4), 0, st, c, units, row_tiles);
+    };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    if (plan.tile)
+        hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(static_cast<long>(units) * row_tiles * plan.parts)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
+    else if (plan.rows_at_once == 16) plan.once ? few(one, std::true_type{}) : few(one, std::false_type{});
+    else plan.once ? few(two, std::true_type{}) : few(two, std::false_type{});
+    if (plan.parts > 1) {
+        const Parts parts = {nullptr, c.part_o, nullptr, c.part_ml, 0, plan.parts};
+        const long all_rows = static_cast<long>(units) * c.rows;
+        auto join = [&](auto p) {
+            constexpr int P = decltype(p)::value, ROWS = 1024 / D / P;
+            hipLaunchKernelGGL((cache_attention_join_kernel<D, P>), dim3(static_cast<unsigned>((all_rows + ROWS - 1) / ROWS)), dim3(256), 0, st, c, parts, all_rows);
+        };
+        if (plan.parts > 8) join(std::integral_constant<int, 8>{});
+        else join(std::integral_constant<int, 1>{});
+    }
+    return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;
+}
+
+// Sizes alone: what a call or a workspace query takes
+int refuse_sizes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks) {
+    if (B <= 0 || H <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || d <= 0 || H % Hkv || window <= 0 || sinks < 0) return IFA_ERR_SHAPE;
+    const long heads = static_cast<long>(B) * H, N = Nq > Nk ? Nq : Nk;
+    if (heads > (1L << 40) / N / d) return IFA_ERR_SHAPE;
+    if (d != 64 && d != 128) return IFA_ERR_UNSUPPORTED;
+    if (static_cast<long>(Nk) * d * 2 > 0x7ff00000L) return IFA_ERR_UNSUPPORTED;
+    if (heads * Nq > 1L << 26 || heads > 1L << 23) return IFA_ERR_UNSUPPORTED;      // a launch has less than 2^32 threads: 256 to 16 rows or to a unit, d / 4 to a joined row
+    return IFA_OK;
+}
+
+}  // namespace
+
+extern "C" long ifa_int4_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks) {
+    if (refuse_sizes(B, H, Hkv, Nq, Nk, d, window, sinks)) return -1;
+    return int4_plan(B, Hkv, H / Hkv, Nq, Nk, d, imin(window, Nk), imin(sinks, Nk)).bytes;
+}
+
+extern "C" int int_flash_attn_fwd_int4(const signed char *Q_i8, const void *K_i4, const void *V_i4, const float *s_Q, const float *s_K, const float *s_V, const int *lens,
+                                       int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks, void *O, int o_dtype, void *workspace, long workspace_bytes, void *hip_stream) {
+    if (const int rc = refuse_sizes(B, H, Hkv, Nq, Nk, d, window, sinks)) return rc;
+    if (!Q_i8 || !K_i4 || !V_i4 || !s_Q || !s_K || !s_V || !O) return IFA_ERR_NULL;
+    if (o_dtype < IFA_F32 || o_dtype > IFA_BF16) return IFA_ERR_DTYPE;
+    for (const void *p : {static_cast<const void *>(Q_i8), K_i4, V_i4, static_cast<const void *>(O)})
+        if (!ifa_aligned16(p)) return IFA_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(s_Q), static_cast<const void *>(s_K), static_cast<const void *>(s_V), static_cast<const void *>(lens)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return IFA_ERR_UNSUPPORTED;
+    Call c = {};
+    c.Q = Q_i8, c.K = static_cast<const int8_t *>(K_i4), c.V = V_i4, c.sQ = s_Q, c.sK = s_K, c.sV = s_V, c.lens = lens;
+    c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.window = imin(window, Nk), c.sinks = imin(sinks, Nk);
+    c.rows = c.G * Nq, c.O = O, c.o_dtype = o_dtype;
+    const Int4Plan plan = int4_plan(B, Hkv, c.G, Nq, Nk, d, c.window, c.sinks);
+    if (plan.bytes) {
+        if (!workspace) return IFA_ERR_NULL;
+        if (reinterpret_cast<uintptr_t>(workspace) & 255) return IFA_ERR_UNSUPPORTED;
+        if (workspace_bytes < plan.bytes) return IFA_ERR_WORKSPACE;
+    }
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return d == 128 ? launch<128>(c, plan, workspace, st) : launch<64>(c, plan, workspace, st);
+}

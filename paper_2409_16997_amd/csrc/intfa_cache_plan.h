@@ -78,6 +78,25 @@ static inline AttentionPlan attention_plan(int B, int Hkv, int G, int Nq, int Np
     return p;
 }
 
+// ---- attention over a cache in 4 bits ----
+struct Int4Plan {
+    bool tile, once;                       // tiles of 128 rows; K and V past the caches
+    int rows_at_once, parts;               // of a workgroup; parts of the keys
+    long row_tiles, bytes;                 // of a unit; of workspace
+};
+static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks) {
+    const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
+    const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
+    Int4Plan p = {};
+    p.tile = !few_rows(false, units, rows);
+    p.rows_at_once = p.tile ? TILE_ROWS : rows <= 16 ? 16 : 32;
+    p.row_tiles = (rows + p.rows_at_once - 1) / p.rows_at_once;
+    p.parts = parts_for(512, units * p.row_tiles, keys, 256);
+    p.once = !p.tile && p.row_tiles == 1 && units * keys * (d + 8) > 64L << 20;
+    p.bytes = p.parts > 1 ? units * rows * p.parts * (4L * d + 8) : 0;
+    return p;
+}
+
 // ---- key weights ---------------------------------------------------------------------------------------------------
 // Most rows whose scores are stored, 8 bytes a row and key out and in, rather than K read and multiplied again, d bytes a key.  Stored / again, us, d = 128: 16 sequences x 8 heads x 16384 keys, 8 rows
 // 77 / 120, 16 rows 101 / 120; 1 x 8 x 4096, 16 rows 10.3 / 11.0; 32 x 8 x 2000 30.4 / 34.6.  d = 64: 16 x 8 x 16384, 9 rows 63 / 71, 12 rows 73 / 72, 16 rows 86 / 72; 4 x 8 x 8192 17.4 / 18.5, 19.3 / 18.6, 21.3 / 18.7;
