@@ -347,7 +347,7 @@ typedef enum { IFA_CACHE_I8_F16 = 0, IFA_CACHE_I8 = 1, IFA_CACHE_I4 = 2 } ifa_ca
  *   V      rounded to fp16; or q = clamp(rint(x * (1 / s_V)), -127, 127) by the given scale (0: codes 0); or in 4 bits as K (never rotated).
  *   s_V    null; or [B, Hkv], read; or [B, Hkv, Nk], written.
  * Tokens at p < 0 (padding in front) are not written, nothing else of the cache is changed.  fp32 with round-half-to-even, bit-exact against that definition.  NaN/Inf are outside the contract.
- * Supported: d in {64, 128}; B Hkv Nn <= 2^29.  The cache's arrays overlap neither the tokens, nor lens, nor each other (else IFA_ERR_UNSUPPORTED).
+ * Supported: d in {64, 128}; B Hkv Nn <= 2^28.  The cache's arrays overlap neither the tokens, nor lens, nor each other (else IFA_ERR_UNSUPPORTED).
  */
 int append_keys(const void *K, const void *V, int x_dtype, long K_stride_b, long K_stride_h, long K_stride_n, long V_stride_b, long V_stride_h, long V_stride_n,
                 const int *lens, int B, int Hkv, int Nn, int Nk, int d, int held, int hadamard, void *K_c, float *s_K, void *V_c, float *s_V, void *hip_stream);
@@ -357,7 +357,7 @@ int append_keys(const void *K, const void *V, int x_dtype, long K_stride_b, long
  *   first      row i is the key at first + i (0 <= first <= Nk), or with first = -1 the one at L_b - count + i: where append_keys puts `count` tokens.  Rows that lie in front of key 0 or at or
  *              beyond L_b are zeros.
  *   hadamard   non-zero: K is rotated back (H_d x / d, fp32 butterflies)
- * Supported: d in {64, 128}; B Hkv count <= 2^29.  K and V overlap neither the cache, nor lens, nor each other.
+ * Supported: d in {64, 128}; B Hkv count <= 2^28.  K and V overlap neither the cache, nor lens, nor each other.
  */
 int read_keys(const void *K_c, const float *s_K, const void *V_c, const float *s_V, const int *lens, int B, int Hkv, int Nk, int d, int held, int hadamard,
               long first, int count, void *K, void *V, int x_dtype, void *hip_stream);

@@ -84,7 +84,8 @@ _NATIVE_PATH = os.path.join(_HERE, "_intfa_host.so")
 # the functions of the C ABI that the module calls, in its order
 _NATIVE_CALLS = ("quantize_tokenwise_ex", "quantize_headwise_ex", "quantize_blockwise", "quantize_qkv", "quantize_qk", "int_flash_attn_fwd_rect", "int_flash_attn_fwd_vblock_rect",
                  "int_flash_attn_fwd_half_rect", "int_flash_attn_fwd_splitk", "int_flash_attn_fwd_splitk_static", "ifa_window_workspace_bytes", "int_flash_attn_fwd_window", "ifa_prefix_workspace_bytes",
-                 "int_flash_attn_fwd_prefix", "ifa_key_weights_workspace_bytes", "key_weights", "evict_keys", "ifa_block_cols")
+                 "int_flash_attn_fwd_prefix", "ifa_key_weights_workspace_bytes", "key_weights", "evict_keys", "append_keys", "read_keys", "ifa_int4_workspace_bytes", "int_flash_attn_fwd_int4",
+                 "ifa_block_cols")
 
 
 def _address(fn):
@@ -588,6 +589,8 @@ def append_keys(K, V, K_c, s_K, V_c, s_V=None, lens=None, hadamard=False):
     """New tokens K, V [B, Hkv, Nn, d] fp32/fp16/bf16 (any strides of b, h and n) quantized into a cache: int8 K_c [B, Hkv, Nk, d] with V_c fp16, or int8 by the
     given s_V [B, Hkv]; or uint8 K_c, V_c [B, Hkv, Nk, d / 2] in 4 bits with s_V [B, Hkv, Nk]; s_K [B, Hkv, Nk].  lens[b] keys (int32 [B]; None: Nk) count the new ones, which are the last
     Nn: token i goes to lens[b] - Nn + i, and nowhere if that is below 0.  hadamard=True rotates K as quantize_tokenwise does.  The cache is changed in place."""
+    if (_native or _load_native()).append(K, V, K_c, s_K, V_c, s_V, lens, hadamard):
+        return
     import torch
     dev = torch.cuda.current_device()
     held, (B, Hkv, Nk, d), at = _held(K_c, s_K, V_c, s_V, lens, dev)
@@ -602,10 +605,14 @@ def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=
     """A run of the cache (as append_keys has it) back as values: (K, V) [B, Hkv, count, d], fp16 unless out_dtype/out says otherwise.  Row i is the key at first + i, or with first=None at
     lens[b] - count + i; rows in front of key 0 or behind the last one are zeros.  count: None for all from `first` on.  hadamard=True rotates K back.
     out: optional tuple of the two tensors to write into."""
+    first = -1 if first is None else int(first)
+    if out is None and count is not None:
+        r = (_native or _load_native()).read(K_c, s_K, V_c, s_V, lens, first, count, hadamard, out_dtype)
+        if r is not None:
+            return r
     import torch
     dev = torch.cuda.current_device()
     held, (B, Hkv, Nk, d), at = _held(K_c, s_K, V_c, s_V, lens, dev)
-    first = -1 if first is None else int(first)
     if first == -1 and count is None:
         count = Nk
     count = Nk - first if count is None else int(count)
@@ -632,6 +639,10 @@ def int_flash_attn_fwd_int4(Q_i8, K_i4, V_i4, s_Q, s_K, s_V, window=None, sinks=
     """Attention over a cache in 4 bits, as append_keys writes it: int8 Q [B, H, Nq, d] (H a multiple of Hkv) with s_Q [B, H, Nq], uint8 K, V [B, Hkv, Nk, d / 2] with s_K, s_V [B, Hkv, Nk].
     Queries, lens, window (None: every key up to the query's own) and sinks as in int_flash_attn_fwd_window.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).
     `workspace`: a uint8 device tensor of int4_workspace_bytes(...) bytes (allocated here if not given)."""
+    if out is None:
+        r = (_native or _load_native()).int4(Q_i8, K_i4, V_i4, s_Q, s_K, s_V, window, sinks, lens, out_dtype, workspace)
+        if r is not None:
+            return r
     import torch
     if getattr(Q_i8, "dim", int)() != 4 or getattr(K_i4, "dim", int)() != 4:
         raise IntfaError("Q [B, H, Nq, d] and K [B, Hkv, Nk, d / 2] are 4-dimensional")

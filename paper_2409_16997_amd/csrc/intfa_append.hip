@@ -56,7 +56,7 @@ struct ReadCall {
 };
 
 constexpr int THREADS = 256;
-constexpr long MOST_ROWS = 1L << 29;        // a launch has less than 2^32 threads: up to 4 to a row
+constexpr long MOST_ROWS = 1L << 28;        // a launch has less than 2^32 threads: 8 or 16 to a row, or to two
 
 __device__ __forceinline__ int keys_of(const int *lens, unsigned b, int Nk) {
     if (!lens) return Nk;
@@ -228,11 +228,12 @@ __global__ __launch_bounds__(THREADS) void read_keys_kernel(ReadCall c) {
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
-// Rows of a thread: one while that leaves CUs without a workgroup, then four
-constexpr int MANY = 4;
+// Rows of a thread: one for the first 8192 workgroups' worth, then two, which saves divisions (us with one, two, four everywhere: 5331 x 12 rows of 64 fp32 numbers, rotated, into 8 bits and back 17.8, 20.0,
+// 22.8; 32768 x 8 of 128 bf16 numbers into 4 bits and back 61.0, 60.6, 63.7; 16 x 8 x 16384 read from 4 bits 247, 236, 240).
+constexpr int MANY = 2;
 template <typename F> void by_rows(long rows, int lpr, F f) {
     const long per = THREADS / lpr, one = (rows + per - 1) / per;
-    if (one <= 1024) f(std::integral_constant<int, 1>{}, static_cast<unsigned>(one));
+    if (one <= 8192) f(std::integral_constant<int, 1>{}, static_cast<unsigned>(one));
     else f(std::integral_constant<int, MANY>{}, static_cast<unsigned>((one + MANY - 1) / MANY));
 }
 template <typename F> void by_type(int dtype, F f) {

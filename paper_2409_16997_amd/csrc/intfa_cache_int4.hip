@@ -26,29 +26,32 @@ using namespace ifa_cache;
 constexpr int KEYS4 = 64;                  // keys of a tile
 template <int D> constexpr int ROW4 = D / 2;                 // bytes of a row of codes,
 template <int D> constexpr int TILE4 = KEYS4 * D / 2;        // and of a tile's K or V
-constexpr int WAVES4 = 4;
 [[maybe_unused]] constexpr float LEAST_SCALE = 0x1p-64f;
 [[maybe_unused]] constexpr float FEW4_BELOW = 15.0f, TILE4_BELOW = 7.0f, SLACK4 = 8.0f;     // the largest weight is 2^15; in tiles 2^7, and 2^15 until M moves
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// 16-byte chunks of a row are exchanged by the row so that what is read at once spreads over the banks.  K is read a row to a lane; V transposed, rows 4 q .. 4 q + 3 and those 16
-// further (kernel for few rows), or 8 further (tiles), at once.
+// 16-byte chunks of a row are exchanged by the row so that what is read at once spreads over the banks.  K is read a row to a lane; V transposed, rows 4 q .. 4 q + 3
+// and those 16 further at once.
 template <int D> __device__ __forceinline__ int k4_slot(int row) { return D == 128 ? (row >> 1) & 3 : (row >> 2) & 1; }
-template <int D> __device__ __forceinline__ int v4_slot_few(int row) { return D == 128 ? (((row >> 1) ^ (row >> 2)) & 1) | (row >> 3 & 2) : row >> 4 & 1; }
-template <int D> __device__ __forceinline__ int v4_slot_tile(int row) { return D == 128 ? (row >> 1 & 1) | (row >> 2 & 2) : row >> 3 & 1; }
+template <int D> __device__ __forceinline__ int v4_slot(int row) { return D == 128 ? (((row >> 1) ^ (row >> 2)) & 1) | (row >> 3 & 2) : row >> 4 & 1; }
 
 constexpr uint32_t LOW4 = 0x0f0f0f0fu;
 
 // 8 keys of a column of bytes (dwords of keys 0 - 3 and 4 - 7) as fp16 operands of the low and of the high channel; keys in the order 0, 2, 1, 3, 4, 6, 5, 7.  u in bits 0 - 3 of a half with the
 // exponent of 1024 above it is 1024 + u, u in bits 4 - 7 with that of 64 is 64 + u; what is taken off leaves u - 8 exactly.  (u alone, as a subnormal number, would save the subtraction, but the matrix
 // unit aligns such operands by their exponent: sums of them were off by 2^-14 and, in bits 4 - 7, 2^-18.)
-__device__ __forceinline__ h2 low_codes(uint32_t w) { return __builtin_bit_cast(h2, (w & 0x000f000fu) | 0x64006400u) - h2{(_Float16)1032.0f, (_Float16)1032.0f}; }
-__device__ __forceinline__ h2 high_codes(uint32_t w) { return __builtin_bit_cast(h2, (w & 0x00f000f0u) | 0x54005400u) - h2{(_Float16)72.0f, (_Float16)72.0f}; }
-__device__ __forceinline__ void values_of(const v2i &w, h8 &low, h8 &high) {
+// (v_and_or_b32 takes one scalar operand: the masks live in two registers.)
+struct NibbleMasks {
+    uint32_t low = 0x000f000fu, high = 0x00f000f0u;
+    __device__ __forceinline__ NibbleMasks() { asm volatile("" : "+v"(low), "+v"(high)); }
+};
+__device__ __forceinline__ h2 low_codes(uint32_t w, const NibbleMasks &m) { return __builtin_bit_cast(h2, (w & m.low) | 0x64006400u) - h2{(_Float16)1032.0f, (_Float16)1032.0f}; }
+__device__ __forceinline__ h2 high_codes(uint32_t w, const NibbleMasks &m) { return __builtin_bit_cast(h2, (w & m.high) | 0x54005400u) - h2{(_Float16)72.0f, (_Float16)72.0f}; }
+__device__ __forceinline__ void values_of(const v2i &w, const NibbleMasks &m, h8 &low, h8 &high) {
     const uint32_t a = static_cast<uint32_t>(w[0]), b = static_cast<uint32_t>(w[1]), a8 = a >> 8, b8 = b >> 8;
-    const h2 l0 = low_codes(a), l1 = low_codes(a8), l2 = low_codes(b), l3 = low_codes(b8), h0 = high_codes(a), h1 = high_codes(a8), h2_ = high_codes(b), h3 = high_codes(b8);
+    const h2 l0 = low_codes(a, m), l1 = low_codes(a8, m), l2 = low_codes(b, m), l3 = low_codes(b8, m), u0 = high_codes(a, m), u1 = high_codes(a8, m), u2 = high_codes(b, m), u3 = high_codes(b8, m);
     low = h8{l0[0], l0[1], l1[0], l1[1], l2[0], l2[1], l3[0], l3[1]};
-    high = h8{h0[0], h0[1], h1[0], h1[1], h2_[0], h2_[1], h3[0], h3[1]};
+    high = h8{u0[0], u0[1], u1[0], u1[1], u2[0], u2[1], u3[0], u3[1]};
 }
 __device__ __forceinline__ int high_nibbles(int w) { return static_cast<int>(static_cast<uint32_t>(w) >> 4 & LOW4); }
 __device__ __forceinline__ int low_nibbles(int w) { return w & static_cast<int>(LOW4); }
@@ -56,6 +59,12 @@ __device__ __forceinline__ int low_nibbles(int w) { return w & static_cast<int>(
 __device__ __forceinline__ float swap16_max(float x) {           // with the lane 16 apart
     const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+__device__ __forceinline__ float quarters_sum(float x) {         // of the four lanes 16 apart
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 // the largest of 64 lanes, in all of them
 __device__ __forceinline__ float wave_max(float x) {
@@ -72,30 +81,28 @@ __device__ __forceinline__ float scale_bound(float sv) { return __builtin_amdgcn
 // ---- up to 16 RT rows against many keys: every wavefront for itself ----------------------------------------------------
 // As in the kernel for 8 bits, the four wavefronts of a workgroup hold the same rows, take every fourth tile of keys, without a barrier in the loop, and meet once at the end.  A matrix
 // instruction has 16 query columns, so that a decode step's few rows leave fewer of them idle, and all of a lane's softmax work is for keys of its 16 bytes of K.
-template <int D, int RT, int ST> struct SmemFew4 {
+template <int D, int W, int ST> struct SmemFew4 {
     union {
         struct {
-            alignas(4096) int8_t k[WAVES4][ST][TILE4<D>];
-            alignas(4096) int8_t v[WAVES4][ST][TILE4<D>];
-            alignas(256) float sk[WAVES4][ST][KEYS4], sv[WAVES4][ST][KEYS4];
+            alignas(4096) int8_t k[W][ST][TILE4<D>];
+            alignas(4096) int8_t v[W][ST][TILE4<D>];
+            alignas(256) float sk[W][ST][KEYS4], sv[W][ST][KEYS4];
         };
-        float o[WAVES4][16 * RT][64];                            // when the loop is over: 64 columns at a time
+        float o[W][16][D];                                       // when the loop is over
     };
-    float2 ml[WAVES4][16 * RT];
+    float2 ml[W][16];
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
-template <int D, int RT, int ST, bool NT>
-__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, const Call &c, int block, int units, int row_tiles) {
-    constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, KS = D / 64, CT = D / 32, ROWS = 16 * RT;
+template <int D, int RT, int W, int ST, bool NT>
+__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, const Call &c, int share, int row0, int units) {
+    constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, KS = D / 64, CT = D / 32;
     constexpr int PER_TILE = 2 * PIECES + 2;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // the row tiles of one share of the keys run 8 apart: on one XCD
-    const int in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), tile_of_rows = in8 >> 3;
     const int unit = share / c.splits, split = share % c.splits;
     if (unit >= units) return;
-    const int row0 = ROWS * tile_of_rows, last_row = imin(row0 + ROWS - 1, c.rows - 1);
+    const int last_row = imin(row0 + 16 * RT - 1, c.rows - 1);
     const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
     auto position = [&](int row) { return L - c.Nq + row / c.G; };
     const int p0 = position(row0), p1 = position(last_row);
@@ -111,7 +118,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
     constexpr int CH = ROW / 16;
     const int crow = lane / CH, cslot = lane % CH;               // of a copied piece; an odd one is 16 (d = 64: 32) rows further
     const unsigned gk = crow * ROW + 16 * (cslot ^ k4_slot<D>(crow));
-    const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot_few<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot_few<D>(crow + 1024 / ROW));
+    const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow + 1024 / ROW));
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]), svbuf = (lds_ptr)(&sm.sv[wave][0][0]);
     auto stage = [&](int t, int slot) {                          // (a tile past the last costs as many copies, of nothing)
         const bool inA = t < tilesA;
@@ -124,12 +131,12 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
     };
     const int first = t0 + wave;
 #pragma unroll
-    for (int s = 0; s < ST; ++s) stage(first + s * WAVES4, s);
+    for (int s = 0; s < ST; ++s) stage(first + s * W, s);
 
     // where this lane reads K (key r of 16; the 16 bytes, at d = 64 8 bytes, of quarter q) and V (row i / 2 of the 8 that are transposed, half i & 1 of 16 columns)
     const unsigned k0 = D == 128 ? r * ROW + 16 * (q ^ k4_slot<D>(r)) : r * ROW + 16 * ((q >> 1) ^ k4_slot<D>(r)) + 8 * (q & 1);
     const int vkey = 4 * q + (r >> 1 & 3) + 16 * (r >> 3);
-    const unsigned v0 = vkey * ROW + 16 * v4_slot_few<D>(vkey) + 8 * (r & 1);
+    const unsigned v0 = vkey * ROW + 16 * v4_slot<D>(vkey) + 8 * (r & 1);
 
     v4i qf[RT][KS], bias[RT];
     float sq2[RT];
@@ -165,8 +172,9 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
             for (int ct = 0; ct < CT; ++ct) o[rt][h][ct] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    const NibbleMasks masks;
     int slot = 0;
-    for (int t = first; t < t1; t += WAVES4) {
+    for (int t = first; t < t1; t += W) {
         wait_vmcnt<PER_TILE *(ST - 1)>();                        // this tile has landed
         __builtin_amdgcn_sched_barrier(0);
         memory_fence_of_the_compiler();
@@ -195,7 +203,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
         wait_lds();
         __builtin_amdgcn_sched_barrier(0);
         memory_fence_of_the_compiler();
-        stage(t + ST * WAVES4, slot);                            // into the place this tile has left
+        stage(t + ST * W, slot);                            // into the place this tile has left
         __builtin_amdgcn_sched_barrier(0);
         slot = slot == ST - 1 ? 0 : slot + 1;
 
@@ -270,7 +278,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 h8 low, high;
-                values_of(vw[h][ct], low, high);
+                values_of(vw[h][ct], masks, low, high);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     o[rt][0][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(low, pb[rt][h], o[rt][0][ct], 0, 0, 0);
@@ -281,81 +289,64 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, ST> &sm, con
     wait_all_memory();                                           // requests past the last tile
     __syncthreads();                                             // every wavefront is done with its buffers: o may lie there
 
-    // ---- the four meet
-    float f[RT];
+    // ---- they meet, 16 rows at a time: M, l and o of each as they are, then whoever has four columns of a row weighs them
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        l[rt] += swap32(l[rt]);
-        l[rt] += __shfl_xor(l[rt], 16);
-        if (q == 0) sm.ml[wave][16 * rt + r] = float2{m2[rt], l[rt]};
-    }
-    __syncthreads();
+        if (rt) __syncthreads();
+        const float sum = quarters_sum(l[rt]);
+        if (q == 0) sm.ml[wave][r] = float2{m2[rt], sum};
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        float m_all = -INFINITY;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int w = 0; w < WAVES4; ++w) m_all = fmaxf(m_all, sm.ml[w][16 * rt + r].x);
-        f[rt] = m2[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2[rt] - m_all);
-    }
-    const int valid = last_row - row0 + 1;
-    for (int half = 0; half < D / 64; ++half) {
-        if (half) __syncthreads();
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (D == 64 || h == half) {
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
-                        const int chunk = ((D == 64 ? 8 * h : 0) + 4 * ct + q) ^ r;
-                        *reinterpret_cast<v4f *>(&sm.o[wave][16 * rt + r][4 * chunk]) = o[rt][h][ct] * f[rt];
-                    }
-                }
+            for (int ct = 0; ct < CT; ++ct)                      // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
+                *reinterpret_cast<v4f *>(&sm.o[wave][r][4 * ((D / 8 * h + 4 * ct + q) ^ r)]) = o[rt][h][ct];
         __syncthreads();
-        for (int at = tid; at < valid * 16; at += 64 * WAVES4) {
-            const int rr = at / 16, cc = at % 16;
+        const int valid = imin(last_row - row0 - 16 * rt + 1, 16);
+        for (int at = tid; at < valid * (D / 4); at += 64 * W) {
+            const int rr = at / (D / 4), cc = at % (D / 4), to = row0 + 16 * rt + rr;
+            float2 x[W];
             float m = -INFINITY, ls = 0.0f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) x[k] = sm.ml[k][rr], m = fmaxf(m, x[k].x);
+            const float m_at = m == -INFINITY ? 0.0f : m;        // (a row that has seen nothing: factors of 0)
             v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int w = 0; w < WAVES4; ++w) m = fmaxf(m, sm.ml[w][rr].x);
-#pragma unroll
-            for (int w = 0; w < WAVES4; ++w) {
-                const float2 x = sm.ml[w][rr];
-                ls += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - m);
-                s += *reinterpret_cast<const v4f *>(&sm.o[w][rr][4 * (cc ^ (rr & 15))]);
+            for (int k = 0; k < W; ++k) {
+                const float f = __builtin_amdgcn_exp2f(x[k].x - m_at);
+                ls = __builtin_fmaf(x[k].y, f, ls);
+                s += *reinterpret_cast<const v4f *>(&sm.o[k][rr][4 * (cc ^ rr)]) * f;
             }
             if (c.part_o) {
-                const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows + row0 + rr;
-                *reinterpret_cast<v4f *>(c.part_o + pr * D + 64 * half + 4 * cc) = s;
-                if (cc == 0 && half == 0) c.part_ml[pr] = float2{m, ls};
+                const long pr = static_cast<long>(share) * c.rows + to;
+                *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = s;
+                if (cc == 0) c.part_ml[pr] = float2{m, ls};
             } else {
                 const float i = ls > 0.0f ? 1.0f / ls : 0.0f;    // a row that sees nothing: zeros
-                store4(c.O, c.o_dtype, row_of(c, false, unit, row0 + rr) * D + 64 * half + 4 * cc, s[0] * i, s[1] * i, s[2] * i, s[3] * i);
+                store4(c.O, c.o_dtype, row_of(c, false, unit, to) * D + 4 * cc, s[0] * i, s[1] * i, s[2] * i, s[3] * i);
             }
         }
     }
 }
 #endif
-template <int D, int RT, int ST, bool NT>
-__global__ __launch_bounds__(64 * WAVES4, 2) void int4_few_kernel(Call c, int units, int row_tiles) {
+// Two tiles of 16 rows take a key in 1.45 times what one does; the last workgroup of a unit's rows may have one only (8 sequences x 4 heads, 40 rows on up to 16391 keys DRAFT us, with two throughout DRAFT2).
+template <int D, int RT, int W, int ST, bool NT>
+__global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ SmemFew4<D, RT, ST> sm;
-    few4_rows_of_a_unit<D, RT, ST, NT>(sm, c, blockIdx.x, units, row_tiles);
+    __shared__ SmemFew4<D, W, ST> sm;
+    // the row tiles of one share of the keys run 8 apart: on one XCD
+    const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), row0 = 16 * RT * (in8 >> 3);
+    if (RT == 2 && row0 > 0 && row0 + 16 >= c.rows) few4_rows_of_a_unit<D, 1, W, ST, NT>(sm, c, share, row0, units);
+    else few4_rows_of_a_unit<D, RT, W, ST, NT>(sm, c, share, row0, units);
 #endif
 }
 
 // ---- many rows: tiles of 128 ------------------------------------------------------------------------------------------
-// Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered), where they stay in 4 bits; each wavefront unpacks its operands.
+// Four wavefronts of 32 rows share the keys, 64 at a time, through LDS (double-buffered).  What bounds it is the vector unit, so a block is unpacked once for the four: each thread takes
+// 16 bytes of a row of K and of V from memory a block ahead, and writes them to LDS as the matrix operands are: K in bytes, V in fp16, which the transposing reads then serve as in the kernel for 8 bits.
 template <int D> struct SmemTile4 {
-    union {
-        struct {
-            alignas(4096) int8_t k[2][TILE4<D>];
-            alignas(4096) int8_t v[2][TILE4<D>];
-            alignas(256) float sk[2][KEYS4], sv[2][KEYS4];
-        };
-        int8_t out[4][64 * D];
-    };
+    alignas(4096) int8_t k[2][KEYS4 * D];
+    alignas(4096) int8_t v[2][KEYS4 * 2 * D];
+    alignas(256) float sk[2][KEYS4], sv[2][KEYS4];
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -364,30 +355,54 @@ template <int D> struct RowState4 {
     v16f o[D / 32];
 };
 
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+// 16 bytes of a row of codes to where they belong: `low` and, for the high nibbles, `high`
+__device__ __forceinline__ void unpack_k(const u4 &w, lds_ptr low, lds_ptr high) {
+    *reinterpret_cast<LDS_AS u4 *>(low) = w & LOW4;
+    *reinterpret_cast<LDS_AS u4 *>(high) = w >> 4 & LOW4;
+}
+__device__ __forceinline__ void unpack_v(const u4 &w, const NibbleMasks &m, lds_ptr low, lds_ptr high) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        u4 lo, hi;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t a = __builtin_amdgcn_perm(0, w[i + e], 0x0c010c00u), b = __builtin_amdgcn_perm(0, w[i + e], 0x0c030c02u);      // bytes 0, 1 and 2, 3 apart
+            lo[2 * e] = __builtin_bit_cast(uint32_t, low_codes(a, m)), lo[2 * e + 1] = __builtin_bit_cast(uint32_t, low_codes(b, m));
+            hi[2 * e] = __builtin_bit_cast(uint32_t, high_codes(a, m)), hi[2 * e + 1] = __builtin_bit_cast(uint32_t, high_codes(b, m));
+        }
+        *reinterpret_cast<LDS_AS u4 *>(low + 8 * i) = lo;
+        *reinterpret_cast<LDS_AS u4 *>(high + 8 * i) = hi;
+    }
+}
+
 // 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.
 template <int D>
-__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, int lane, unsigned k0, unsigned v0, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
+__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, int lane, const Lane<D, false> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
                                             const v16i &bias, RowState4<D> &st) {
-    constexpr int ROW = ROW4<D>, KS = D / 32, HALF = D / 64, DT = D / 32;
+    constexpr int KS = D / 32, DT = D / 32;
     const int g = lane >> 5;
+    v16i acc[2];
     float a[2][16];
-    const float below = TILE4_BELOW - scale_bound(*reinterpret_cast<LDS_AS const float *>(sv + 4 * lane));
+    v4i kop[KS];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
-        v16i acc = bias;
 #pragma unroll
-        for (int x = 0; x < HALF; ++x) {
-            const v4i w = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(ks + 32 * mt * ROW, 32 * x, k0));
-            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{low_nibbles(w[0]), low_nibbles(w[1]), low_nibbles(w[2]), low_nibbles(w[3])}, qf[x], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{high_nibbles(w[0]), high_nibbles(w[1]), high_nibbles(w[2]), high_nibbles(w[3])}, qf[x + KS / 2], acc, 0, 0, 0);
-        }
+        for (int kk = 0; kk < KS; ++kk) kop[kk] = *reinterpret_cast<LDS_AS const v4i *>(lds_xor(ks, 32 * kk, lo.k0) + 32 * mt * D);
+        acc[mt] = bias;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) acc[mt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc[mt], 0, 0, 0);
+    }
+    const float below = TILE4_BELOW - scale_bound(*reinterpret_cast<LDS_AS const float *>(sv + 4 * lane));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int vq = 0; vq < 4; ++vq) {
             const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(sk + 16 * g + 128 * mt + 32 * vq);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[4 * vq + e]) - ACC_BIAS_F) * skv[e];
+            for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[mt][4 * vq + e]) - ACC_BIAS_F) * skv[e];
         }
-    }
     if (!clear) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
@@ -400,6 +415,7 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
+    __builtin_amdgcn_sched_barrier(0);
     const float top = __builtin_fmaf(pair_max(bmax), sq2, -below);
     const bool moves = top > st.m2 + SLACK4;                     // (st.m2 = -inf: whenever a key counts)
     if (__any(moves)) {
@@ -413,41 +429,51 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
             for (int v = 0; v < 16; ++v) st.o[dt][v] *= alpha;
     }
     const float m = st.m2 == -INFINITY ? 0.0f : st.m2;           // a row that has seen nothing yet: weights of 0, no NaN
-    float psum = 0.0f;
+    h2 ph[2][8];
+    float sum = 0.0f;                                            // of the block: small weights do not meet l one by one
+    auto weights = [&](int mt, int vq) {                         // of 4 keys
+        const v4f svv = *reinterpret_cast<LDS_AS const v4f *>(sv + 16 * g + 128 * mt + 32 * vq);
+        float x[4];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-        h2 w[8];
-#pragma unroll
-        for (int vq = 0; vq < 4; ++vq) {
-            const v4f svv = *reinterpret_cast<LDS_AS const v4f *>(sv + 16 * g + 128 * mt + 32 * vq);
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][4 * vq + i], sq2, -m));
-                psum += e;
-                x[i] = e * svv[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) w[2 * vq + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
+        for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][4 * vq + i], sq2, -m));
+            sum += e;
+            x[i] = e * svv[i];
         }
+        ph[mt][2 * vq] = h2{(_Float16)x[0], (_Float16)x[1]};
+        ph[mt][2 * vq + 1] = h2{(_Float16)x[2], (_Float16)x[3]};
+    };
+    // the weights of the second 32 keys between the products of the first
+    h8 vop[DT][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {                            // 16 keys each
-            const h8 pb = {w[4 * s][0], w[4 * s][1], w[4 * s + 1][0], w[4 * s + 1][1], w[4 * s + 2][0], w[4 * s + 2][1], w[4 * s + 3][0], w[4 * s + 3][1]};
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int x = 0; x < HALF; ++x) {
-                h8 low, high;
-                values_of(__builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_AS v2i *>(lds_xor(vs, 32 * x, v0) + (32 * mt + 16 * s) * ROW)), low, high);
-                st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(low, pb, st.o[x], 0, 0, 0);
-                st.o[x + HALF] = __builtin_amdgcn_mfma_f32_32x32x16_f16(high, pb, st.o[x + HALF], 0, 0, 0);
+        for (int s = 0; s < 2; ++s) vop[dt][s] = v_operand<D, false>(vs, lo.v0, dt, 16 * s);
+#pragma unroll
+    for (int vq = 0; vq < 4; ++vq) weights(0, vq);
+    __builtin_amdgcn_s_setprio(3);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const h8 pb = {ph[mt][4 * s][0], ph[mt][4 * s][1], ph[mt][4 * s + 1][0], ph[mt][4 * s + 1][1], ph[mt][4 * s + 2][0], ph[mt][4 * s + 2][1], ph[mt][4 * s + 3][0], ph[mt][4 * s + 3][1]};
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vop[dt][s], pb, st.o[dt], 0, 0, 0);
+                if (mt == 0) vop[dt][s] = v_operand<D, false>(vs, lo.v0, dt, 32 + 16 * s);
+            }
+            if (mt == 0) {
+#pragma unroll
+                for (int q = 0; q < 4 / DT; ++q) weights(1, dt * (4 / DT) + q);
             }
         }
-    }
-    st.l += psum;
+    st.l += sum;
+    __builtin_amdgcn_s_setprio(0);
 }
 
 template <int D>
 __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c, int block, int units, int row_tiles, int head_group) {
-    constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, DT = D / 32, CH = ROW / 16, PIECE_ROWS = 1024 / ROW;
+    constexpr int ROW = ROW4<D>, KB = KEYS4 * D, VB = KEYS4 * 2 * D, DT = D / 32, CH = ROW / 16;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
@@ -466,25 +492,33 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     const int w0 = position(imin(row0 + 32 * wave, last_row)), w1 = position(imin(row0 + 32 * wave + 31, last_row));      // of the wavefront's first and last row
     const int hi0 = w0 < 0 ? -1 : w0 - gap, hi1 = w1 < 0 ? -1 : w1 - gap;
 
+    // Of a block this thread takes 16 bytes of K and of V (d = 64: the first half of the threads of K, the second of V), and a scale of K (first wavefront) or of V (second)
     const long first_key = static_cast<long>(unit) * c.Nk;
     const int seen_end = imax(0, pos1 + 1);
-    const BufRsrc rK = make_rsrc(c.K + first_key * ROW, seen_end * ROW), rV = make_rsrc(static_cast<const int8_t *>(c.V) + first_key * ROW, seen_end * ROW), rSK = make_rsrc(c.sK + first_key, seen_end * 4),
-                  rSV = make_rsrc(c.sV + first_key, seen_end * 4);
-    const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]), svbuf = (lds_ptr)(&sm.sv[0][0]);
-    const int crow = lane / CH, cslot = lane % CH;
-    auto stage = [&](int t, int slot) {                          // K and V: pieces of 1 KB, shared out over the wavefronts; scales by the last two
-        const int v0 = KEYS4 * t;
-        const bool seam = v0 < lenA && v0 + KEYS4 > lenA;        // the block with the seam: row by row
-        const int shift = v0 >= lenA ? gap : 0;
-        auto copy = [&](const BufRsrc &from, lds_ptr to, int piece, int chunk) {
-            const int in = piece * PIECE_ROWS + crow;
-            lds_copy16(from, to + slot * TB + 1024 * piece, in * ROW + 16 * chunk + (seam && v0 + in >= lenA ? gap * ROW : 0), (v0 + shift) * ROW);
-        };
-        if (D == 128 || wave < 2) copy(rK, kbuf, wave & (PIECES - 1), cslot ^ k4_slot<D>((wave & (PIECES - 1)) * PIECE_ROWS + crow));
-        if (D == 128 || wave >= 2) copy(rV, vbuf, wave & (PIECES - 1), cslot ^ v4_slot_tile<D>((wave & (PIECES - 1)) * PIECE_ROWS + crow));
-        if (wave >= 2) lds_copy4(pick(wave == 2, rSK, rSV), (wave == 2 ? skbuf : svbuf) + slot * 256, 4 * (lane + (seam && v0 + lane >= lenA ? gap : 0)), (v0 + shift) * 4);
+    const auto rsrc = [&](const void *at, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, bytes, 0x00020000); };
+    const auto rK = rsrc(c.K + first_key * ROW, seen_end * ROW), rV = rsrc(static_cast<const int8_t *>(c.V) + first_key * ROW, seen_end * ROW), rSK = rsrc(c.sK + first_key, seen_end * 4),
+               rSV = rsrc(c.sV + first_key, seen_end * 4);
+    const int piece = D == 128 ? tid : tid & 127, prow = piece / CH, pc = piece % CH;
+    u4 kraw = {}, vraw = {};
+    float sraw = 0.0f;
+    auto fetch = [&](int t) {
+        const int at = KEYS4 * t;
+        auto key = [&](int in) { return at + in + (at + in >= lenA ? gap : 0); };       // (row by row: a block may hold the seam)
+        const int from = key(prow) * ROW + 16 * pc;
+        if (D == 128 || wave < 2) kraw = __builtin_amdgcn_raw_buffer_load_b128(rK, from, 0, 0);
+        if (D == 128 || wave >= 2) vraw = __builtin_amdgcn_raw_buffer_load_b128(rV, from, 0, 0);
+        if (wave < 2) sraw = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(wave == 0 ? rSK : rSV, key(lane) * 4, 0, 0));
     };
-    if (t0 < t1) stage(t0, 0);
+    const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]), svbuf = (lds_ptr)(&sm.sv[0][0]);
+    const NibbleMasks masks;
+    const unsigned kat = prow * D, kx = k_slot<D>(prow), vat = prow * 2 * D + 32 * (pc & 1), vx = v_slot<D, false>(prow);
+    auto unpack = [&](int slot) {
+        const lds_ptr k = kbuf + slot * KB + kat, v = vbuf + slot * VB + vat;
+        if (D == 128 || wave < 2) unpack_k(kraw, k + 16 * (pc ^ kx), k + 16 * ((pc + D / 32) ^ kx));
+        if (D == 128 || wave >= 2) unpack_v(vraw, masks, v + 64 * ((pc >> 1) ^ vx), v + 64 * (((pc >> 1) + D / 64) ^ vx));
+        if (wave < 2) *reinterpret_cast<LDS_AS float *>((wave == 0 ? skbuf : svbuf) + slot * 256 + 4 * lane) = sraw;
+    };
+    if (t0 < t1) fetch(t0);
 
     const long qrow = row_of(c, false, unit, row);
     v4i qf[DT];
@@ -499,9 +533,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
 #pragma unroll
     for (int v = 0; v < 16; ++v) bias[v] = ACC_BIAS_I - 8 * bias[v];
     asm volatile("" : "+v"(bias));
-    const unsigned k0 = r * ROW + 16 * (g ^ k4_slot<D>(r));      // chunk 2 x + g at k0 ^ 32 x
-    const int i16 = lane & 15, G = lane >> 4, vkey = 8 * (i16 >> 3) + 4 * g + (i16 >> 1 & 3);
-    const unsigned vo = vkey * ROW + 16 * ((G & 1) ^ v4_slot_tile<D>(vkey)) + 8 * (i16 & 1);    // columns 32 x .. at vo ^ 32 x
+    const Lane<D, false> lo(lane);
     RowState4<D> st;
     st.m2 = -INFINITY, st.l = 0.0f;
 #pragma unroll
@@ -509,20 +541,20 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
 #pragma unroll
         for (int v = 0; v < 16; ++v) st.o[dt][v] = 0.0f;
 
-    const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows copies only
-    wait_all_memory();
+    const bool alive = row0 + 32 * wave < c.rows;                // (wave-uniform) a wavefront without rows unpacks only
+    if (t0 < t1) unpack(0);
+    if (t0 + 1 < t1) fetch(t0 + 1);
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int slot = (t - t0) & 1, v0 = KEYS4 * t;
-        if (t + 1 < t1) stage(t + 1, slot ^ 1);
+        if (t + 1 < t1) unpack(slot ^ 1);                        // (whose readers have passed the last barrier)
+        if (t + 2 < t1) fetch(t + 2);
         // (wave-uniform) whether some of the rows see some of the keys, and whether all see all
         const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + KEYS4 - 1 || v0 < sink);
         const bool clear = hi0 >= v0 + KEYS4 - 1 && (hi1 - window < v0 || v0 + KEYS4 <= sink);
         const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
-        memory_fence_of_the_compiler();
-        if (any) tile4_block<D>(kbuf + slot * TB, vbuf + slot * TB, skbuf + slot * 256, svbuf + slot * 256, lane, k0, vo, qf, sq2, clear, seen, bias, st);
-        wait_all_memory();                                       // my part of the next block has landed
-        __syncthreads();                                         // everyone's has, and this one's place is free
+        if (any) tile4_block<D>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, svbuf + slot * 256, lane, lo, qf, sq2, clear, seen, bias, st);
+        __syncthreads();
     }
 
     const float l = st.l + swap32(st.l);
@@ -558,23 +590,27 @@ __global__ __launch_bounds__(256, 2) void int4_tile_kernel(Call c, int units, in
 // ---- host --------------------------------------------------------------------------------------------------------------
 template <int D>
 int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
-    const int units = c.B * c.Hkv;
+    const int units = c.B * c.Hkv, row_tiles = static_cast<int>(plan.row_tiles);
     c.splits = plan.parts;
     if (plan.parts > 1) {
         c.part_o = static_cast<float *>(workspace);
         c.part_ml = reinterpret_cast<float2 *>(c.part_o + static_cast<long>(units) * plan.parts * c.rows * D);
     }
-    const int row_tiles = static_cast<int>(plan.row_tiles);
-    auto few = [&](auto rt, auto once) {
-        const long grid = (static_cast<long>(units) * plan.parts + 7) / 8 * 8 * row_tiles;
-        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, 1, decltype(once)::value>), dim3(static_cast<unsigned>(grid)), dim3(64 * WAVES4), 0, st, c, units, row_tiles);
+    auto few = [&](auto rt, auto waves, auto once) {
+        constexpr int W = decltype(waves)::value;
+        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, W, W == 8 ? 2 : 1, decltype(once)::value>), dim3(static_cast<unsigned>((static_cast<long>(units) * plan.parts + 7) / 8 * 8 * row_tiles)),
+                           dim3(64 * W), 0, st, c, units, row_tiles);
     };
-    constexpr std::integral_constant<int, 1> one{};
-    constexpr std::integral_constant<int, 2> two{};
+    auto few_waves = [&](auto rt) {
+        constexpr std::integral_constant<int, 4> four{};
+        if (plan.waves == 8) few(rt, std::integral_constant<int, 8>{}, std::false_type{});
+        else if (plan.once) few(rt, four, std::true_type{});
+        else few(rt, four, std::false_type{});
+    };
     if (plan.tile)
         hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(static_cast<long>(units) * row_tiles * plan.parts)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
-    else if (plan.rows_at_once == 16) plan.once ? few(one, std::true_type{}) : few(one, std::false_type{});
-    else plan.once ? few(two, std::true_type{}) : few(two, std::false_type{});
+    else if (plan.rows_at_once == 16) few_waves(std::integral_constant<int, 1>{});
+    else few_waves(std::integral_constant<int, 2>{});
     if (plan.parts > 1) {
         const Parts parts = {nullptr, c.part_o, nullptr, c.part_ml, 0, plan.parts};
         const long all_rows = static_cast<long>(units) * c.rows;
@@ -603,7 +639,7 @@ int refuse_sizes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int s
 
 extern "C" long ifa_int4_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks) {
     if (refuse_sizes(B, H, Hkv, Nq, Nk, d, window, sinks)) return -1;
-    return int4_plan(B, Hkv, H / Hkv, Nq, Nk, d, imin(window, Nk), imin(sinks, Nk)).bytes;
+    return int4_plan(B, Hkv, H / Hkv, Nq, Nk, d, imin(window, Nk), imin(sinks, Nk), true).bytes;
 }
 
 extern "C" int int_flash_attn_fwd_int4(const signed char *Q_i8, const void *K_i4, const void *V_i4, const float *s_Q, const float *s_K, const float *s_V, const int *lens,
@@ -619,7 +655,7 @@ extern "C" int int_flash_attn_fwd_int4(const signed char *Q_i8, const void *K_i4
     c.Q = Q_i8, c.K = static_cast<const int8_t *>(K_i4), c.V = V_i4, c.sQ = s_Q, c.sK = s_K, c.sV = s_V, c.lens = lens;
     c.B = B, c.Hkv = Hkv, c.G = H / Hkv, c.Nq = Nq, c.Nk = Nk, c.window = imin(window, Nk), c.sinks = imin(sinks, Nk);
     c.rows = c.G * Nq, c.O = O, c.o_dtype = o_dtype;
-    const Int4Plan plan = int4_plan(B, Hkv, c.G, Nq, Nk, d, c.window, c.sinks);
+    const Int4Plan plan = int4_plan(B, Hkv, c.G, Nq, Nk, d, c.window, c.sinks, lens != nullptr);
     if (plan.bytes) {
         if (!workspace) return IFA_ERR_NULL;
         if (reinterpret_cast<uintptr_t>(workspace) & 255) return IFA_ERR_UNSUPPORTED;

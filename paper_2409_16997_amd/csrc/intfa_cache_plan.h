@@ -78,20 +78,36 @@ static inline AttentionPlan attention_plan(int B, int Hkv, int G, int Nq, int Np
     return p;
 }
 
-// ---- attention over a cache in 4 bits ----
+// ---- attention over a cache in 4 bits ------------------------------------------------------------------------
 struct Int4Plan {
     bool tile, once;                       // tiles of 128 rows; K and V past the caches
-    int rows_at_once, parts;               // of a workgroup; parts of the keys
+    int rows_at_once, waves, parts;        // of a workgroup; parts of the keys of a unit
     long row_tiles, bytes;                 // of a unit; of workspace
 };
-static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks) {
+#ifndef RP2
+#define RP2 512
+#endif
+static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool ragged) {
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
     Int4Plan p = {};
-    p.tile = !few_rows(false, units, rows);
+    const long few_tiles = row_tiles(true, rows), tiles = row_tiles(false, rows);
+    p.tile = 2 * few_tiles >= 7 * tiles && units * few_tiles * keys > 900L << 10;
     p.rows_at_once = p.tile ? TILE_ROWS : rows <= 16 ? 16 : 32;
     p.row_tiles = (rows + p.rows_at_once - 1) / p.rows_at_once;
-    p.parts = parts_for(512, units * p.row_tiles, keys, 256);
+    const long groups = units * p.row_tiles;
+    p.waves = 4;
+    p.parts = 1;
+    if (p.tile) p.parts = parts_for(512, groups, keys, 256);
+    else if (groups <= 128 && keys > 320 && keys <= (d == 64 ? 1024 : 896)) p.waves = 8;
+    else {
+        const long rounds = (keys + 255) / 256;                  // of four wavefronts
+        long parts = (ragged ? (p.rows_at_once == 32 ? RP2 : 768) : 512) / groups;
+        if (parts > rounds) parts = rounds;
+        if (parts > MOST_PARTS) parts = MOST_PARTS;
+        const long fewer = parts > 0 ? rounds - (rounds + parts - 1) / parts : 0;
+        if (fewer >= 3 && 64 * fewer >= 3 * groups) p.parts = static_cast<int>(parts);
+    }
     p.once = !p.tile && p.row_tiles == 1 && units * keys * (d + 8) > 64L << 20;
     p.bytes = p.parts > 1 ? units * rows * p.parts * (4L * d + 8) : 0;
     return p;

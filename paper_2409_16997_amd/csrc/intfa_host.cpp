@@ -39,6 +39,10 @@ struct Abi {
     decltype(&::ifa_key_weights_workspace_bytes) weights_bytes;
     decltype(&::key_weights) weights;
     decltype(&::evict_keys) evict;
+    decltype(&::append_keys) append;
+    decltype(&::read_keys) read;
+    decltype(&::ifa_int4_workspace_bytes) int4_bytes;
+    decltype(&::int_flash_attn_fwd_int4) int4;
     decltype(&::ifa_block_cols) block_cols;
 } abi;
 constexpr int ABI_FUNCTIONS = sizeof(Abi) / sizeof(void *);
@@ -392,8 +396,89 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- writing the cache, and a cache in 4 bits
+// The cache's arrays K, s_K, V, s_V (None for fp16 V) and lens, from a[0] on
+struct Held {
+    const at::Tensor *k, *sk, *v, *sv = nullptr, *lens = nullptr;
+    int held, B, Hkv, Nk, d;
+    bool take(c10::DeviceIndex dev, PyObject *const *a, PyObject *lens_) {
+        if (!(k = plain(a[0], dev)) || !(sk = plain(a[1], dev)) || !(v = plain(a[2], dev)) || !optional(a[3], dev, sv) || !optional(lens_, dev, lens) || k->dim() != 4) return false;
+        for (const auto s : k->sizes()) if (s > INT_MAX / 2) return false;
+        B = static_cast<int>(k->size(0)), Hkv = static_cast<int>(k->size(1)), Nk = static_cast<int>(k->size(2)), d = static_cast<int>(k->size(3));
+        const bool four = k->scalar_type() == at::kByte;
+        if (!four && k->scalar_type() != at::kChar) return false;
+        held = four ? IFA_CACHE_I4 : sv ? IFA_CACHE_I8 : IFA_CACHE_I8_F16;
+        if (four) d *= 2;
+        if (!is(v, four ? at::kByte : sv ? at::kChar : at::kHalf, k->sizes()) || !is(sk, at::kFloat, {B, Hkv, Nk}) || (lens && !is(lens, at::kInt, {B}))) return false;
+        return four ? sv && is(sv, at::kFloat, {B, Hkv, Nk}) : !sv || is(sv, at::kFloat, {B, Hkv});
+    }
+    float *scale() const { return sv ? f32(*sv) : nullptr; }
+    const int *lengths() const { return lens ? static_cast<const int *>(lens->data_ptr()) : nullptr; }
+};
+// Activations [B, Hkv, Nn, d] whose rows are contiguous, of any strides otherwise
+const at::Tensor *tokens(PyObject *o, c10::DeviceIndex device, const Held &c) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.defined() && t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.is_neg() && !t.is_conj() && t.numel() > 0 && t.device().index() == device && t.dim() == 4 &&
+           t.stride(3) == 1 && t.size(0) == c.B && t.size(1) == c.Hkv && t.size(2) <= INT_MAX && t.size(3) == c.d ? &t : nullptr;
+}
+
+// append(K, V, K_c, s_K, V_c, s_V, lens, hadamard): True when it is done
+PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Held c;
+        const at::Tensor *k, *v;
+        if (n != 8 || !c.take(dev, a + 2, a[6]) || !(k = tokens(a[0], dev, c)) || !(v = tokens(a[1], dev, c)) || !PyBool_Check(a[7])) return nullptr;
+        const int dt = dtype_enum(k->scalar_type());
+        if (dt < 0 || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes()) return nullptr;
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.append, k->data_ptr(), v->data_ptr(), dt, k->stride(0), k->stride(1), k->stride(2), v->stride(0), v->stride(1), v->stride(2), c.lengths(), c.B, c.Hkv,
+                                static_cast<int>(k->size(2)), c.Nk, c.d, c.held, static_cast<int>(a[7] == Py_True), c.k->data_ptr(), f32(*c.sk), c.v->data_ptr(), c.scale(), st);
+        if (!succeeded(rc, "append_keys")) return nullptr;
+        Py_RETURN_TRUE;
+    });
+}
+
+// read(K_c, s_K, V_c, s_V, lens, first (-1: the last), count, hadamard, out_dtype)
+PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Held c;
+        int count, overflow = 0;
+        if (n != 9 || !c.take(dev, a, a[4]) || !PyLong_CheckExact(a[5]) || !integer(a[6], count) || count < 1 || !PyBool_Check(a[7])) return nullptr;
+        const long first = PyLong_AsLongAndOverflow(a[5], &overflow);
+        const at::ScalarType ot = a[8] == Py_None ? at::kHalf : THPDtype_Check(a[8]) ? reinterpret_cast<THPDtype *>(a[8])->scalar_type : at::kChar;
+        const int dt = dtype_enum(ot);
+        if (overflow || first < -1 || first > c.Nk || dt < 0 || static_cast<long>(c.B) * c.Hkv * count > 1L << 28 || (c.d != 64 && c.d != 128)) return nullptr;      // (sizes that are refused allocate nothing)
+        const at::Tensor k = at::detail::empty_cuda({c.B, c.Hkv, count, c.d}, ot, c.k->device(), std::nullopt), v = at::detail::empty_cuda({c.B, c.Hkv, count, c.d}, ot, c.k->device(), std::nullopt);
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.read, c.k->data_ptr(), f32(*c.sk), c.v->data_ptr(), c.scale(), c.lengths(), c.B, c.Hkv, c.Nk, c.d, c.held, static_cast<int>(a[7] == Py_True), first, count, k.data_ptr(),
+                                v.data_ptr(), dt, st);
+        return succeeded(rc, "read_keys") ? tuple({k, v}) : nullptr;
+    });
+}
+
+// int4(Q, K, V, s_Q, s_K, s_V, window or None, sinks, lens, out_dtype, workspace)
+PyObject *int4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&](c10::DeviceIndex dev) -> PyObject * {
+        Held c;
+        const at::Tensor *q, *sq, *given = nullptr;
+        int w = INT_MAX, sinks, o_dtype;
+        at::Tensor out;
+        Workspace ws;
+        if (n != 11) return nullptr;
+        PyObject *const cache[4] = {a[1], a[4], a[2], a[5]};
+        if (!c.take(dev, cache, a[8]) || c.held != IFA_CACHE_I4 || !(q = plain(a[0], dev)) || !(sq = plain(a[3], dev)) || (a[6] != Py_None && !integer(a[6], w)) || !integer(a[7], sinks) || !optional(a[10], dev, given) ||
+            q->dim() != 4 || q->scalar_type() != at::kChar || q->size(0) != c.B || q->size(1) > INT_MAX || q->size(1) % c.Hkv || q->size(2) > INT_MAX || q->size(3) != c.d) return nullptr;
+        const int H = static_cast<int>(q->size(1)), Nq = static_cast<int>(q->size(2));
+        if (!is(sq, at::kFloat, {c.B, H, Nq}) || !output(*q, a[9], out, o_dtype) || !ws.take(given, abi.int4_bytes(c.B, H, c.Hkv, Nq, c.Nk, c.d, w, sinks), q->device())) return nullptr;
+        const hipStream_t st = stream(dev);
+        const int rc = unlocked(abi.int4, i8(*q), c.k->data_ptr(), c.v->data_ptr(), f32(*sq), f32(*c.sk), f32(*c.sv), c.lengths(), c.B, H, c.Hkv, Nq, c.Nk, c.d, w, sinks, out.data_ptr(), o_dtype, ws.p, ws.bytes, st);
+        return succeeded(rc, "int_flash_attn_fwd_int4") ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
 #define FASTCALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FASTCALL(init), FASTCALL(tokenwise), FASTCALL(headwise), FASTCALL(blockwise), FASTCALL(qkv), FASTCALL(qk), FASTCALL(fwd), FASTCALL(half), FASTCALL(splitk), FASTCALL(window), FASTCALL(prefix), FASTCALL(weights), FASTCALL(evict), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FASTCALL(init), FASTCALL(tokenwise), FASTCALL(headwise), FASTCALL(blockwise), FASTCALL(qkv), FASTCALL(qk), FASTCALL(fwd), FASTCALL(half), FASTCALL(splitk), FASTCALL(window), FASTCALL(prefix), FASTCALL(weights), FASTCALL(evict), FASTCALL(append), FASTCALL(read), FASTCALL(int4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_intfa_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -39,7 +39,7 @@ def test_append(L):
         assert append(L, **bad) == -2, bad
     for bad in (dict(dt=3), dict(dt=-1), dict(held=3), dict(held=-1)):
         assert append(L, **bad) == -3, bad
-    for bad in (dict(d=32), dict(d=256), dict(B=1 << 15, Hkv=1 << 10, Nn=17, Nk=64, d=64), dict(ks=(4, 0, 0)), dict(vs=(0, 0, 12)), dict(ks=(0, 2, 0), dt=0)):
+    for bad in (dict(d=32), dict(d=256), dict(B=1 << 15, Hkv=1 << 10, Nn=9, Nk=64, d=64), dict(ks=(4, 0, 0)), dict(vs=(0, 0, 12)), dict(ks=(0, 2, 0), dt=0)):
         assert append(L, **bad) == -4, bad
     for i, off in ((0, 8), (1, 8), (3, 8), (5, 8), (2, 2), (4, 2), (6, 2)):
         assert append(L, put(i, BASE[i] + off)) == -4, i
@@ -59,7 +59,7 @@ def test_read(L):
         assert read(L, **bad) == -2, bad
     for bad in (dict(dt=3), dict(dt=-1), dict(held=3), dict(held=-1)):
         assert read(L, **bad) == -3, bad
-    for bad in (dict(d=96), dict(B=1 << 15, Hkv=1 << 10, Nk=1, count=17)):
+    for bad in (dict(d=96), dict(B=1 << 15, Hkv=1 << 10, Nk=1, count=9)):
         assert read(L, **bad) == -4, bad
     for i, off in ((0, 8), (2, 8), (5, 8), (6, 8), (1, 2), (3, 2), (4, 2)):
         assert read(L, put(i, BASE[i] + off)) == -4, i
