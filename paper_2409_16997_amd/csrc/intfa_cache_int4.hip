@@ -5,7 +5,8 @@
 //     O = sum w~ (u - 8) / l                v_mfma_f32_16x16x32_f16 (32x32x16 in tiles), fp32 accumulation
 //
 // The scale of a token joins its weight, one multiplication a score, where applied to V it would be one a code.  Then the weights' range is that of p s_V: M follows log2 of the
-// largest |s_V| of the keys at hand, and what fp16 cuts off is small beside the largest summand that could be there.  Scales are expected below 2^64; below 2^-64 they count as that for M alone.
+// largest |s_V| of the keys at hand, and what fp16 cuts off is small beside the largest summand that could be there.  Scales are expected
+// below 2^64; where all are below 2^-80 M stays where that would put it, so that p <= 2^95 and the sum of 2^24 of them is a number.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_bf16.h>
@@ -26,10 +27,67 @@ using namespace ifa_cache;
 constexpr int KEYS4 = 64;                  // keys of a tile
 template <int D> constexpr int ROW4 = D / 2;                 // bytes of a row of codes,
 template <int D> constexpr int TILE4 = KEYS4 * D / 2;        // and of a tile's K or V
-[[maybe_unused]] constexpr float LEAST_SCALE = 0x1p-64f;
+[[maybe_unused]] constexpr float LEAST_SCALE = 0x1p-80f;
 [[maybe_unused]] constexpr float FEW4_BELOW = 15.0f, TILE4_BELOW = 7.0f, SLACK4 = 8.0f;     // the largest weight is 2^15; in tiles 2^7, and 2^15 until M moves
 
+// Sequences of different lengths, which the host does not know: a sequence of t tiles has ceil(t / C) parts, at least one, with C so that there are about `places` parts of all units, which is what the chip
+// holds at once; workgroup w counts its way to its part.  (In as many parts each, the longest sequence decides: 8 x 4 heads, 40 rows on 0 .. 16391 keys 30.2 us, like this 26.3; 16 x 8 heads, one of 16384 keys and 15 of 100 21.2 and 14.4.)  A unit in one part goes straight
+// to O; parts_of[unit] = (its first part, their number).
+struct Sharing {
+    int places;                            // 0: c.splits parts of every unit
+    int2 *parts_of;
+};
+
 #if defined(__HIP_DEVICE_COMPILE__)
+// Sums over the lanes up to each: inside rows of 16, then row by row
+__device__ __forceinline__ int sums_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(sums_up_to(x), 63); }
+struct Part { int unit, split, splits, first; };                 // `first`: of the unit's
+// False: there is no part w
+__device__ __forceinline__ bool part_of(const Call &c, const Sharing &sh, int units, int w, int lane, Part &p) {
+    if (!sh.places) {
+        p.splits = c.splits, p.unit = w / c.splits, p.split = w % c.splits, p.first = p.unit * c.splits;
+        return p.unit < units;
+    }
+    const int span = imin(c.Nk, c.window + c.Nq + c.sinks);      // (window, sinks <= Nk < 2^25, Nq <= 2^26) the keys that some query sees, nearly
+    auto tiles_of = [&](int b) { return b < c.B ? (imin(imax(c.lens[b], 0), span) + KEYS4 - 1) / KEYS4 : 0; };
+    auto parts_of = [&](int t, int C) { return imax(1, (t + C - 1) / C); };
+    int all = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64) all += wave_sum(tiles_of(b0 + lane));
+    // C: whole rounds of the wavefronts; half a part a unit is lost to rounding up, and where it is more C grows
+    const int wanted = imax(1, sh.places - units / 2);
+    int C = imax(1, static_cast<int>((static_cast<unsigned>(all) * static_cast<unsigned>(c.Hkv) / wanted + 3) / 4)) * 4;      // (less than 2^31 tiles: B Hkv Nk d <= 2^40)
+    for (int tries = 0; tries < 4; ++tries) {
+        int n = 0;
+        for (int b0 = 0; b0 < c.B; b0 += 64) n += wave_sum(b0 + lane < c.B ? parts_of(tiles_of(b0 + lane), C) : 0);
+        if (n * c.Hkv <= sh.places) break;
+        C += 4;
+    }
+    int base = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64) {
+        const int n = b0 + lane < c.B ? parts_of(tiles_of(b0 + lane), C) : 0;
+        const int end = base + sums_up_to(n * c.Hkv);
+        const uint64_t past = __ballot(end > w);
+        if (past) {
+            const int at = __ffsll(static_cast<long long>(past)) - 1;
+            p.splits = __builtin_amdgcn_readlane(n, at);
+            const int begin = __builtin_amdgcn_readlane(end, at) - p.splits * c.Hkv, head = (w - begin) / p.splits;
+            p.unit = (b0 + at) * c.Hkv + head, p.split = (w - begin) % p.splits, p.first = begin + head * p.splits;
+            return true;
+        }
+        base = __builtin_amdgcn_readlane(end, 63);
+    }
+    return false;
+}
+
 // 16-byte chunks of a row are exchanged by the row so that what is read at once spreads over the banks.  K is read a row to a lane; V transposed, rows 4 q .. 4 q + 3
 // and those 16 further at once.
 template <int D> __device__ __forceinline__ int k4_slot(int row) { return D == 128 ? (row >> 1) & 3 : (row >> 2) & 1; }
@@ -95,20 +153,18 @@ template <int D, int W, int ST> struct SmemFew4 {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 template <int D, int RT, int W, int ST, bool NT>
-__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, const Call &c, int share, int row0, int units) {
+__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, const Call &c, const Part &part, int share, int row0) {
     constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, KS = D / 64, CT = D / 32;
     constexpr int PER_TILE = 2 * PIECES + 2;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int unit = share / c.splits, split = share % c.splits;
-    if (unit >= units) return;
-    const int last_row = imin(row0 + 16 * RT - 1, c.rows - 1);
+    const int unit = part.unit, last_row = imin(row0 + 16 * RT - 1, c.rows - 1);
     const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
     auto position = [&](int row) { return L - c.Nq + row / c.G; };
     const int p0 = position(row0), p1 = position(last_row);
     const Runs runs(false, 0, c.window, c.sinks, p0, p1);
     const int tilesA = (runs.lenA + KEYS4 - 1) / KEYS4, tiles = tilesA + (runs.lenB + KEYS4 - 1) / KEYS4;
-    const int per = (tiles + c.splits - 1) / c.splits, t0 = split * per, t1 = imin(tiles, t0 + per);
+    const int per = (tiles + part.splits - 1) / part.splits, t0 = part.split * per, t1 = imin(tiles, t0 + per);
 
     const long kA = static_cast<long>(unit) * c.Nk, kB = kA + runs.lo;
     const int8_t *const V = static_cast<const int8_t *>(c.V);
@@ -316,7 +372,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
                 ls = __builtin_fmaf(x[k].y, f, ls);
                 s += *reinterpret_cast<const v4f *>(&sm.o[k][rr][4 * (cc ^ rr)]) * f;
             }
-            if (c.part_o) {
+            if (part.splits > 1) {
                 const long pr = static_cast<long>(share) * c.rows + to;
                 *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = s;
                 if (cc == 0) c.part_ml[pr] = float2{m, ls};
@@ -328,16 +384,79 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
     }
 }
 #endif
-// Two tiles of 16 rows take a key in 1.45 times what one does; the last workgroup of a unit's rows may have one only (8 sequences x 4 heads, 40 rows on up to 16391 keys DRAFT us, with two throughout DRAFT2).
 template <int D, int RT, int W, int ST, bool NT>
-__global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, int units, int row_tiles) {
+__global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, Sharing sh, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemFew4<D, W, ST> sm;
     // the row tiles of one share of the keys run 8 apart: on one XCD
     const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), row0 = 16 * RT * (in8 >> 3);
-    if (RT == 2 && row0 > 0 && row0 + 16 >= c.rows) few4_rows_of_a_unit<D, 1, W, ST, NT>(sm, c, share, row0, units);
-    else few4_rows_of_a_unit<D, RT, W, ST, NT>(sm, c, share, row0, units);
+    Part part;
+    if (!part_of(c, sh, units, share, threadIdx.x & 63, part)) return;
+    if (sh.places && row0 == 0 && part.split == 0 && threadIdx.x == 0) sh.parts_of[part.unit] = int2{part.first, part.splits};
+    few4_rows_of_a_unit<D, RT, W, ST, NT>(sm, c, part, share, row0);
 #endif
+}
+
+// ---- as many parts of a row as its unit has, joined --------------------------------------------------------------------
+// D / 4 threads a row, JOIN4_GROUPS of them taking every such part, with AT_ONCE loads in flight each; then they meet in LDS.
+constexpr int JOIN4_GROUPS = 8;
+template <int D>
+__global__ __launch_bounds__(JOIN4_GROUPS * D / 4) void int4_join_kernel(Call c, Sharing sh) {
+    constexpr int TPR = D / 4, P = JOIN4_GROUPS, AT_ONCE = 4;
+    __shared__ v4f so[P][TPR];
+    __shared__ float2 sml[P];
+    const int unit = blockIdx.x / c.rows, row = blockIdx.x % c.rows, cc = threadIdx.x % TPR, pg = threadIdx.x / TPR;
+    const int2 of = sh.parts_of[unit];
+    const int n = of.y;
+    if (n <= 1) return;                                          // (it is in O already)
+    float m = -INFINITY, l = 0.0f;
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = pg; i0 < n; i0 += AT_ONCE * P) {
+        float2 x[AT_ONCE];
+        v4f y[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = i0 + k * P;
+            x[k] = float2{-INFINITY, 0.0f};
+            y[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i < n) {
+                const long at = static_cast<long>(of.x + i) * c.rows + row;
+                x[k] = c.part_ml[at];
+                y[k] = *reinterpret_cast<const v4f *>(c.part_o + at * D + 4 * cc);
+            }
+        }
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) m_new = fmaxf(m_new, x[k].x);
+        if (m_new == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(m - m_new);       // exp2(-inf) = 0
+        l *= f, s *= f, m = m_new;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float w = __builtin_amdgcn_exp2f(x[k].x - m);
+            l += x[k].y * w;
+            s += y[k] * w;
+        }
+    }
+    so[pg][cc] = s;
+    if (cc == 0) sml[pg] = float2{m, l};
+    __syncthreads();
+    if (pg) return;
+    float m_all = m;
+#pragma unroll
+    for (int k = 1; k < P; ++k) m_all = fmaxf(m_all, sml[k].x);
+    if (m_all != -INFINITY) {
+        const float f = __builtin_amdgcn_exp2f(m - m_all);
+        l *= f, s *= f;
+#pragma unroll
+        for (int k = 1; k < P; ++k) {
+            const float w = __builtin_amdgcn_exp2f(sml[k].x - m_all);
+            l += sml[k].y * w;
+            s += so[k][cc] * w;
+        }
+    }
+    const float q = l > 0.0f ? 1.0f / l : 0.0f;
+    store4(c.O, c.o_dtype, row_of(c, false, unit, row) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
 }
 
 // ---- many rows: tiles of 128 ------------------------------------------------------------------------------------------
@@ -591,15 +710,16 @@ __global__ __launch_bounds__(256, 2) void int4_tile_kernel(Call c, int units, in
 template <int D>
 int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv, row_tiles = static_cast<int>(plan.row_tiles);
-    c.splits = plan.parts;
-    if (plan.parts > 1) {
+    c.splits = static_cast<int>(plan.parts / units);
+    Sharing sh = {plan.places, nullptr};
+    if (plan.parts > units) {
         c.part_o = static_cast<float *>(workspace);
-        c.part_ml = reinterpret_cast<float2 *>(c.part_o + static_cast<long>(units) * plan.parts * c.rows * D);
+        c.part_ml = reinterpret_cast<float2 *>(c.part_o + plan.parts * c.rows * D);
+        sh.parts_of = reinterpret_cast<int2 *>(c.part_ml + plan.parts * c.rows);
     }
     auto few = [&](auto rt, auto waves, auto once) {
         constexpr int W = decltype(waves)::value;
-        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, W, W == 8 ? 2 : 1, decltype(once)::value>), dim3(static_cast<unsigned>((static_cast<long>(units) * plan.parts + 7) / 8 * 8 * row_tiles)),
-                           dim3(64 * W), 0, st, c, units, row_tiles);
+        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, W, W == 8 ? 2 : 1, decltype(once)::value>), dim3(static_cast<unsigned>((plan.parts + 7) / 8 * 8 * row_tiles)), dim3(64 * W), 0, st, c, sh, units, row_tiles);
     };
     auto few_waves = [&](auto rt) {
         constexpr std::integral_constant<int, 4> four{};
@@ -607,18 +727,18 @@ int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
         else if (plan.once) few(rt, four, std::true_type{});
         else few(rt, four, std::false_type{});
     };
-    if (plan.tile)
-        hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(static_cast<long>(units) * row_tiles * plan.parts)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
+    if (plan.tile) hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(plan.parts * row_tiles)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
     else if (plan.rows_at_once == 16) few_waves(std::integral_constant<int, 1>{});
     else few_waves(std::integral_constant<int, 2>{});
-    if (plan.parts > 1) {
-        const Parts parts = {nullptr, c.part_o, nullptr, c.part_ml, 0, plan.parts};
-        const long all_rows = static_cast<long>(units) * c.rows;
+    const long all_rows = static_cast<long>(units) * c.rows;
+    if (plan.places) hipLaunchKernelGGL((int4_join_kernel<D>), dim3(static_cast<unsigned>(all_rows)), dim3(JOIN4_GROUPS * D / 4), 0, st, c, sh);
+    else if (c.splits > 1) {
+        const Parts parts = {nullptr, c.part_o, nullptr, c.part_ml, 0, c.splits};
         auto join = [&](auto p) {
             constexpr int P = decltype(p)::value, ROWS = 1024 / D / P;
             hipLaunchKernelGGL((cache_attention_join_kernel<D, P>), dim3(static_cast<unsigned>((all_rows + ROWS - 1) / ROWS)), dim3(256), 0, st, c, parts, all_rows);
         };
-        if (plan.parts > 8) join(std::integral_constant<int, 8>{});
+        if (c.splits > 8) join(std::integral_constant<int, 8>{});
         else join(std::integral_constant<int, 1>{});
     }
     return hipGetLastError() == hipSuccess ? IFA_OK : IFA_ERR_HIP;

@@ -81,13 +81,17 @@ static inline AttentionPlan attention_plan(int B, int Hkv, int G, int Nq, int Np
 // ---- attention over a cache in 4 bits ------------------------------------------------------------------------
 struct Int4Plan {
     bool tile, once;                       // tiles of 128 rows; K and V past the caches
-    int rows_at_once, waves, parts;        // of a workgroup; parts of the keys of a unit
-    long row_tiles, bytes;                 // of a unit; of workspace
+    int rows_at_once, waves, places;       // of a workgroup; > 0: parts by the sequences' lengths, about that many
+    long row_tiles, parts, bytes;          // of a unit; of all units, at most; of workspace
 };
-#ifndef RP2
-#define RP2 512
-#endif
-static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool ragged) {
+// Tiles of 128 rows, which unpack a key once for all of them but start and end late, from 900 K keys of 32-row tiles on where these are three and a half times as many (us, 32 rows / 128, key heads x rows x keys, d = 128:
+// 64 x 100 x 1000 14.7 / 21.1, x 4000 34.8 / 33.0, x 16000 96 / 85; 16 x 256 x 4000 25.6 / 30.6, x 16000 53.7 / 52.0; 64 x 40 x 16000 56.7 / 74.1; 8 x 1000 causal 13.9 / 21.0, 8 x 2000 30.4 / 30.1).
+//   Otherwise 16 or 32 rows to a workgroup of four wavefronts that take 64 keys each in a round.  A round takes 1.2 us, parts and their join 2.9 us more than none: parts of as few rounds as there are places for two
+// workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 13.0, in four parts 13.8; 256 x 3000 23.3, in two 25.3; 64 x 1100 10.8 and 10.4;
+// 8 x 2200 12.9 and 8.3).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.5, 9.0 in two parts, 8.9 whole; d = 64 6.1, 7.9, 6.9).
+//   With lens, parts by the lengths where that is more than three rounds a part (8 x 8 x up to 2048 10.1 us in as many each, 11.4 counted out), for as many places as registers leave: three workgroups of 16 rows on a
+// CU (16 x 8 x 8191 of 16384 32.3, for two 35.6), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 26.3, for three 33.5).
+static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool lens) {
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
     Int4Plan p = {};
@@ -97,19 +101,22 @@ static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, i
     p.row_tiles = (rows + p.rows_at_once - 1) / p.rows_at_once;
     const long groups = units * p.row_tiles;
     p.waves = 4;
-    p.parts = 1;
-    if (p.tile) p.parts = parts_for(512, groups, keys, 256);
+    p.parts = units;
+    if (p.tile) p.parts = units * parts_for(512, groups, keys, 256);
     else if (groups <= 128 && keys > 320 && keys <= (d == 64 ? 1024 : 896)) p.waves = 8;
     else {
         const long rounds = (keys + 255) / 256;                  // of four wavefronts
-        long parts = (ragged ? (p.rows_at_once == 32 ? RP2 : 768) : 512) / groups;
+        long parts = 512 / groups;
         if (parts > rounds) parts = rounds;
         if (parts > MOST_PARTS) parts = MOST_PARTS;
         const long fewer = parts > 0 ? rounds - (rounds + parts - 1) / parts : 0;
-        if (fewer >= 3 && 64 * fewer >= 3 * groups) p.parts = static_cast<int>(parts);
+        if (fewer >= 3 && 64 * fewer >= 3 * groups) {
+            p.parts = units * parts;
+            if (lens && B > 1 && rounds > 3 * parts) p.places = static_cast<int>((p.rows_at_once == 16 ? 768 : 512) / p.row_tiles), p.parts = units + p.places;
+        }
     }
     p.once = !p.tile && p.row_tiles == 1 && units * keys * (d + 8) > 64L << 20;
-    p.bytes = p.parts > 1 ? units * rows * p.parts * (4L * d + 8) : 0;
+    p.bytes = p.parts > units ? p.parts * rows * (4L * d + 8) + units * 8 : 0;
     return p;
 }
 

@@ -69,6 +69,40 @@ CASES = [
 ]
 
 
+# (long: fp16 out alone)
+LONG = [
+    (1, 2, 8, 3, 700, 128, None, 0, None),               # 24 rows, eight wavefronts
+    (1, 2, 4, 1, 600, 64, None, 0, (555,)),
+    (2, 2, 4, 1, 800, 128, None, 0, (800, 333)),
+    (3, 2, 9, 2, 500, 64, None, 0, (500, 320, 64)),
+    (2, 1, 20, 1, 4000, 64, 3000, 3, (4000, 2222)),      # 20 rows, in parts
+    (1, 3, 4, 1, 20000, 128, None, 0, None),             # more parts than 8
+    (1, 1, 2, 1, 30000, 64, None, 0, (29999,)),
+    (2, 32, 1, 600, 1500, 128, None, 0, (1500, 1111)),   # tiles of 128 rows
+    (1, 4, 1, 512, 9000, 128, None, 0, None),            # ... in parts
+    (2, 40, 1, 700, 900, 64, 700, 5, (900, 640)),
+    (2, 20, 1, 256, 8000, 64, None, 0, (8000, 200)),
+    (36, 2, 4, 64, 64, 128, None, 0, tuple(range(29, 65))),
+]
+# Parts by the lengths: more sequences than lanes, empty ones, one long
+UNEVEN = [
+    (64, 2, 1, 1, 3500, 64, None, 0, tuple((37 * b * b) % 3501 for b in range(64))),
+    (70, 1, 2, 1, 6000, 128, None, 0, tuple(0 if b % 3 else 85 * b for b in range(70))),
+    (16, 4, 3, 1, 7000, 128, None, 0, (7000,) + (100,) * 14 + (1,)),
+    (16, 2, 8, 5, 6500, 64, None, 0, tuple(6500 * b // 15 for b in range(16))),       # 40 rows
+    (24, 2, 20, 1, 9000, 128, 8000, 70, (9000, 8999, 3) + tuple(range(0, 2100, 100))),
+    (12, 8, 4, 1, 5000, 64, None, 0, (0,) * 12),
+]
+
+
+@pytest.mark.parametrize("case", LONG + UNEVEN, ids=[f"long {i}" for i in range(len(LONG))] + [f"uneven {i}" for i in range(len(UNEVEN))])
+def test_long(ifa, case):
+    B, Hkv, G, Nq, Nk, d, w, sinks, lens = case
+    s = ref.problem(11, B, Hkv, G, Nq, Nk, d)
+    want, tol = ref.attention(s, torch.float16, lens, w, sinks)
+    check(int4(ifa, s, w, sinks, lens), want, tol)
+
+
 @pytest.mark.parametrize("out", [torch.float32, torch.float16, torch.bfloat16], ids=str)
 @pytest.mark.parametrize("case", CASES, ids=[f"{i}" for i in range(len(CASES))])
 def test_int4(ifa, case, out):
@@ -76,3 +110,120 @@ def test_int4(ifa, case, out):
     s = ref.problem(7, B, Hkv, G, Nq, Nk, d)
     want, tol = ref.attention(s, out, lens, w, sinks)
     check(int4(ifa, s, w, sinks, lens, out_dtype=out), want, tol)
+
+
+# One of each kernel: few rows whole, in eight wavefronts, in parts, by lengths; tiles
+KINDS = {
+    "whole": (2, 2, 3, 1, 200, 128), "eight wavefronts": (2, 2, 3, 2, 600, 64), "in parts": (2, 2, 4, 2, 3000, 128), "by lengths": (64, 2, 2, 1, 3400, 64), "32 rows": (1, 2, 5, 5, 250, 64),
+    "tiles": (2, 40, 1, 512, 1000, 64), "tiles in parts": (2, 8, 1, 256, 9000, 128)}
+
+
+def of_kind(kind, seed=5):
+    B, Hkv, G, Nq, Nk, d = KINDS[kind]
+    return ref.problem(seed, B, Hkv, G, Nq, Nk, d), [Nk - (b * 13) % (Nk // 2) for b in range(B)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_what_no_query_sees_is_not_looked_at(ifa, kind):
+    """NaN and infinities in the scales behind L_b and, where every query is past it, in front of the window."""
+    s, lens = of_kind(kind)
+    B, Hkv, _, Nk = s["k4"].shape[0], s["k4"].shape[1], 0, s["k4"].shape[2]
+    Nq, w, sinks = s["q8"].shape[2], 100, 3
+    clean, tol = ref.attention(s, torch.float16, lens, w, sinks)
+    for bad in (math.nan, math.inf, -3e38):
+        for b in range(B):
+            hidden = torch.ones(Nk, dtype=torch.bool)
+            hidden[max(0, lens[b] - Nq - w + 1):lens[b]] = False
+            hidden[:sinks] = False
+            s["sk"][b][:, hidden] = bad
+            s["sv"][b][:, hidden] = bad
+        check(int4(ifa, s, w, sinks, lens), clean, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_padding_queries_give_zeros_whatever_they_hold(ifa, kind):
+    s, lens = of_kind(kind)
+    Nq = s["q8"].shape[2]
+    lens[0] = Nq // 2
+    for bad in (0.0, math.nan, math.inf):
+        s["sq"][0, :, :Nq - lens[0]] = bad
+        s["sq"][1:, :, :] = s["sq"][1:, :, :].abs()
+        clean = dict(s, sq=torch.nan_to_num(s["sq"], nan=1.0, posinf=1.0))
+        want, tol = ref.attention(clean, torch.float16, lens)
+        assert not want[0, :, :Nq - lens[0]].any()
+        check(int4(ifa, s, None, 0, lens), want, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_scales(ifa, kind):
+    """s_Q = 0: all keys alike.  s_K of either sign and 0.  s_V of either sign, 0, apart by 2^40, all of them tiny or huge."""
+    s, lens = of_kind(kind)
+    g = torch.Generator().manual_seed(1)
+    sign = torch.randint(0, 2, s["sk"].shape, generator=g) * 2.0 - 1.0
+    zero = torch.rand(s["sk"].shape, generator=g) < 0.1
+    spread = torch.exp2(torch.rand(s["sv"].shape, generator=g) * 20 - 10)
+    one = dict(s, sq=s["sq"].clone(), sk=s["sk"] * sign * ~zero, sv=s["sv"] * sign.flip(2) * ~zero.flip(2) * spread)
+    one["sq"][:, ::2] = 0.0
+    for v in (one, dict(s, sv=s["sv"] * 2.0 ** -70), dict(s, sv=s["sv"] * 2.0 ** 60), dict(s, sv=torch.zeros_like(s["sv"]))):
+        big = v["sv"].abs().max().item() > 1e4
+        out = torch.float32 if big or v["sv"].abs().max().item() < 1e-9 else torch.float16
+        want, tol = ref.attention(v, out, lens)
+        check(int4(ifa, v, None, 0, lens, out_dtype=out), want, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_key_of_all_the_weight_beside_large_values(ifa, kind):
+    """The key that draws all the weight has values 2^-20 of its neighbours': the weights' range follows the products."""
+    s, lens = of_kind(kind)
+    s["k4"][:] = 0x88                                    # codes 0: scores 0
+    s["k4"][:, :, 1] = 0xff                              # ... but for key 1, which every query sees
+    s["q8"][:] = 100
+    s["sq"][:], s["sk"][:] = 1.0, 0.0005                 # score 700 x 64 (128) x .0005 = 22 (45)
+    s["sv"][:] = 1.0
+    s["sv"][:, :, 1] = 2.0 ** -20
+    want, tol = ref.attention(s, torch.float32, lens)
+    check(int4(ifa, s, None, 0, lens, out_dtype=torch.float32), want, tol)
+
+
+def test_a_long_rest_of_small_weights_counts(ifa):
+    """One key 2^20 above all others, which together weigh 1 % of it, and all of the values."""
+    for B, Hkv, Nq, Nk, d in ((1, 1, 1, 12000, 64), (2, 8, 256, 9000, 128)):
+        s = ref.problem(3, B, Hkv, 1, Nq, Nk, d)
+        s["q8"][:], s["k4"][:] = 10, 0x88
+        s["k4"][:, :, 0] = 0x99                          # a score of d 10 s_Q s_K = 20 log 2
+        s["sq"][:], s["sk"][:] = 20 * math.log(2) / (10 * d), 1.0
+        s["sv"][:] = 1.0
+        s["v4"][:] = 0xff
+        s["v4"][:, :, 0] = 0x88
+        want, tol = ref.attention(s, torch.float32)
+        tol = torch.minimum(tol, want.abs() * 0.02)
+        check(int4(ifa, s, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_equal_calls_give_equal_bits(ifa, kind):
+    s, lens = of_kind(kind)
+    a = int4(ifa, s, 150, 2, lens, out_dtype=torch.float32)
+    for _ in range(3):
+        assert torch.equal(a, int4(ifa, s, 150, 2, lens, out_dtype=torch.float32))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_given_outputs_and_workspaces(ifa, kind):
+    """Workspaces hold whatever: of a given size, larger ones, with any bytes in them; outputs of each type."""
+    s, lens = of_kind(kind)
+    t = ref.on_gpu(s)
+    B, H, Nq, d = s["q8"].shape
+    Hkv, Nk = s["k4"].shape[1:3]
+    need = ifa.int4_workspace_bytes(B, H, Hkv, Nq, Nk, d)
+    want = int4(ifa, s, None, 0, lens, out_dtype=torch.bfloat16)
+    for fill in (0, 255):
+        for n in (need, need + 4096):
+            ws = torch.full((max(n, 1),), fill, dtype=torch.uint8, device="cuda")
+            out = torch.full((B, H, Nq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+            call = lambda **kw: ifa.int_flash_attn_fwd_int4(t["q8"], t["k4"], t["v4"], t["sq"], t["sk"], t["sv"], lens=dev_lens(lens), workspace=ws, **kw)  # noqa: E731
+            assert call(out=out) is out and torch.equal(out, want)
+            assert torch.equal(call(out_dtype=torch.bfloat16), want)
+    if need:
+        with pytest.raises(ifa.IntfaError, match="WORKSPACE"):
+            ifa.int_flash_attn_fwd_int4(t["q8"], t["k4"], t["v4"], t["sq"], t["sk"], t["sv"], lens=dev_lens(lens), workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
