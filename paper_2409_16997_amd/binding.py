@@ -597,6 +597,8 @@ def append_keys(K, V, K_c, s_K, V_c, s_V=None, lens=None, hadamard=False):
     if getattr(K, "dim", int)() != 4 or K.shape[2] == 0:
         raise IntfaError("K is [B, Hkv, Nn, d] with at least one token")
     Nn = K.shape[2]
+    if B * Hkv * Nn > 1 << 28:
+        raise IntfaError(f"{Nn} tokens of {B} x {Hkv} heads: at most 2^28 rows")
     (k, ks), (v, vs) = _tokens(K, "K", K.dtype, (B, Hkv, Nn, d), dev), _tokens(V, "V", K.dtype, (B, Hkv, Nn, d), dev)
     _check(lib().append_keys(k, v, _dtype_enum(K), *ks, *vs, at[4], B, Hkv, Nn, Nk, d, held, int(bool(hadamard)), *at[:4], _stream()), "append_keys")
 
@@ -616,8 +618,8 @@ def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=
     if first == -1 and count is None:
         count = Nk
     count = Nk - first if count is None else int(count)
-    if first < -1 or first > Nk or count < 1:
-        raise IntfaError(f"{count} keys from {first} on of {Nk}")
+    if first < -1 or first > Nk or count < 1 or B * Hkv * count > 1 << 28:
+        raise IntfaError(f"{count} keys from {first} on of {Nk} (at least one, and at most 2^28 rows in all)")
     shape = (B, Hkv, count, d)
     if out is None:
         out = tuple(torch.empty(shape, dtype=out_dtype or torch.float16, device=K_c.device) for _ in range(2))
