@@ -1,12 +1,12 @@
 // Attention over a cache held in 4 bits for gfx950: K and V as codes u - 8, u = 0 .. 15, with one fp32 scale a token and head, window and sinks as for the cache in 8 bits.
 //
 //     S = s_Q s_K (sum q u - 8 sum q)       v_mfma_i32_16x16x64_i8 (32x32x32 in tiles), exact in int32: the accumulator starts at -8 sum q
-//     p = exp(S - M),  w~ = fp16(p s_V)     M per row: 15 (tiles: 7 to 15) log2 units below a bound of log2(p s_V), so that |w~| <= 2^15; l = sum p in fp32
+//     w~ = fp16(exp(S - M) |s_V|)           M per row: 15 log2 units below the largest exp(S) |s_V| (tiles: 7 to 15 below a bound of it), so that w~ <= 2^15; l = sum of exp(S - M) in fp32
 //     O = sum w~ (u - 8) / l                v_mfma_f32_16x16x32_f16 (32x32x16 in tiles), fp32 accumulation
 //
-// The scale of a token joins its weight, one multiplication a score, where applied to V it would be one a code.  Then the weights' range is that of p s_V: M follows log2 of the
-// largest |s_V| of the keys at hand, and what fp16 cuts off is small beside the largest summand that could be there.  Scales are expected
-// below 2^64; where all are below 2^-80 M stays where that would put it, so that p <= 2^95 and the sum of 2^24 of them is a number.
+// The scale of a token joins its weight, where applied to V it would cost a multiplication a code.  Then the weights' range is that of p s_V, and what fp16 cuts off is small beside the largest summand.
+// For few rows M is that summand itself, 2^15 exactly: the key that draws most of a row is not rounded at all.  (With a bound in its place single rows were off by up to 2^-11, a decode step of 32 rows by
+// 1.6 times what the rounding of its output leaves.)  Scales are expected below 2^64; below 2^-80 they count as 2^-80 for M and l, so that exp(S - M) <= 2^95 and the sum of 2^24 of them is a number.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_bf16.h>
@@ -145,6 +145,7 @@ template <int D, int W, int ST> struct SmemFew4 {
             alignas(4096) int8_t k[W][ST][TILE4<D>];
             alignas(4096) int8_t v[W][ST][TILE4<D>];
             alignas(256) float sk[W][ST][KEYS4], sv[W][ST][KEYS4];
+            alignas(256) float log_sv[W][KEYS4], inv_sv[W][KEYS4], sign[W][KEYS4];     // of the tile at hand
         };
         float o[W][16][D];                                       // when the loop is over
     };
@@ -176,6 +177,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
     const unsigned gk = crow * ROW + 16 * (cslot ^ k4_slot<D>(crow));
     const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow + 1024 / ROW));
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]), svbuf = (lds_ptr)(&sm.sv[wave][0][0]);
+    const lds_ptr logbuf = (lds_ptr)(&sm.log_sv[wave][0]), invbuf = (lds_ptr)(&sm.inv_sv[wave][0]), signbuf = (lds_ptr)(&sm.sign[wave][0]);
     auto stage = [&](int t, int slot) {                          // (a tile past the last costs as many copies, of nothing)
         const bool inA = t < tilesA;
         const int j0 = KEYS4 * (inA ? t : t - tilesA);
@@ -236,7 +238,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
         memory_fence_of_the_compiler();
         v4i kw[4];                                               // 16 keys each: the bytes of this lane (d = 64: two dwords)
         v2i vw[2][CT];                                           // 32 keys each
-        v4f skv[4], svv[4];
+        v4f skv[4];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
             const lds_ptr at = lds_xor(kbuf + slot * TB + 16 * kb * ROW, 0, k0);
@@ -247,10 +249,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
             }
         }
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            skv[kb] = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 256 + 16 * q + 64 * kb);
-            svv[kb] = *reinterpret_cast<LDS_AS const v4f *>(svbuf + slot * 256 + 16 * q + 64 * kb);
-        }
+        for (int kb = 0; kb < 4; ++kb) skv[kb] = *reinterpret_cast<LDS_AS const v4f *>(skbuf + slot * 256 + 16 * q + 64 * kb);
         const float sv_here = *reinterpret_cast<LDS_AS const float *>(svbuf + slot * 256 + 4 * lane);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -263,7 +262,12 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
         __builtin_amdgcn_sched_barrier(0);
         slot = slot == ST - 1 ? 0 : slot + 1;
 
-        const float below = FEW4_BELOW - scale_bound(sv_here);
+        // log2 |s_V| and 1 / |s_V|, a key to a lane, handed round to the lanes that have the key's scores; a scale of 0 or a negative one also leaves a factor, later
+        const float sv_size = fmaxf(fabsf(sv_here), LEAST_SCALE);
+        *reinterpret_cast<LDS_AS float *>(logbuf + 4 * lane) = __builtin_amdgcn_logf(sv_size);
+        *reinterpret_cast<LDS_AS float *>(invbuf + 4 * lane) = __builtin_amdgcn_rcpf(sv_size);
+        const bool odd = __any(!(sv_here > 0.0f));
+        if (odd) *reinterpret_cast<LDS_AS float *>(signbuf + 4 * lane) = sv_here > 0.0f ? 1.0f : sv_here < 0.0f ? -1.0f : 0.0f;
         v4i kop[4][KS];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
@@ -299,9 +303,15 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
                         if (!(static_cast<uint32_t>(seen >> (32 * (kb >> 1))) & (1u << (16 * (kb & 1) + i)))) a[4 * kb + i] = -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, a[e]);
-            tmax = pair_max(swap16_max(tmax));
-            const float m_new = fmaxf(m2[rt], __builtin_fmaf(tmax, sq2[rt], -below));
+            for (int kb = 0; kb < 4; ++kb) {                     // log2 (p s_V), but for M
+                const v4f ls = *reinterpret_cast<LDS_AS const v4f *>(logbuf + 16 * q + 64 * kb);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    a[4 * kb + i] = __builtin_fmaf(a[4 * kb + i], sq2[rt], ls[i]);
+                    tmax = fmaxf(tmax, a[4 * kb + i]);
+                }
+            }
+            const float m_new = fmaxf(m2[rt], pair_max(swap16_max(tmax)) - FEW4_BELOW);
             const float m_at = m_new == -INFINITY ? 0.0f : m_new;    // a row that has seen nothing yet: weights of 0, no NaN
             const float alpha = __builtin_amdgcn_exp2f(m2[rt] - m_at);   // exp2(-inf) = 0
             m2[rt] = m_new;
@@ -309,17 +319,25 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
             h2 w[8];                                             // keys 0, 2 and 1, 3 of each four: the order of values_of
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
+                const v4f is = *reinterpret_cast<LDS_AS const v4f *>(invbuf + 16 * q + 64 * kb);
                 float x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[4 * kb + i], sq2[rt], -m_at));
-                    psum += e;
-                    x[i] = e * svv[kb][i];
+                    x[i] = __builtin_amdgcn_exp2f(a[4 * kb + i] - m_at);
+                    psum = __builtin_fmaf(x[i], is[i], psum);
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) w[2 * kb + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
             }
             l[rt] = __builtin_fmaf(l[rt], alpha, psum);
+            if (odd) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) {
+                    const v4f f = *reinterpret_cast<LDS_AS const v4f *>(signbuf + 16 * q + 64 * kb);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) w[2 * kb + i] *= h2{(_Float16)f[i], (_Float16)f[i + 2]};
+                }
+            }
             if (__any(alpha != 1.0f)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -328,6 +346,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) pb[rt][h] = h8{w[4 * h][0], w[4 * h][1], w[4 * h + 1][0], w[4 * h + 1][1], w[4 * h + 2][0], w[4 * h + 2][1], w[4 * h + 3][0], w[4 * h + 3][1]};
+            __builtin_amdgcn_sched_barrier(0);                   // (two row tiles between each other take 26 more registers than there are)
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
