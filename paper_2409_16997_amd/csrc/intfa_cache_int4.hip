@@ -637,14 +637,14 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     const auto rK = rsrc(c.K + first_key * ROW, seen_end * ROW), rV = rsrc(static_cast<const int8_t *>(c.V) + first_key * ROW, seen_end * ROW), rSK = rsrc(c.sK + first_key, seen_end * 4),
                rSV = rsrc(c.sV + first_key, seen_end * 4);
     const int piece = D == 128 ? tid : tid & 127, prow = piece / CH, pc = piece % CH;
-    u4 kraw = {}, vraw = {};
+    u4 kraw = {}, vraw = {};                                     // (d = 64: `kraw` of either)
     float sraw = 0.0f;
     auto fetch = [&](int t) {
         const int at = KEYS4 * t;
         auto key = [&](int in) { return at + in + (at + in >= lenA ? gap : 0); };       // (row by row: a block may hold the seam)
         const int from = key(prow) * ROW + 16 * pc;
-        if (D == 128 || wave < 2) kraw = __builtin_amdgcn_raw_buffer_load_b128(rK, from, 0, 0);
-        if (D == 128 || wave >= 2) vraw = __builtin_amdgcn_raw_buffer_load_b128(rV, from, 0, 0);
+        kraw = __builtin_amdgcn_raw_buffer_load_b128(D == 128 || wave < 2 ? rK : rV, from, 0, 0);
+        if constexpr (D == 128) vraw = __builtin_amdgcn_raw_buffer_load_b128(rV, from, 0, 0);
         if (wave < 2) sraw = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(wave == 0 ? rSK : rSV, key(lane) * 4, 0, 0));
     };
     const lds_ptr kbuf = (lds_ptr)(&sm.k[0][0]), vbuf = (lds_ptr)(&sm.v[0][0]), skbuf = (lds_ptr)(&sm.sk[0][0]), svbuf = (lds_ptr)(&sm.sv[0][0]);
@@ -653,7 +653,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     auto unpack = [&](int slot) {
         const lds_ptr k = kbuf + slot * KB + kat, v = vbuf + slot * VB + vat;
         if (D == 128 || wave < 2) unpack_k(kraw, k + 16 * (pc ^ kx), k + 16 * ((pc + D / 32) ^ kx));
-        if (D == 128 || wave >= 2) unpack_v(vraw, masks, v + 64 * ((pc >> 1) ^ vx), v + 64 * (((pc >> 1) + D / 64) ^ vx));
+        if (D == 128 || wave >= 2) unpack_v(D == 128 ? vraw : kraw, masks, v + 64 * ((pc >> 1) ^ vx), v + 64 * (((pc >> 1) + D / 64) ^ vx));
         if (wave < 2) *reinterpret_cast<LDS_AS float *>((wave == 0 ? skbuf : svbuf) + slot * 256 + 4 * lane) = sraw;
     };
     if (t0 < t1) fetch(t0);
@@ -717,8 +717,9 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     else store(__hip_bfloat16{});
 }
 #endif
+// (d = 64: three wavefronts on a SIMD, 32 heads, prompts of 4096 114 -> 102 us; at d = 128 there are 60 registers too few for it, 284 -> 873)
 template <int D>
-__global__ __launch_bounds__(256, 2) void int4_tile_kernel(Call c, int units, int row_tiles, int head_group) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void int4_tile_kernel(Call c, int units, int row_tiles, int head_group) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemTile4<D> sm;
     tile4_of_a_unit<D>(sm, c, blockIdx.x, units, row_tiles, head_group);
