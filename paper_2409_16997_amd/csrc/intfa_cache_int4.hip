@@ -12,6 +12,7 @@
 #include <hip/hip_bf16.h>
 #include <stdint.h>
 #include <type_traits>
+#include <utility>
 
 #include "intfa.h"
 #include "intfa_internal.h"
@@ -132,6 +133,10 @@ __device__ __forceinline__ float wave_max(float x) {
     x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xf, 0xf, true)));
     return pair_max(swap16_max(x));
 }
+// Lane 16 r + N of x in every lane 16 r .. 16 r + 15: an operand modifier of the instruction that takes it.  Scales of keys reach the lanes that hold their scores so, a register for 16 keys; read from LDS, four
+// at a time, they took 128 of the 294 cycles that LDS is busy for 32 rows and 64 keys in tiles (2 x 32 heads, prompts of 4096 284 -> 272 us).
+template <int N> __device__ __forceinline__ float of_row(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x150 + N, 0xf, 0xf, true)); }
+template <typename F, int... I> __device__ __forceinline__ void unrolled(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 // log2 of a bound of |s_V| over the tile, from this lane's key
 __device__ __forceinline__ float scale_bound(float sv) { return __builtin_amdgcn_logf(fmaxf(wave_max(fabsf(sv)), LEAST_SCALE)); }
 #endif
@@ -485,12 +490,14 @@ template <int D> struct SmemTile4 {
     alignas(4096) int8_t k[2][KEYS4 * D];
     alignas(4096) int8_t v[2][KEYS4 * 2 * D];
     alignas(256) float sk[2][KEYS4], sv[2][KEYS4];
+    float sv_log[2];                       // log2 of a bound of |s_V|
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
 template <int D> struct RowState4 {
     float m2, l;                                                 // m2: M
-    v16f o[D / 32];
+    v16f o[D / 32];                                              // channels 1 and 2 of four are exchanged, as V's columns are
+    __device__ __forceinline__ float channel(int dt, int v) const { return o[dt][(v & ~3) | (v & 1) << 1 | (v >> 1 & 1)]; }
 };
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -505,7 +512,7 @@ __device__ __forceinline__ void unpack_v(const u4 &w, const NibbleMasks &m, lds_
         u4 lo, hi;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t a = __builtin_amdgcn_perm(0, w[i + e], 0x0c010c00u), b = __builtin_amdgcn_perm(0, w[i + e], 0x0c030c02u);      // bytes 0, 1 and 2, 3 apart
+            const uint32_t a = w[i + e], b = w[i + e] >> 8;      // channels 0, 2 and 1, 3 of four: columns lie in LDS in this order
             lo[2 * e] = __builtin_bit_cast(uint32_t, low_codes(a, m)), lo[2 * e + 1] = __builtin_bit_cast(uint32_t, low_codes(b, m));
             hi[2 * e] = __builtin_bit_cast(uint32_t, high_codes(a, m)), hi[2 * e + 1] = __builtin_bit_cast(uint32_t, high_codes(b, m));
         }
@@ -516,7 +523,7 @@ __device__ __forceinline__ void unpack_v(const u4 &w, const NibbleMasks &m, lds_
 
 // 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.
 template <int D>
-__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, int lane, const Lane<D, false> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
+__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, float below, int lane, const Lane<D, false> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
                                             const v16i &bias, RowState4<D> &st) {
     constexpr int KS = D / 32, DT = D / 32;
     const int g = lane >> 5;
@@ -531,16 +538,17 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) acc[mt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kop[kk], qf[kk], acc[mt], 0, 0, 0);
     }
-    const float below = TILE4_BELOW - scale_bound(*reinterpret_cast<LDS_AS const float *>(sv + 4 * lane));
+    const unsigned mine = 4 * (8 * (lane >> 2 & 3) + 4 * g + (lane & 3));        // lane 16 x + v: the key whose scores lie in element v of acc[0]
+    float skv[2], svv[2];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+        skv[mt] = *reinterpret_cast<LDS_AS const float *>(sk + mine + 128 * mt);
+        svv[mt] = *reinterpret_cast<LDS_AS const float *>(sv + mine + 128 * mt);
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int vq = 0; vq < 4; ++vq) {
-            const v4f skv = *reinterpret_cast<LDS_AS const v4f *>(sk + 16 * g + 128 * mt + 32 * vq);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[mt][4 * vq + e] = (__int_as_float(acc[mt][4 * vq + e]) - ACC_BIAS_F) * skv[e];
-        }
+        unrolled([&](auto v_) { constexpr int v = decltype(v_)::value; a[mt][v] = (__int_as_float(acc[mt][v]) - ACC_BIAS_F) * of_row<v>(skv[mt]); }, std::make_integer_sequence<int, 16>{});
     if (!clear) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
@@ -569,15 +577,14 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
     const float m = st.m2 == -INFINITY ? 0.0f : st.m2;           // a row that has seen nothing yet: weights of 0, no NaN
     h2 ph[2][8];
     float sum = 0.0f;                                            // of the block: small weights do not meet l one by one
-    auto weights = [&](int mt, int vq) {                         // of 4 keys
-        const v4f svv = *reinterpret_cast<LDS_AS const v4f *>(sv + 16 * g + 128 * mt + 32 * vq);
+    auto weights = [&](int mt, auto vq_) {                      // of 4 keys
+        constexpr int vq = decltype(vq_)::value;
         float x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        unrolled([&](auto i) {
             const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(a[mt][4 * vq + i], sq2, -m));
             sum += e;
-            x[i] = e * svv[i];
-        }
+            x[i] = e * of_row<4 * vq + decltype(i)::value>(svv[mt]);
+        }, std::make_integer_sequence<int, 4>{});
         ph[mt][2 * vq] = h2{(_Float16)x[0], (_Float16)x[1]};
         ph[mt][2 * vq + 1] = h2{(_Float16)x[2], (_Float16)x[3]};
     };
@@ -587,24 +594,19 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int s = 0; s < 2; ++s) vop[dt][s] = v_operand<D, false>(vs, lo.v0, dt, 16 * s);
-#pragma unroll
-    for (int vq = 0; vq < 4; ++vq) weights(0, vq);
+    unrolled([&](auto vq) { weights(0, vq); }, std::make_integer_sequence<int, 4>{});
     __builtin_amdgcn_s_setprio(3);
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
+        unrolled([&](auto dt) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const h8 pb = {ph[mt][4 * s][0], ph[mt][4 * s][1], ph[mt][4 * s + 1][0], ph[mt][4 * s + 1][1], ph[mt][4 * s + 2][0], ph[mt][4 * s + 2][1], ph[mt][4 * s + 3][0], ph[mt][4 * s + 3][1]};
                 st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vop[dt][s], pb, st.o[dt], 0, 0, 0);
                 if (mt == 0) vop[dt][s] = v_operand<D, false>(vs, lo.v0, dt, 32 + 16 * s);
             }
-            if (mt == 0) {
-#pragma unroll
-                for (int q = 0; q < 4 / DT; ++q) weights(1, dt * (4 / DT) + q);
-            }
-        }
+            if (mt == 0) unrolled([&](auto q) { weights(1, std::integral_constant<int, decltype(dt)::value * (4 / DT) + decltype(q)::value>{}); }, std::make_integer_sequence<int, 4 / DT>{});
+        }, std::make_integer_sequence<int, DT>{});
     st.l += sum;
     __builtin_amdgcn_s_setprio(0);
 }
@@ -655,6 +657,10 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
         if (D == 128 || wave < 2) unpack_k(kraw, k + 16 * (pc ^ kx), k + 16 * ((pc + D / 32) ^ kx));
         if (D == 128 || wave >= 2) unpack_v(D == 128 ? vraw : kraw, masks, v + 64 * ((pc >> 1) ^ vx), v + 64 * (((pc >> 1) + D / 64) ^ vx));
         if (wave < 2) *reinterpret_cast<LDS_AS float *>((wave == 0 ? skbuf : svbuf) + slot * 256 + 4 * lane) = sraw;
+        if (wave == 1) {
+            const float bound = scale_bound(sraw);
+            if (lane == 0) sm.sv_log[slot] = bound;
+        }
     };
     if (t0 < t1) fetch(t0);
 
@@ -691,7 +697,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
         const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + KEYS4 - 1 || v0 < sink);
         const bool clear = hi0 >= v0 + KEYS4 - 1 && (hi1 - window < v0 || v0 + KEYS4 <= sink);
         const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
-        if (any) tile4_block<D>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, svbuf + slot * 256, lane, lo, qf, sq2, clear, seen, bias, st);
+        if (any) tile4_block<D>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, svbuf + slot * 256, TILE4_BELOW - sm.sv_log[slot], lane, lo, qf, sq2, clear, seen, bias, st);
         __syncthreads();
     }
 
@@ -701,7 +707,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     if (c.part_o) {
         const long pr = (static_cast<long>(unit) * c.splits + split) * c.rows;
         float *const po = c.part_o + pr * D;
-        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v]; },
+        store_rows<D, float>(stage_out, lane, [&](int dt, int v) { return st.channel(dt, v); },
                              [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(po + static_cast<long>(first + k) * D) : nullptr; });
         if (g == 0 && first + r < c.rows) c.part_ml[pr + first + r] = float2{st.m2, l};
         return;
@@ -709,7 +715,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     const float f = l > 0.0f ? 1.0f / l : 0.0f;                  // a row that sees nothing: zeros
     auto store = [&](auto type) {
         using OutT = decltype(type);
-        store_rows<D, OutT>(stage_out, lane, [&](int dt, int v) { return st.o[dt][v] * f; },
+        store_rows<D, OutT>(stage_out, lane, [&](int dt, int v) { return st.channel(dt, v) * f; },
                             [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(static_cast<OutT *>(c.O) + row_of(c, false, unit, first + k) * D) : nullptr; });
     };
     if (c.o_dtype == IFA_F32) store(float{});
