@@ -6,7 +6,8 @@
 //
 // The scale of a token joins its weight, where applied to V it would cost a multiplication a code.  Then the weights' range is that of p s_V, and what fp16 cuts off is small beside the largest summand.
 // For few rows M is that summand itself, 2^15 exactly: the key that draws most of a row is not rounded at all.  (With a bound in its place single rows were off by up to 2^-11, a decode step of 32 rows by
-// 1.6 times what the rounding of its output leaves.)  Scales are expected below 2^64; below 2^-80 they count as 2^-80 for M and l, so that exp(S - M) <= 2^95 and the sum of 2^24 of them is a number.
+// 1.6 times what the rounding of its output leaves.)  Scales below 2^-80 count as 2^-80 for M and l, so that exp(S - M) <= 2^95 and the sum of 2^24 of them is a number; the largest are below 2^20, so that
+// a weight of 2^-100 of the largest product, or what an M that moves by 100 leaves of l, is still 26 powers of 2 above the smallest normal number.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_bf16.h>

@@ -172,6 +172,20 @@ def test_scales(ifa, kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_scales_at_both_ends_of_their_range(ifa, kind):
+    """s_V just below 2^20 beside 0, beside less than counts and beside 2^-20: the sum of the weights has every key in it, whichever comes first."""
+    s, lens = of_kind(kind)
+    g = torch.Generator().manual_seed(2)
+    ends = torch.tensor([2.0 ** 20 * (1 - 2.0 ** -23), 0.0, 2.0 ** -90, -2.0 ** -20])
+    for turn in (ends, ends.flip(0)[:3]):
+        which = torch.randint(0, len(turn), s["sv"].shape, generator=g)
+        which[:, :, :s["sv"].shape[2] // 2] = len(turn) - 1          # the first half alike, and among the smallest or the largest
+        v = dict(s, sv=turn[which])
+        want, tol = ref.attention(v, torch.float32, lens)
+        check(int4(ifa, v, None, 0, lens, out_dtype=torch.float32), want, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_a_key_of_all_the_weight_beside_large_values(ifa, kind):
     """The key that draws all the weight has values 2^-20 of its neighbours': the weights' range follows the products."""
     s, lens = of_kind(kind)
