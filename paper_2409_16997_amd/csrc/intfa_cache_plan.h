@@ -84,9 +84,12 @@ struct Int4Plan {
     int rows_at_once, waves, places;       // of a workgroup; > 0: parts by the sequences' lengths, about that many
     long row_tiles, parts, bytes;          // of a unit; of all units, at most; of workspace
 };
-// Tiles of 128 rows, which unpack a key once for all of them but start and end late, where these are at most two sevenths as many as tiles of 32, from 192 of them on, and from 900 K keys of 32-row tiles on (us,
-// 32 rows / 128, key heads x rows x keys, d = 128: 192 x 100 x 300 21.3 / 14.0, 128 x 100 x 300 13.3 / 13.7, 128 x 256 x 456 26.6 / 19.1, 64 x 256 x 456 14.3 / 18.1; 64 heads, 1000 queries, window 256 44.6 / 23.8,
-// 32 heads 25.8 / 18.4; 64 x 100 x 4000 34.8 / 33.0, x 16000 96 / 85; 16 x 256 x 4000 25.6 / 30.6, x 16000 53.7 / 52.0; 64 x 40 x 16000 56.7 / 74.1; 8 x 1000 causal 13.9 / 21.0, 8 x 2048 30.8 / 29.3).
+// Tiles of 128 rows, which unpack a key once for all of them but start and end late, where these are at most two sevenths as many as tiles of 32 and those are more than fit the chip at once, two workgroups to a CU,
+// or have more than 900 K keys (us, 32 rows / 128, key heads x rows x keys, d = 128: 160 x 100 x 300 21.2 / 13.5, 128 x 100 x 300 13.4 / 13.5; 80 x 256 x 456 22.0 / 17.9, 64 x 256 x 456 14.5 / 17.2; window 256, 20 heads of 1000
+// queries 22.8 / 16.1, 16 heads 13.5 / 15.4; causal, 9 x 2048 48.2 / 30.5, 8 x 1500 21.4 / 26.2, 4 x 3500 56.4 / 35.2; 64 x 100 x 4000 37.9 / 32.0, 16 x 256 x 4000 25.4 / 28.7, x 16000 54.7 / 51.4; 64 x 40 x 16000 60.9 / 70.9.
+// d = 64: 136 x 100 x 300 15.3 / 10.6, 24 heads of 1000 causal 21.4 / 21.8, 64 x 256 x 1000 14.5 / 20.4).  In full turns also with fewer rows to a tile, on short keys, where a turn of
+// 32-row workgroups is mostly its start and end (400 x 40 x 300 23.9 / 16.5, x 512 24.8 / 21.7, 640 x 64 x 64 25.1 / 13.6, 600 x 80 x 500 43.8 / 35.8; 260 x 64 x 768 24.9 / 28.8, 300 x 96 x 2000 63.5 / 71.5; up to 32 rows: 600 x 32 x 64
+// 15.5 / 11.8, x 300 23.1 / 24.3; 16: 600 x 16 x 64 7.7 / 11.2).
 //   Otherwise 16 or 32 rows to a workgroup of four wavefronts that take 64 keys each in a round.  A round takes 1.2 us, parts and their join 2.9 us more than none: parts of as few rounds as there are places for two
 // workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 13.0, in four parts 13.8; 256 x 3000 23.3, in two 25.3; 64 x 1100 10.8 and 10.4;
 // 8 x 2200 12.9 and 8.3).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.5, 9.0 in two parts, 8.9 whole; d = 64 6.1, 7.9, 6.9).
@@ -97,7 +100,8 @@ static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, i
     const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
     Int4Plan p = {};
     const long few_tiles = row_tiles(true, rows), tiles = row_tiles(false, rows);
-    p.tile = 2 * few_tiles >= 7 * tiles && (units * tiles >= 192 || units * few_tiles * keys > 900L << 10);
+    const bool many = units * few_tiles > 512;
+    p.tile = 2 * few_tiles >= 7 * tiles ? many || units * few_tiles * keys > 900L << 10 : many && rows > 16 && keys <= (rows > 32 ? 512 : 64);
     p.rows_at_once = p.tile ? TILE_ROWS : rows <= 16 ? 16 : 32;
     p.row_tiles = (rows + p.rows_at_once - 1) / p.rows_at_once;
     const long groups = units * p.row_tiles;

@@ -83,6 +83,8 @@ LONG = [
     (2, 40, 1, 700, 900, 64, 700, 5, (900, 640)),
     (2, 20, 1, 256, 8000, 64, None, 0, (8000, 200)),
     (36, 2, 4, 64, 64, 128, None, 0, tuple(range(29, 65))),
+    (150, 4, 1, 20, 40, 128, None, 0, tuple(b % 43 for b in range(150))),                 # ... of few rows, on short keys
+    (90, 3, 3, 15, 300, 64, 100, 2, tuple(3 * b for b in range(90))),
 ]
 # Parts by the lengths: more sequences than lanes, empty ones, one long
 UNEVEN = [

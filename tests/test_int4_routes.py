@@ -50,6 +50,9 @@ def test_the_workspace_of_a_shape_serves_it_with_lengths_and_without():
     (8, 4, 300, 128, (16, 4, "whole")), (8, 4, 700, 128, (16, 8, "whole")), (8, 4, 2200, 128, (16, 4, "in parts")), (64, 4, 1100, 128, (16, 4, "in parts")), (128, 4, 1500, 128, (16, 4, "whole")),
     (256, 4, 3000, 128, (16, 4, "whole")), (8, 4, 700, 64, (16, 8, "whole")), (64, 40, 16000, 128, (32, 4, "in parts")), (64, 100, 1000, 128, (32, 4, "whole")), (64, 100, 16000, 128, ("tiles", True)),
     (16, 256, 4000, 128, (32, 4, "in parts")), (8, 4096, 4096, 128, ("tiles", True)), (16, 4096, 4096, 128, ("tiles", False)),
-    (192, 100, 300, 128, ("tiles", False)), (128, 100, 300, 128, (32, 4, "whole")), (128, 256, 456, 64, ("tiles", False))])
+    (192, 100, 300, 128, ("tiles", False)), (128, 100, 300, 128, (32, 4, "whole")), (128, 256, 456, 64, ("tiles", False)),
+    (160, 100, 300, 128, ("tiles", False)), (80, 256, 456, 128, ("tiles", False)), (64, 256, 456, 128, (32, 4, "whole")), (64, 256, 1000, 64, (32, 4, "whole")),
+    (400, 40, 300, 128, ("tiles", False)), (600, 80, 500, 64, ("tiles", False)), (300, 96, 2000, 128, (32, 4, "whole")), (600, 32, 64, 128, ("tiles", False)), (600, 32, 300, 128, (32, 4, "whole")),
+    (600, 16, 64, 128, (16, 4, "whole"))])
 def test_on_the_faster_side(units, rows, Nk, d, want):
     assert kind(routes.plan(1, units, rows, 1, Nk, d)) == want
