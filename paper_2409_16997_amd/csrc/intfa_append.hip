@@ -13,21 +13,13 @@
 
 #include "intfa.h"
 #include "intfa_internal.h"
+#include "intfa_divisor.h"
 #include "intfa_rows.h"
 
 namespace {
 
 using namespace ifa_rows;
-
-// n / d for n < 2^31 by a multiplication: the quotient's multiplier of 33 bits, the 33rd being the + n
-struct Divisor {
-    unsigned d, m, s;
-    explicit Divisor(unsigned d_) : d(d_), s(0) {
-        while ((1ull << s) < d) ++s;
-        m = static_cast<unsigned>(((1ull << 32) * ((1ull << s) - d)) / d + 1);
-    }
-    __device__ __forceinline__ unsigned of(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
-};
+using ifa::Divisor;
 
 struct Tokens {                            // activations [B, Hkv, Nn, d], rows contiguous
     const void *X;

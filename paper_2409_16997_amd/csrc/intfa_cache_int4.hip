@@ -21,10 +21,12 @@
 #include "intfa_cache.h"
 #include "intfa_cache_plan.h"
 #include "intfa_cache_rows.h"
+#include "intfa_divisor.h"
 
 namespace {
 
 using namespace ifa_cache;
+using ifa::Divisor;
 
 constexpr int KEYS4 = 64;                  // keys of a tile
 template <int D> constexpr int ROW4 = D / 2;                 // bytes of a row of codes,
@@ -40,6 +42,18 @@ struct Sharing {
     int2 *parts_of;
 };
 
+// What indexes are divided by.  (A quotient by a number that comes as an argument takes 30 instructions, one after the other, and the start and end of a workgroup had a dozen: a decode step on 700 keys 6.0 -> 5.8 us,
+// 12 heads of 1777 queries under a window 19.4 -> 19.0.)
+struct Divisors {
+    Divisor G, Hkv, splits, row_tiles8;
+};
+
+// Row `row` of a unit in Q and O (in rows): heads of a unit, and units, follow each other there
+__device__ __forceinline__ long row_of(const Call &c, const Divisors &by, int unit, int row) {
+    const int i = by.G.of(row), g = row - i * c.G;
+    return static_cast<long>(unit) * c.rows + static_cast<long>(g) * c.Nq + i;
+}
+
 #if defined(__HIP_DEVICE_COMPILE__)
 // Sums over the lanes up to each: inside rows of 16, then row by row
 __device__ __forceinline__ int sums_up_to(int x) {
@@ -54,28 +68,30 @@ __device__ __forceinline__ int sums_up_to(int x) {
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(sums_up_to(x), 63); }
 struct Part { int unit, split, splits, first; };                 // `first`: of the unit's
 // False: there is no part w
-__device__ __forceinline__ bool part_of(const Call &c, const Sharing &sh, int units, int w, int lane, Part &p) {
+__device__ __forceinline__ bool part_of(const Call &c, const Sharing &sh, const Divisors &by, int units, int w, int lane, Part &p) {
     if (!sh.places) {
-        p.splits = c.splits, p.unit = w / c.splits, p.split = w % c.splits, p.first = p.unit * c.splits;
+        p.splits = c.splits, p.unit = by.splits.of(w), p.first = p.unit * c.splits, p.split = w - p.first;
         return p.unit < units;
     }
     const int span = imin(c.Nk, c.window + c.Nq + c.sinks);      // (window, sinks <= Nk < 2^25, Nq <= 2^26) the keys that some query sees, nearly
-    auto tiles_of = [&](int b) { return b < c.B ? (imin(imax(c.lens[b], 0), span) + KEYS4 - 1) / KEYS4 : 0; };
+    auto load = [&](int b) { return b < c.B ? (imin(imax(c.lens[b], 0), span) + KEYS4 - 1) / KEYS4 : 0; };
+    const int of_first_64 = load(lane);
+    auto tiles_of = [&](int b0) { return b0 == 0 ? of_first_64 : load(b0 + lane); };
     auto parts_of = [&](int t, int C) { return imax(1, (t + C - 1) / C); };
     int all = 0;
-    for (int b0 = 0; b0 < c.B; b0 += 64) all += wave_sum(tiles_of(b0 + lane));
+    for (int b0 = 0; b0 < c.B; b0 += 64) all += wave_sum(tiles_of(b0));
     // C: whole rounds of the wavefronts; half a part a unit is lost to rounding up, and where it is more C grows
     const int wanted = imax(1, sh.places - units / 2);
     int C = imax(1, static_cast<int>((static_cast<unsigned>(all) * static_cast<unsigned>(c.Hkv) / wanted + 3) / 4)) * 4;      // (less than 2^31 tiles: B Hkv Nk d <= 2^40)
     for (int tries = 0; tries < 4; ++tries) {
         int n = 0;
-        for (int b0 = 0; b0 < c.B; b0 += 64) n += wave_sum(b0 + lane < c.B ? parts_of(tiles_of(b0 + lane), C) : 0);
+        for (int b0 = 0; b0 < c.B; b0 += 64) n += wave_sum(b0 + lane < c.B ? parts_of(tiles_of(b0), C) : 0);
         if (n * c.Hkv <= sh.places) break;
         C += 4;
     }
     int base = 0;
     for (int b0 = 0; b0 < c.B; b0 += 64) {
-        const int n = b0 + lane < c.B ? parts_of(tiles_of(b0 + lane), C) : 0;
+        const int n = b0 + lane < c.B ? parts_of(tiles_of(b0), C) : 0;
         const int end = base + sums_up_to(n * c.Hkv);
         const uint64_t past = __ballot(end > w);
         if (past) {
@@ -145,7 +161,7 @@ __device__ __forceinline__ float scale_bound(float sv) { return __builtin_amdgcn
 // ---- up to 16 RT rows against many keys: every wavefront for itself ----------------------------------------------------
 // As in the kernel for 8 bits, the four wavefronts of a workgroup hold the same rows, take every fourth tile of keys, without a barrier in the loop, and meet once at the end.  A matrix
 // instruction has 16 query columns, so that a decode step's few rows leave fewer of them idle, and all of a lane's softmax work is for keys of its 16 bytes of K.
-template <int D, int W, int ST> struct SmemFew4 {
+template <int D, int RT, int W, int ST> struct SmemFew4 {
     union {
         struct {
             alignas(4096) int8_t k[W][ST][TILE4<D>];
@@ -153,21 +169,21 @@ template <int D, int W, int ST> struct SmemFew4 {
             alignas(256) float sk[W][ST][KEYS4], sv[W][ST][KEYS4];
             alignas(256) float log_sv[W][KEYS4], inv_sv[W][KEYS4], sign[W][KEYS4];     // of the tile at hand
         };
-        float o[W][16][D];                                       // when the loop is over
+        float o[W][16 * RT][D];                                  // when the loop is over
     };
-    float2 ml[W][16];
+    float2 ml[W][16 * RT];
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
 template <int D, int RT, int W, int ST, bool NT>
-__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, const Call &c, const Part &part, int share, int row0) {
+__device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, const Call &c, const Divisors &by, const Part &part, int share, int row0) {
     constexpr int ROW = ROW4<D>, TB = TILE4<D>, PIECES = TB / 1024, KS = D / 64, CT = D / 32;
     constexpr int PER_TILE = 2 * PIECES + 2;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int unit = part.unit, last_row = imin(row0 + 16 * RT - 1, c.rows - 1);
-    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk);
-    auto position = [&](int row) { return L - c.Nq + row / c.G; };
+    const int L = keys_of(c.lens, by.Hkv.of(unit), c.Nk);
+    auto position = [&](int row) { return L - c.Nq + static_cast<int>(by.G.of(row)); };
     const int p0 = position(row0), p1 = position(last_row);
     const Runs runs(false, 0, c.window, c.sinks, p0, p1);
     const int tilesA = (runs.lenA + KEYS4 - 1) / KEYS4, tiles = tilesA + (runs.lenB + KEYS4 - 1) / KEYS4;
@@ -209,7 +225,8 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
     for (int rt = 0; rt < RT; ++rt) {
         const int row = imin(row0 + 16 * rt + r, c.rows - 1);
         p[rt] = position(row);
-        const int8_t *const at = c.Q + row_of(c, false, unit, row) * D;
+        const long qrow = row_of(c, by, unit, row);
+        const int8_t *const at = c.Q + qrow * D;
         if constexpr (D == 128) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) qf[rt][s] = *reinterpret_cast<const v4i *>(at + 64 * s + 16 * q);
@@ -217,7 +234,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
             const v2i a = *reinterpret_cast<const v2i *>(at + 8 * q), b = *reinterpret_cast<const v2i *>(at + 32 + 8 * q);
             qf[rt][0] = v4i{a[0], a[1], b[0], b[1]};
         }
-        sq2[rt] = p[rt] >= 0 ? query_scale(c.sQ[row_of(c, false, unit, row)], qf[rt]) : 1.0f;        // (padding: whatever its scale holds, its row is zeros)
+        sq2[rt] = p[rt] >= 0 ? query_scale(c.sQ[qrow], qf[rt]) : 1.0f;        // (padding: whatever its scale holds, its row is zeros)
         v4i sum = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(v4i{0x01010101, 0x01010101, 0x01010101, 0x01010101}, qf[rt][s], sum, 0, 0, 0);
@@ -370,55 +387,63 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, W, ST> &sm, cons
     wait_all_memory();                                           // requests past the last tile
     __syncthreads();                                             // every wavefront is done with its buffers: o may lie there
 
-    // ---- they meet, 16 rows at a time: M, l and o of each as they are, then whoever has four columns of a row weighs them
+    // ---- they meet: M, l and o of each as they are, then whoever has four columns of a row weighs them.  (All rows at once: 16 by 16, 8 x 4 heads with 40 rows on up to 16391 keys 27.3 -> 26.7 us.)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        if (rt) __syncthreads();
         const float sum = quarters_sum(l[rt]);
-        if (q == 0) sm.ml[wave][r] = float2{m2[rt], sum};
+        if (q == 0) sm.ml[wave][16 * rt + r] = float2{m2[rt], sum};
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)                      // 16-byte chunks, the row's bits mixed into the chunk so that a column of rows spreads over the banks
-                *reinterpret_cast<v4f *>(&sm.o[wave][r][4 * ((D / 8 * h + 4 * ct + q) ^ r)]) = o[rt][h][ct];
-        __syncthreads();
-        const int valid = imin(last_row - row0 - 16 * rt + 1, 16);
-        for (int at = tid; at < valid * (D / 4); at += 64 * W) {
-            const int rr = at / (D / 4), cc = at % (D / 4), to = row0 + 16 * rt + rr;
-            float2 x[W];
-            float m = -INFINITY, ls = 0.0f;
+                *reinterpret_cast<v4f *>(&sm.o[wave][16 * rt + r][4 * ((D / 8 * h + 4 * ct + q) ^ r)]) = o[rt][h][ct];
+    }
+    __syncthreads();
+    const int valid = last_row - row0 + 1;
+    constexpr int N = (RT * 4 * D + 64 * W - 1) / (64 * W);
+    float m[N], ls[N];
+    v4f sum[N];
 #pragma unroll
-            for (int k = 0; k < W; ++k) x[k] = sm.ml[k][rr], m = fmaxf(m, x[k].x);
-            const float m_at = m == -INFINITY ? 0.0f : m;        // (a row that has seen nothing: factors of 0)
-            v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < N; ++n) {                                // (rows past the last are added up, too)
+        const int at = tid + 64 * W * n, rr = imin(at / (D / 4), 16 * RT - 1), cc = at % (D / 4);
+        float2 x[W];
+        m[n] = -INFINITY, ls[n] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
-                const float f = __builtin_amdgcn_exp2f(x[k].x - m_at);
-                ls = __builtin_fmaf(x[k].y, f, ls);
-                s += *reinterpret_cast<const v4f *>(&sm.o[k][rr][4 * (cc ^ rr)]) * f;
-            }
-            if (part.splits > 1) {
-                const long pr = static_cast<long>(share) * c.rows + to;
-                *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = s;
-                if (cc == 0) c.part_ml[pr] = float2{m, ls};
-            } else {
-                const float i = ls > 0.0f ? 1.0f / ls : 0.0f;    // a row that sees nothing: zeros
-                store4(c.O, c.o_dtype, row_of(c, false, unit, to) * D + 4 * cc, s[0] * i, s[1] * i, s[2] * i, s[3] * i);
-            }
+        for (int k = 0; k < W; ++k) x[k] = sm.ml[k][rr], m[n] = fmaxf(m[n], x[k].x);
+        const float m_at = m[n] == -INFINITY ? 0.0f : m[n];      // (a row that has seen nothing: factors of 0)
+        sum[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const float f = __builtin_amdgcn_exp2f(x[k].x - m_at);
+            ls[n] = __builtin_fmaf(x[k].y, f, ls[n]);
+            sum[n] += *reinterpret_cast<const v4f *>(&sm.o[k][rr][4 * (cc ^ (rr & 15))]) * f;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int at = tid + 64 * W * n, rr = at / (D / 4), cc = at % (D / 4), to = row0 + rr;
+        if (rr >= valid) break;
+        if (part.splits > 1) {
+            const long pr = static_cast<long>(share) * c.rows + to;
+            *reinterpret_cast<v4f *>(c.part_o + pr * D + 4 * cc) = sum[n];
+            if (cc == 0) c.part_ml[pr] = float2{m[n], ls[n]};
+        } else {
+            const float i = ls[n] > 0.0f ? 1.0f / ls[n] : 0.0f;  // a row that sees nothing: zeros
+            store4(c.O, c.o_dtype, row_of(c, by, unit, to) * D + 4 * cc, sum[n][0] * i, sum[n][1] * i, sum[n][2] * i, sum[n][3] * i);
         }
     }
 }
 #endif
 template <int D, int RT, int W, int ST, bool NT>
-__global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, Sharing sh, int units, int row_tiles) {
+__global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, Sharing sh, Divisors by, int units, int row_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ SmemFew4<D, W, ST> sm;
+    __shared__ SmemFew4<D, RT, W, ST> sm;
     // the row tiles of one share of the keys run 8 apart: on one XCD
-    const int block = blockIdx.x, in8 = block % (8 * row_tiles), share = block / (8 * row_tiles) * 8 + (in8 & 7), row0 = 16 * RT * (in8 >> 3);
+    const int block = blockIdx.x, eight = by.row_tiles8.of(block), in8 = block - eight * 8 * row_tiles, share = 8 * eight + (in8 & 7), row0 = 16 * RT * (in8 >> 3);
     Part part;
-    if (!part_of(c, sh, units, share, threadIdx.x & 63, part)) return;
+    if (!part_of(c, sh, by, units, share, threadIdx.x & 63, part)) return;
     if (sh.places && row0 == 0 && part.split == 0 && threadIdx.x == 0) sh.parts_of[part.unit] = int2{part.first, part.splits};
-    few4_rows_of_a_unit<D, RT, W, ST, NT>(sm, c, part, share, row0);
+    few4_rows_of_a_unit<D, RT, W, ST, NT>(sm, c, by, part, share, row0);
 #endif
 }
 
@@ -426,11 +451,11 @@ __global__ __launch_bounds__(64 * W, 2) void int4_few_kernel(Call c, Sharing sh,
 // D / 4 threads a row, JOIN4_GROUPS of them taking every such part, with AT_ONCE loads in flight each; then they meet in LDS.
 constexpr int JOIN4_GROUPS = 8;
 template <int D>
-__global__ __launch_bounds__(JOIN4_GROUPS * D / 4) void int4_join_kernel(Call c, Sharing sh) {
+__global__ __launch_bounds__(JOIN4_GROUPS * D / 4) void int4_join_kernel(Call c, Sharing sh, Divisors by) {
     constexpr int TPR = D / 4, P = JOIN4_GROUPS, AT_ONCE = 4;
     __shared__ v4f so[P][TPR];
     __shared__ float2 sml[P];
-    const int unit = blockIdx.x / c.rows, row = blockIdx.x % c.rows, cc = threadIdx.x % TPR, pg = threadIdx.x / TPR;
+    const int unit = blockIdx.y, row = blockIdx.x, cc = threadIdx.x % TPR, pg = threadIdx.x / TPR;
     const int2 of = sh.parts_of[unit];
     const int n = of.y;
     if (n <= 1) return;                                          // (it is in O already)
@@ -481,7 +506,7 @@ __global__ __launch_bounds__(JOIN4_GROUPS * D / 4) void int4_join_kernel(Call c,
         }
     }
     const float q = l > 0.0f ? 1.0f / l : 0.0f;
-    store4(c.O, c.o_dtype, row_of(c, false, unit, row) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
+    store4(c.O, c.o_dtype, row_of(c, by, unit, row) * D + 4 * cc, s[0] * q, s[1] * q, s[2] * q, s[3] * q);
 }
 
 // ---- many rows: tiles of 128 ------------------------------------------------------------------------------------------
@@ -613,16 +638,16 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
 }
 
 template <int D>
-__device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c, int block, int units, int row_tiles, int head_group) {
+__device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c, const Divisors &by, int block, int units, int row_tiles, int head_group) {
     constexpr int ROW = ROW4<D>, KB = KEYS4 * D, VB = KEYS4 * 2 * D, DT = D / 32, CH = ROW / 16;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit, ord;                                               // the row tiles and parts of a unit on one XCD, the last rows, which may see more, first
     map_workgroup(block, units, row_tiles * c.splits, head_group, true, unit, ord);
-    const int rt = row_tiles - 1 - ord / c.splits, split = ord % c.splits;
-    const int L = keys_of(c.lens, unit / c.Hkv, c.Nk), window = c.window;
+    const int tile = by.splits.of(ord), rt = row_tiles - 1 - tile, split = ord - tile * c.splits;
+    const int L = keys_of(c.lens, by.Hkv.of(unit), c.Nk), window = c.window;
     const int row0 = TILE_ROWS * rt, last_row = imin(row0 + TILE_ROWS - 1, c.rows - 1), row = imin(row0 + 32 * wave + r, last_row);
-    auto position = [&](int i) { return L - c.Nq + i / c.G; };
+    auto position = [&](int i) { return L - c.Nq + static_cast<int>(by.G.of(i)); };
     const int pos0 = position(row0), pos1 = position(last_row);
     // The two runs one after the other, cut into blocks of 64 with no seam: key v of them is key v for v < lenA, else key v + gap.  All of it lies in front of key pos1 + 1.
     const Runs runs(false, 0, window, c.sinks, pos0, pos1);
@@ -665,7 +690,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     };
     if (t0 < t1) fetch(t0);
 
-    const long qrow = row_of(c, false, unit, row);
+    const long qrow = row_of(c, by, unit, row);
     v4i qf[DT];
 #pragma unroll
     for (int kk = 0; kk < DT; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
@@ -717,7 +742,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     auto store = [&](auto type) {
         using OutT = decltype(type);
         store_rows<D, OutT>(stage_out, lane, [&](int dt, int v) { return st.channel(dt, v) * f; },
-                            [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(static_cast<OutT *>(c.O) + row_of(c, false, unit, first + k) * D) : nullptr; });
+                            [&](int k) { return first + k < c.rows ? reinterpret_cast<char *>(static_cast<OutT *>(c.O) + row_of(c, by, unit, first + k) * D) : nullptr; });
     };
     if (c.o_dtype == IFA_F32) store(float{});
     else if (c.o_dtype == IFA_F16) store(__half{});
@@ -726,10 +751,10 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
 #endif
 // (d = 64: three wavefronts on a SIMD, 32 heads, prompts of 4096 114 -> 102 us; at d = 128 there are 60 registers too few for it, 284 -> 873)
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void int4_tile_kernel(Call c, int units, int row_tiles, int head_group) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void int4_tile_kernel(Call c, Divisors by, int units, int row_tiles, int head_group) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ SmemTile4<D> sm;
-    tile4_of_a_unit<D>(sm, c, blockIdx.x, units, row_tiles, head_group);
+    tile4_of_a_unit<D>(sm, c, by, blockIdx.x, units, row_tiles, head_group);
 #endif
 }
 
@@ -739,6 +764,7 @@ int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
     const int units = c.B * c.Hkv, row_tiles = static_cast<int>(plan.row_tiles);
     c.splits = static_cast<int>(plan.parts / units);
     Sharing sh = {plan.places, nullptr};
+    const Divisors by = {Divisor(c.G), Divisor(c.Hkv), Divisor(c.splits), Divisor(8 * row_tiles)};
     if (plan.parts > units) {
         c.part_o = static_cast<float *>(workspace);
         c.part_ml = reinterpret_cast<float2 *>(c.part_o + plan.parts * c.rows * D);
@@ -746,7 +772,7 @@ int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
     }
     auto few = [&](auto rt, auto waves, auto once) {
         constexpr int W = decltype(waves)::value;
-        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, W, W == 8 ? 2 : 1, decltype(once)::value>), dim3(static_cast<unsigned>((plan.parts + 7) / 8 * 8 * row_tiles)), dim3(64 * W), 0, st, c, sh, units, row_tiles);
+        hipLaunchKernelGGL((int4_few_kernel<D, decltype(rt)::value, W, W == 8 ? 2 : 1, decltype(once)::value>), dim3(static_cast<unsigned>((plan.parts + 7) / 8 * 8 * row_tiles)), dim3(64 * W), 0, st, c, sh, by, units, row_tiles);
     };
     auto few_waves = [&](auto rt) {
         constexpr std::integral_constant<int, 4> four{};
@@ -754,11 +780,11 @@ int launch(Call c, const Int4Plan &plan, void *workspace, hipStream_t st) {
         else if (plan.once) few(rt, four, std::true_type{});
         else few(rt, four, std::false_type{});
     };
-    if (plan.tile) hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(plan.parts * row_tiles)), dim3(256), 0, st, c, units, row_tiles, head_group_for(true, 0, 0));
+    if (plan.tile) hipLaunchKernelGGL((int4_tile_kernel<D>), dim3(static_cast<unsigned>(plan.parts * row_tiles)), dim3(256), 0, st, c, by, units, row_tiles, head_group_for(true, 0, 0));
     else if (plan.rows_at_once == 16) few_waves(std::integral_constant<int, 1>{});
     else few_waves(std::integral_constant<int, 2>{});
     const long all_rows = static_cast<long>(units) * c.rows;
-    if (plan.places) hipLaunchKernelGGL((int4_join_kernel<D>), dim3(static_cast<unsigned>(all_rows)), dim3(JOIN4_GROUPS * D / 4), 0, st, c, sh);
+    if (plan.places) hipLaunchKernelGGL((int4_join_kernel<D>), dim3(static_cast<unsigned>(c.rows), static_cast<unsigned>(units)), dim3(JOIN4_GROUPS * D / 4), 0, st, c, sh, by);
     else if (c.splits > 1) {
         const Parts parts = {nullptr, c.part_o, nullptr, c.part_ml, 0, c.splits};
         auto join = [&](auto p) {
