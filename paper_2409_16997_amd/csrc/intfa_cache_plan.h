@@ -85,16 +85,16 @@ struct Int4Plan {
     long row_tiles, parts, bytes;          // of a unit; of all units, at most; of workspace
 };
 // Tiles of 128 rows, which unpack a key once for all of them but start and end late, where these are at most two sevenths as many as tiles of 32 and those are more than fit the chip at once, two workgroups to a CU,
-// or have more than 900 K keys (us, 32 rows / 128, key heads x rows x keys, d = 128: 160 x 100 x 300 21.2 / 13.5, 128 x 100 x 300 13.4 / 13.5; 80 x 256 x 456 22.0 / 17.9, 64 x 256 x 456 14.5 / 17.2; window 256, 20 heads of 1000
-// queries 22.8 / 16.1, 16 heads 13.5 / 15.4; causal, 9 x 2048 48.2 / 30.5, 8 x 1500 21.4 / 26.2, 4 x 3500 56.4 / 35.2; 64 x 100 x 4000 37.9 / 32.0, 16 x 256 x 4000 25.4 / 28.7, x 16000 54.7 / 51.4; 64 x 40 x 16000 60.9 / 70.9.
-// d = 64: 136 x 100 x 300 15.3 / 10.6, 24 heads of 1000 causal 21.4 / 21.8, 64 x 256 x 1000 14.5 / 20.4).  In full turns also with fewer rows to a tile, on short keys, where a turn of
-// 32-row workgroups is mostly its start and end (400 x 40 x 300 23.9 / 16.5, x 512 24.8 / 21.7, 640 x 64 x 64 25.1 / 13.6, 600 x 80 x 500 43.8 / 35.8; 260 x 64 x 768 24.9 / 28.8, 300 x 96 x 2000 63.5 / 71.5; up to 32 rows: 600 x 32 x 64
-// 15.5 / 11.8, x 300 23.1 / 24.3; 16: 600 x 16 x 64 7.7 / 11.2).
+// or have more than 900 K keys (us, 32 rows / 128, key heads x rows x keys, d = 128: 160 x 100 x 300 20.2 / 13.3, 128 x 100 x 300 13.3 / 12.8; 80 x 256 x 456 20.5 / 18.0, 64 x 256 x 456 14.6 / 17.3; window 256, 20 heads of 1000
+// queries 21.0 / 15.4, 16 heads 13.1 / 15.1; causal, 9 x 2048 48.0 / 31.0, 8 x 1500 20.7 / 25.9, 4 x 3500 56.9 / 35.5; 64 x 100 x 4000 37.8 / 32.2, 16 x 256 x 4000 25.9 / 29.3, x 16000 56.5 / 50.1; 64 x 40 x 16000 61.8 / 71.0.
+// d = 64: 136 x 100 x 300 13.9 / 10.2, 24 heads of 1000 causal 20.4 / 21.9, 64 x 256 x 1000 14.6 / 21.0).  In full turns also with fewer rows to a tile, on short keys, where a turn of 32-row workgroups is mostly its start and end
+// (400 x 40 x 300 22.7 / 16.1, x 512 23.8 / 21.1, 640 x 64 x 64 23.1 / 12.8, 600 x 80 x 500 42.7 / 35.8; 260 x 64 x 768 23.9 / 28.3, 300 x 96 x 2000 59.9 / 69.8; up to 32 rows: 600 x 32 x 64 13.9 / 10.7, x 300 21.8 / 23.4;
+// 16: 600 x 16 x 64 7.5 / 10.7).
 //   Otherwise 16 or 32 rows to a workgroup of four wavefronts that take 64 keys each in a round.  A round takes 1.2 us, parts and their join 2.9 us more than none: parts of as few rounds as there are places for two
-// workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 13.0, in four parts 13.8; 256 x 3000 23.3, in two 25.3; 64 x 1100 10.8 and 10.4;
-// 8 x 2200 12.9 and 8.3).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.5, 9.0 in two parts, 8.9 whole; d = 64 6.1, 7.9, 6.9).
+// workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 13.2, in four parts 13.8; 256 x 3000 23.7, in two 25.6; 64 x 1100 11.0 and, in three, 10.1;
+// 8 x 2200 15.3 and, in eight, 9.6).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.3, 8.9 in two parts, 7.9 whole; d = 64 6.0, 7.8, 6.5).
 //   With lens, parts by the lengths where that is more than three rounds a part (8 x 8 x up to 2048 10.1 us in as many each, 11.4 counted out), for as many places as registers leave: three workgroups of 16 rows on a
-// CU (16 x 8 x 8191 of 16384 32.3, for two 35.6), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 26.3, for three 33.5).
+// CU (16 x 8 x 8191 of 16384 33.3, in as many each 35.6), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 26.7, in as many each 31.8, for three 33.5).
 static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool lens) {
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
