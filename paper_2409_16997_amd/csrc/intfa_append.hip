@@ -135,14 +135,17 @@ __global__ __launch_bounds__(THREADS) void append_keys_kernel(AppendCall c) {
 }
 
 // ---- read ---------------------------------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ void store8(void *to, long at, const float (&x)[8]) {
+// Values in fp32 are 32 bytes of a lane's 8 channels, and a store of 16 of them would leave every other 16 bytes to the next: there lane `sub` has channels 4 sub .. and d/2 + 4 sub .. instead, so that a row's lanes
+// store 128 or 256 bytes without a gap (4 x 8 heads x 8000 of 128 numbers from 4 bits 105 -> 44 us, 36 x 1777 of 64 from 8 bits, rotated, 12.5 -> 7.7).
+template <typename T> constexpr bool HALVES = std::is_same_v<T, float>;
+template <typename T, int LPR> __device__ __forceinline__ void store_row(void *to, long row, int sub, const float (&x)[8]) {
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
     typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-    if constexpr (std::is_same_v<T, float>) {
-        u4 *const p = reinterpret_cast<u4 *>(static_cast<float *>(to) + at);
+    if constexpr (HALVES<T>) {
+        u4 *const p = reinterpret_cast<u4 *>(static_cast<float *>(to) + row * (8 * LPR)) + sub;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            __builtin_nontemporal_store(u4{__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]), __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])}, p + h);
+            __builtin_nontemporal_store(u4{__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]), __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])}, p + h * LPR);
     } else {
         u4 w;
 #pragma unroll
@@ -150,8 +153,26 @@ template <typename T> __device__ __forceinline__ void store8(void *to, long at, 
             if constexpr (std::is_same_v<T, __half>) w[e] = __builtin_bit_cast(uint32_t, __floats2half2_rn(x[2 * e], x[2 * e + 1]));
             else w[e] = __builtin_bit_cast(uint32_t, bf2{static_cast<__bf16>(x[2 * e]), static_cast<__bf16>(x[2 * e + 1])});
         }
-        __builtin_nontemporal_store(w, reinterpret_cast<u4 *>(static_cast<T *>(to) + at));
+        __builtin_nontemporal_store(w, reinterpret_cast<u4 *>(static_cast<T *>(to) + row * (8 * LPR)) + sub);
     }
+}
+// hadamard_row for channels 4 sub .. and d/2 + 4 sub ..: the same sums in the same order
+template <int LPR> __device__ __forceinline__ void hadamard_halves(float (&x)[8], int sub) {
+    auto inside = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((i & h) == 0) {
+                const float a = x[i], b = x[i + h];
+                x[i] = a + b;
+                x[i + h] = a - b;
+            }
+    };
+    inside(1), inside(2);
+    hadamard_lane_stage<1, LPR>(x, sub);
+    hadamard_lane_stage<2, LPR>(x, sub);
+    hadamard_lane_stage<4, LPR>(x, sub);
+    hadamard_lane_stage<8, LPR>(x, sub);
+    inside(4);
 }
 // (u - 8) s of four nibbles, one a byte
 __device__ __forceinline__ void values4(uint32_t w, float s, float *x) {
@@ -166,7 +187,7 @@ __device__ __forceinline__ void values8(uint32_t w, float s, float *x) {
 template <typename T, int LPR, int HELD, bool HADAMARD, int AT_ONCE>
 __global__ __launch_bounds__(THREADS) void read_keys_kernel(ReadCall c) {
     constexpr int ROWS = THREADS / LPR, D = 8 * LPR;
-    constexpr bool I4 = HELD == IFA_CACHE_I4, VF16 = HELD == IFA_CACHE_I8_F16;
+    constexpr bool I4 = HELD == IFA_CACHE_I4, VF16 = HELD == IFA_CACHE_I8_F16, HALF = HALVES<T>;
     const int sub = threadIdx.x % LPR;
     const unsigned row0 = blockIdx.x * (ROWS * AT_ONCE) + threadIdx.x / LPR;
     uint2 k[AT_ONCE];
@@ -183,24 +204,37 @@ __global__ __launch_bounds__(THREADS) void read_keys_kernel(ReadCall c) {
         there[i] = p >= 0 && p < L;
         if (!there[i]) continue;
         const long slot = static_cast<long>(u) * c.Nk + p;
-        const long at = I4 ? slot * (D / 2) + 8 * (sub & (LPR / 2 - 1)) : slot * D + 8 * sub;
-        k[i] = *reinterpret_cast<const uint2 *>(c.Kc + at);
-        sk[i] = c.sK[slot];
-        if constexpr (VF16) v[i].load(c.Vc, at);
-        else {
-            v[i] = *reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(c.Vc) + at);
-            sv[i] = c.sV[I4 ? slot : u];
+        const int8_t *const V = static_cast<const int8_t *>(c.Vc);
+        if constexpr (HALF) {                                    // bytes of the two halves; in 4 bits both are in the same four
+            auto codes = [&](const int8_t *p) {
+                const uint32_t *const row = reinterpret_cast<const uint32_t *>(p + slot * (I4 ? D / 2 : D)) + sub;
+                if constexpr (I4) return make_uint2(row[0], row[0] >> 4);
+                else return make_uint2(row[0], row[LPR]);
+            };
+            k[i] = codes(c.Kc);
+            sk[i] = c.sK[slot];
+            if constexpr (VF16) {
+                const uint2 *const row = reinterpret_cast<const uint2 *>(V + slot * (2 * D)) + sub;
+                const uint2 a = row[0], b = row[LPR];
+                v[i].raw = make_uint4(a.x, a.y, b.x, b.y);
+            } else v[i] = codes(V);
+        } else {
+            const long at = I4 ? slot * (D / 2) + 8 * (sub & (LPR / 2 - 1)) : slot * D + 8 * sub;
+            k[i] = *reinterpret_cast<const uint2 *>(c.Kc + at);
+            sk[i] = c.sK[slot];
+            if constexpr (VF16) v[i].load(c.Vc, at);
+            else v[i] = *reinterpret_cast<const uint2 *>(V + at);
         }
+        if constexpr (!VF16) sv[i] = c.sV[I4 ? slot : u];
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
         const unsigned r = row0 + i * ROWS;
         if (r >= c.rows) continue;
-        const long to = static_cast<long>(r) * D + 8 * sub;
         float x[8] = {}, y[8] = {};
         if (there[i]) {
             if constexpr (I4) {
-                const int up = sub >= LPR / 2 ? 4 : 0;           // which nibble of the bytes
+                const int up = !HALF && sub >= LPR / 2 ? 4 : 0;        // which nibble of the bytes
                 values4(k[i].x >> up & 0x0f0f0f0fu, sk[i], x), values4(k[i].y >> up & 0x0f0f0f0fu, sk[i], x + 4);
                 values4(v[i].x >> up & 0x0f0f0f0fu, sv[i], y), values4(v[i].y >> up & 0x0f0f0f0fu, sv[i], y + 4);
             } else {
@@ -210,18 +244,19 @@ __global__ __launch_bounds__(THREADS) void read_keys_kernel(ReadCall c) {
             }
         }
         if constexpr (HADAMARD) {                                // H H = d I, 1 / d is exact
-            hadamard_row<LPR>(x, sub);
+            if constexpr (HALF) hadamard_halves<LPR>(x, sub);
+            else hadamard_row<LPR>(x, sub);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= 1.0f / D;
         }
-        store8<T>(c.K, to, x);
-        store8<T>(c.V, to, y);
+        store_row<T, LPR>(c.K, r, sub, x);
+        store_row<T, LPR>(c.V, r, sub, y);
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
-// Rows of a thread: one for the first 8192 workgroups' worth, then two, which saves divisions (us with one, two, four everywhere: 5331 x 12 rows of 64 fp32 numbers, rotated, into 8 bits and back 17.8, 20.0,
-// 22.8; 32768 x 8 of 128 bf16 numbers into 4 bits and back 61.0, 60.6, 63.7; 16 x 8 x 16384 read from 4 bits 247, 236, 240).
+// Rows of a thread: one for the first 8192 workgroups' worth, then two, which saves divisions (us with one, two, four everywhere: 5331 x 12 rows of 64 fp32 numbers, rotated, into 8 bits and back 14.4, 15.4,
+// 17.8; 32768 x 8 of 128 bf16 numbers into 4 bits and back 60.9, 60.9, 63.7; 16 x 8 x 16384 read from 4 bits 241, 236, 247).
 constexpr int MANY = 2;
 template <typename F> void by_rows(long rows, int lpr, F f) {
     const long per = THREADS / lpr, one = (rows + per - 1) / per;
