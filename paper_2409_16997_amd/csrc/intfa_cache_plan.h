@@ -92,7 +92,7 @@ struct Int4Plan {
 // 16: 600 x 16 x 64 7.5 / 10.7).
 //   Otherwise 16 or 32 rows to a workgroup of four wavefronts that take 64 keys each in a round.  A round takes 1.2 us, parts and their join 2.9 us more than none: parts of as few rounds as there are places for two
 // workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 13.2, in four parts 13.8; 256 x 3000 23.7, in two 25.6; 64 x 1100 11.0 and, in three, 10.1;
-// 8 x 2200 15.3 and, in eight, 9.6).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.3, 8.9 in two parts, 7.9 whole; d = 64 6.0, 7.8, 6.5).
+// 8 x 2200 15.3 and, in eight, 9.6).  Up to 64 parts, or 128 where that is one workgroup on a CU (1 x 200000 25.1 and 19.5, 2 x 131072 19.8 and 16.9, 1 x 40000 11.8 both; 4 x 94150 17.5 and 18.7).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 7.3, 8.9 in two parts, 7.9 whole; d = 64 6.0, 7.8, 6.5).
 //   With lens, parts by the lengths where that is more than three rounds a part (8 x 8 x up to 2048 10.1 us in as many each, 11.4 counted out), for as many places as registers leave: three workgroups of 16 rows on a
 // CU (16 x 8 x 8191 of 16384 33.3, in as many each 35.6), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 26.7, in as many each 31.8, for three 33.5).
 static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool lens) {
@@ -113,7 +113,8 @@ static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, i
         const long rounds = (keys + 255) / 256;                  // of four wavefronts
         long parts = 512 / groups;
         if (parts > rounds) parts = rounds;
-        if (parts > MOST_PARTS) parts = MOST_PARTS;
+        const long most = groups <= 2 ? 2 * MOST_PARTS : MOST_PARTS;
+        if (parts > most) parts = most;
         const long fewer = parts > 0 ? rounds - (rounds + parts - 1) / parts : 0;
         if (fewer >= 3 && 64 * fewer >= 3 * groups) {
             p.parts = units * parts;

@@ -46,6 +46,12 @@ def test_the_workspace_of_a_shape_serves_it_with_lengths_and_without():
         assert with_lens["places"] == 0 or with_lens["parts"] == B * Hkv + with_lens["places"]
 
 
+def test_how_many_parts():
+    """Up to 64 a unit, 128 where there are one or two groups of rows; a case of the GPU tests has more than 64."""
+    assert [routes.plan(1, u, 1, 1, 200000, 128)["splits"] for u in (1, 2, 3, 8, 32)] == [128, 128, 64, 64, 16]
+    assert max(of(c)["splits"] for c in tests.LONG) > 64
+
+
 @pytest.mark.parametrize("units,rows,Nk,d,want", [
     (8, 4, 300, 128, (16, 4, "whole")), (8, 4, 700, 128, (16, 8, "whole")), (8, 4, 2200, 128, (16, 4, "in parts")), (64, 4, 1100, 128, (16, 4, "in parts")), (128, 4, 1500, 128, (16, 4, "whole")),
     (256, 4, 3000, 128, (16, 4, "whole")), (8, 4, 700, 64, (16, 8, "whole")), (64, 40, 16000, 128, (32, 4, "in parts")), (64, 100, 1000, 128, (32, 4, "whole")), (64, 100, 16000, 128, ("tiles", True)),
