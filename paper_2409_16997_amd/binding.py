@@ -639,7 +639,7 @@ def int4_workspace_bytes(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: int, win
 
 def int_flash_attn_fwd_int4(Q_i8, K_i4, V_i4, s_Q, s_K, s_V, window=None, sinks=0, lens=None, out_dtype=None, out=None, workspace=None):
     """Attention over a cache in 4 bits, as append_keys writes it: int8 Q [B, H, Nq, d] (H a multiple of Hkv) with s_Q [B, H, Nq], uint8 K, V [B, Hkv, Nk, d / 2] with s_K, s_V [B, Hkv, Nk].
-    Queries, lens, window (None: every key up to the query's own) and sinks as in int_flash_attn_fwd_window.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).
+    |s_V| < 2^20.  Queries, lens, window (None: every key up to the query's own) and sinks as in int_flash_attn_fwd_window.  Returns O [B, H, Nq, d] (fp16 unless out_dtype/out says otherwise).
     `workspace`: a uint8 device tensor of int4_workspace_bytes(...) bytes (allocated here if not given)."""
     if out is None:
         r = (_native or _load_native()).int4(Q_i8, K_i4, V_i4, s_Q, s_K, s_V, window, sinks, lens, out_dtype, workspace)

@@ -749,7 +749,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     else store(__hip_bfloat16{});
 }
 #endif
-// (d = 64: three wavefronts on a SIMD, 32 heads, prompts of 4096 114 -> 102 us; at d = 128 there are 60 registers too few for it, 284 -> 873)
+// (d = 64: three wavefronts fit a SIMD, which took 32 heads, prompts of 4096 from 114 us to 102, with the scales as lane modifiers 96; at d = 128 there are 52 registers too few for it, 279 -> 700)
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void int4_tile_kernel(Call c, Divisors by, int units, int row_tiles, int head_group) {
 #if defined(__HIP_DEVICE_COMPILE__)
