@@ -200,18 +200,18 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
     const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow + 1024 / ROW));
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]), svbuf = (lds_ptr)(&sm.sv[wave][0][0]);
     const lds_ptr logbuf = (lds_ptr)(&sm.log_sv[wave][0]), invbuf = (lds_ptr)(&sm.inv_sv[wave][0]), signbuf = (lds_ptr)(&sm.sign[wave][0]);
-    auto stage = [&](int t, int slot) {                          // (a tile past the last costs as many copies, of nothing)
+    auto stage = [&](int t, int slot) {
         const bool inA = t < tilesA;
         const int j0 = KEYS4 * (inA ? t : t - tilesA);
-        const bool real = t < t1;
-        copy_pieces<PIECES, NT>(pick(inA, rKA, rKB), kbuf + slot * TB, gk, gk, real ? j0 * ROW : NOTHING);
-        copy_pieces<PIECES, NT>(pick(inA, rVA, rVB), vbuf + slot * TB, gv0, gv1, real ? j0 * ROW : NOTHING);
-        lds_copy4(pick(inA, rSKA, rSKB), skbuf + slot * 256, 4 * lane, real ? j0 * 4 : NOTHING);
-        lds_copy4(pick(inA, rSVA, rSVB), svbuf + slot * 256, 4 * lane, real ? j0 * 4 : NOTHING);
+        copy_pieces<PIECES, NT>(pick(inA, rKA, rKB), kbuf + slot * TB, gk, gk, j0 * ROW);
+        copy_pieces<PIECES, NT>(pick(inA, rVA, rVB), vbuf + slot * TB, gv0, gv1, j0 * ROW);
+        lds_copy4(pick(inA, rSKA, rSKB), skbuf + slot * 256, 4 * lane, j0 * 4);
+        lds_copy4(pick(inA, rSVA, rSVB), svbuf + slot * 256, 4 * lane, j0 * 4);
     };
     const int first = t0 + wave;
 #pragma unroll
-    for (int s = 0; s < ST; ++s) stage(first + s * W, s);
+    for (int s = 0; s < ST; ++s)
+        if (first + s * W < t1) stage(first + s * W, s);
 
     // where this lane reads K (key r of 16; the 16 bytes, at d = 64 8 bytes, of quarter q) and V (row i / 2 of the 8 that are transposed, half i & 1 of 16 columns)
     const unsigned k0 = D == 128 ? r * ROW + 16 * (q ^ k4_slot<D>(r)) : r * ROW + 16 * ((q >> 1) ^ k4_slot<D>(r)) + 8 * (q & 1);
@@ -234,7 +234,11 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
             const v2i a = *reinterpret_cast<const v2i *>(at + 8 * q), b = *reinterpret_cast<const v2i *>(at + 32 + 8 * q);
             qf[rt][0] = v4i{a[0], a[1], b[0], b[1]};
         }
-        sq2[rt] = p[rt] >= 0 ? query_scale(c.sQ[qrow], qf[rt]) : 1.0f;        // (padding: whatever its scale holds, its row is zeros)
+        sq2[rt] = c.sQ[qrow];
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        sq2[rt] = query_scale(p[rt] >= 0 ? sq2[rt] : 1.0f, qf[rt]);      // (padding: whatever its scale holds, its row is zeros)
         v4i sum = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(v4i{0x01010101, 0x01010101, 0x01010101, 0x01010101}, qf[rt][s], sum, 0, 0, 0);
@@ -256,7 +260,8 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
     const NibbleMasks masks;
     int slot = 0;
     for (int t = first; t < t1; t += W) {
-        wait_vmcnt<PER_TILE *(ST - 1)>();                        // this tile has landed
+        if (ST > 1 && t + W < t1) wait_vmcnt<PER_TILE *(ST - 1)>();      // this tile has landed
+        else wait_vmcnt<0>();
         __builtin_amdgcn_sched_barrier(0);
         memory_fence_of_the_compiler();
         v4i kw[4];                                               // 16 keys each: the bytes of this lane (d = 64: two dwords)
@@ -281,7 +286,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
         wait_lds();
         __builtin_amdgcn_sched_barrier(0);
         memory_fence_of_the_compiler();
-        stage(t + ST * W, slot);                            // into the place this tile has left
+        if (t + ST * W < t1) stage(t + ST * W, slot);            // into the place this tile has left
         __builtin_amdgcn_sched_barrier(0);
         slot = slot == ST - 1 ? 0 : slot + 1;
 
@@ -384,7 +389,6 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
                 }
             }
     }
-    wait_all_memory();                                           // requests past the last tile
     __syncthreads();                                             // every wavefront is done with its buffers: o may lie there
 
     // ---- they meet: M, l and o of each as they are, then whoever has four columns of a row weighs them.  (All rows at once: 16 by 16, 8 x 4 heads with 40 rows on up to 16391 keys 27.3 -> 26.7 us.)
@@ -700,7 +704,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
     v4i qf[DT];
 #pragma unroll
     for (int kk = 0; kk < DT; ++kk) qf[kk] = *reinterpret_cast<const v4i *>(c.Q + qrow * D + 32 * kk + 16 * g);
-    const float sq2 = p >= 0 ? query_scale(c.sQ[qrow], qf) : 1.0f;                // (padding: whatever its scale holds, its row is zeros)
+    const float sq = c.sQ[qrow], sq2 = query_scale(p >= 0 ? sq : 1.0f, qf);        // (padding: whatever its scale holds, its row is zeros)
     v16i bias;
 #pragma unroll
     for (int v = 0; v < 16; ++v) bias[v] = 0;
