@@ -35,7 +35,7 @@ template <int D> constexpr int TILE4 = KEYS4 * D / 2;        // and of a tile's 
 [[maybe_unused]] constexpr float FEW4_BELOW = 15.0f, TILE4_BELOW = 7.0f, SLACK4 = 8.0f;     // the largest weight is 2^15; in tiles 2^7, and 2^15 until M moves
 
 // Sequences of different lengths, which the host does not know: a sequence of t tiles has ceil(t / C) parts, at least one, with C so that there are about `places` parts of all units, which is what the chip
-// holds at once; workgroup w counts its way to its part.  (In as many parts each, the longest sequence decides: 8 x 4 heads, 40 rows on 0 .. 16391 keys 31.8 us, like this 26.7; 16 x 8 heads, one of 16384 keys and 15 of 100 26.7 and 13.7.)  A unit in one part goes straight
+// holds at once; workgroup w counts its way to its part.  (In as many parts each, the longest sequence decides: 8 x 4 heads, 40 rows on 0 .. 16391 keys 31.1 us, like this 25.8; 16 x 8 heads, one of 16384 keys and 15 of 100 26.3 and 13.6.)  A unit in one part goes straight
 // to O; parts_of[unit] = (its first part, their number).
 struct Sharing {
     int places;                            // 0: c.splits parts of every unit
