@@ -167,7 +167,7 @@ template <int D, int RT, int W, int ST> struct SmemFew4 {
             alignas(4096) int8_t k[W][ST][TILE4<D>];
             alignas(4096) int8_t v[W][ST][TILE4<D>];
             alignas(256) float sk[W][ST][KEYS4], sv[W][ST][KEYS4];
-            alignas(256) float log_sv[W][KEYS4], inv_sv[W][KEYS4], sign[W][KEYS4];     // of the tile at hand
+            alignas(256) float log_sv[W][KEYS4], inv_sv[W][KEYS4], rest[W][KEYS4];     // of the tile at hand
         };
         float o[W][16 * RT][D];                                  // when the loop is over
     };
@@ -199,7 +199,7 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
     const unsigned gk = crow * ROW + 16 * (cslot ^ k4_slot<D>(crow));
     const unsigned gv0 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow)), gv1 = crow * ROW + 16 * (cslot ^ v4_slot<D>(crow + 1024 / ROW));
     const lds_ptr kbuf = (lds_ptr)(&sm.k[wave][0][0]), vbuf = (lds_ptr)(&sm.v[wave][0][0]), skbuf = (lds_ptr)(&sm.sk[wave][0][0]), svbuf = (lds_ptr)(&sm.sv[wave][0][0]);
-    const lds_ptr logbuf = (lds_ptr)(&sm.log_sv[wave][0]), invbuf = (lds_ptr)(&sm.inv_sv[wave][0]), signbuf = (lds_ptr)(&sm.sign[wave][0]);
+    const lds_ptr logbuf = (lds_ptr)(&sm.log_sv[wave][0]), invbuf = (lds_ptr)(&sm.inv_sv[wave][0]), restbuf = (lds_ptr)(&sm.rest[wave][0]);
     auto stage = [&](int t, int slot) {
         const bool inA = t < tilesA;
         const int j0 = KEYS4 * (inA ? t : t - tilesA);
@@ -290,12 +290,12 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
         __builtin_amdgcn_sched_barrier(0);
         slot = slot == ST - 1 ? 0 : slot + 1;
 
-        // log2 |s_V| and 1 / |s_V|, a key to a lane, handed round to the lanes that have the key's scores; a scale of 0 or a negative one also leaves a factor, later
+        // log2 |s_V| and 1 / |s_V|, at least 2^-80, a key to a lane, handed round to the lanes that have the key's scores.  What s_V is beside that, its sign, 0 or 2^80 s_V, is a factor of the weight, later
         const float sv_size = fmaxf(fabsf(sv_here), LEAST_SCALE);
         *reinterpret_cast<LDS_AS float *>(logbuf + 4 * lane) = __builtin_amdgcn_logf(sv_size);
         *reinterpret_cast<LDS_AS float *>(invbuf + 4 * lane) = __builtin_amdgcn_rcpf(sv_size);
-        const bool odd = __any(!(sv_here > 0.0f));
-        if (odd) *reinterpret_cast<LDS_AS float *>(signbuf + 4 * lane) = sv_here > 0.0f ? 1.0f : sv_here < 0.0f ? -1.0f : 0.0f;
+        const bool odd = __any(!(sv_here >= LEAST_SCALE));
+        if (odd) *reinterpret_cast<LDS_AS float *>(restbuf + 4 * lane) = fminf(fmaxf(sv_here * (1.0f / LEAST_SCALE), -1.0f), 1.0f);
         v4i kop[4][KS];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
@@ -345,27 +345,24 @@ __device__ __forceinline__ void few4_rows_of_a_unit(SmemFew4<D, RT, W, ST> &sm, 
             m2[rt] = m_new;
             float psum = 0.0f;
             h2 w[8];                                             // keys 0, 2 and 1, 3 of each four: the order of values_of
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                const v4f is = *reinterpret_cast<LDS_AS const v4f *>(invbuf + 16 * q + 64 * kb);
-                float x[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[i] = __builtin_amdgcn_exp2f(a[4 * kb + i] - m_at);
-                    psum = __builtin_fmaf(x[i], is[i], psum);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) w[2 * kb + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
-            }
-            l[rt] = __builtin_fmaf(l[rt], alpha, psum);
-            if (odd) {
+            auto weights = [&](auto odd_) {
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb) {
-                    const v4f f = *reinterpret_cast<LDS_AS const v4f *>(signbuf + 16 * q + 64 * kb);
+                    const v4f is = *reinterpret_cast<LDS_AS const v4f *>(invbuf + 16 * q + 64 * kb);
+                    v4f x;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) w[2 * kb + i] *= h2{(_Float16)f[i], (_Float16)f[i + 2]};
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = __builtin_amdgcn_exp2f(a[4 * kb + i] - m_at);
+                        psum = __builtin_fmaf(x[i], is[i], psum);
+                    }
+                    if constexpr (decltype(odd_)::value) x *= *reinterpret_cast<LDS_AS const v4f *>(restbuf + 16 * q + 64 * kb);      // (before the weight is rounded: once)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) w[2 * kb + i] = h2{(_Float16)x[i], (_Float16)x[i + 2]};
                 }
-            }
+            };
+            if (odd) weights(std::true_type{});
+            else weights(std::false_type{});
+            l[rt] = __builtin_fmaf(l[rt], alpha, psum);
             if (__any(alpha != 1.0f)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
