@@ -365,7 +365,7 @@ int read_keys(const void *K_c, const float *s_K, const void *V_c, const float *s
 /*
  * int_flash_attn_fwd_window over a cache in 4 bits (IFA_CACHE_I4): the same queries, lens, window, sinks and rules; s_K, s_V [B, Hkv, Nk].  A prompt, a chunk, draft tokens, a decode step.
  *   O = sum_j p_j s_V[j] v_j / sum_j p_j.  s_K may be any finite numbers whose scores are finite, s_V any with |s_V| < 2^20.  A summand's weight p_j s_V[j] is rounded to fp16: by at most 2^-11 of itself, or by
- * 2^-40 (tiles of 128 rows: 2^-32) of the largest product of a weight of its row and a scale of the keys that its tile has met (2^-80 at least) if that is more.  The sum of the p_j is fp32.
+ * 2^-40 (tiles of 128 rows: 2^-32) of the largest product of a weight and a scale (2^-80 at least) of the keys that its row sees if that is more; what it does not see does not count.  The sum of the p_j is fp32.
  */
 long ifa_int4_workspace_bytes(int B, int H, int Hkv, int Nq, int Nk, int d, int window, int sinks);
 

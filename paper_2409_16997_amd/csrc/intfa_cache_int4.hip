@@ -33,6 +33,7 @@ template <int D> constexpr int ROW4 = D / 2;                 // bytes of a row o
 template <int D> constexpr int TILE4 = KEYS4 * D / 2;        // and of a tile's K or V
 [[maybe_unused]] constexpr float LEAST_SCALE = 0x1p-80f;
 [[maybe_unused]] constexpr float FEW4_BELOW = 15.0f, TILE4_BELOW = 7.0f, SLACK4 = 8.0f;     // the largest weight is 2^15; in tiles 2^7, and 2^15 until M moves
+[[maybe_unused]] constexpr int ALIKE4 = 4;                   // tiles, log2: scales of a block that are no further apart take M to the smallest of them where keys are hidden
 
 // Sequences of different lengths, which the host does not know: a sequence of t tiles has ceil(t / C) parts, at least one, with C so that there are about `places` parts of all units, which is what the chip
 // holds at once; workgroup w counts its way to its part.  (In as many parts each, the longest sequence decides: 8 x 4 heads, 40 rows on 0 .. 16391 keys 31.1 us, like this 25.8; 16 x 8 heads, one of 16384 keys and 15 of 100 26.3 and 13.6.)  A unit in one part goes straight
@@ -154,8 +155,6 @@ __device__ __forceinline__ float wave_max(float x) {
 // at a time, they took 128 of the 294 cycles that LDS is busy for 32 rows and 64 keys in tiles (2 x 32 heads, prompts of 4096 284 -> 272 us).
 template <int N> __device__ __forceinline__ float of_row(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x150 + N, 0xf, 0xf, true)); }
 template <typename F, int... I> __device__ __forceinline__ void unrolled(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
-// log2 of a bound of |s_V| over the tile, from this lane's key
-__device__ __forceinline__ float scale_bound(float sv) { return __builtin_amdgcn_logf(fmaxf(wave_max(fabsf(sv)), LEAST_SCALE)); }
 #endif
 
 // ---- up to 16 RT rows against many keys: every wavefront for itself ----------------------------------------------------
@@ -523,7 +522,7 @@ template <int D> struct SmemTile4 {
     alignas(4096) int8_t k[2][KEYS4 * D];
     alignas(4096) int8_t v[2][KEYS4 * 2 * D];
     alignas(256) float sk[2][KEYS4], sv[2][KEYS4];
-    float sv_log[2];                       // log2 of a bound of |s_V|
+    float2 sv_size[2];                     // log2 of the largest |s_V|; that |s_V| 2^-ALIKE4
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -554,9 +553,9 @@ __device__ __forceinline__ void unpack_v(const u4 &w, const NibbleMasks &m, lds_
     }
 }
 
-// 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`.
+// 64 keys in LDS against the wavefront's rows.  `clear`: all of them count for every row, otherwise those of `seen`, none behind key `last`.
 template <int D>
-__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, float below, int lane, const Lane<D, false> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
+__device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, lds_ptr sv, float2 size, int last, int lane, const Lane<D, false> &lo, const v4i (&qf)[D / 32], float sq2, bool clear, uint64_t seen,
                                             const v16i &bias, RowState4<D> &st) {
     constexpr int KS = D / 32, DT = D / 32;
     const int g = lane >> 5;
@@ -582,12 +581,30 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
         unrolled([&](auto v_) { constexpr int v = decltype(v_)::value; a[mt][v] = (__int_as_float(acc[mt][v]) - ACC_BIAS_F) * of_row<v>(skv[mt]); }, std::make_integer_sequence<int, 16>{});
+    // log2 of bounds of the largest |s_V| that the row sees, from above and from below: M moves when it has to by the one, and to where the other puts it.  A hidden key's scale in M would take the
+    // weights that count under fp16's range.  Scales of a block within 2^ALIKE4 bound each other; otherwise each row finds its own largest.  (M by all 64 keys, seen or not: 3 x 12 heads of 64, up to 1777 queries, window 333, 19.0 us, like
+    // this 19.9, with the row's own in every block that is not clear 21.4.)
+    float high = size.x, low = size.x;
     if (!clear) {
+        const float one = fabsf(*reinterpret_cast<LDS_AS const float *>(sv + 4 * lane));
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 if (!(static_cast<uint32_t>(seen >> (32 * mt)) >> (4 * g) & (1u << (8 * (v >> 2) + (v & 3))))) a[mt][v] = -INFINITY;
+        if (!__any(lane <= last && one < size.y)) low = high - ALIKE4;
+        else {
+            int most = 0;                                        // (as integers, which numbers that are not negative compare like)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                const float abs_sv = fabsf(svv[mt]);
+                unrolled([&](auto v_) {                          // a hidden key's -inf is a negative integer, other scores + 2^100 are above any scale
+                    constexpr int v = decltype(v_)::value;
+                    most = imax(most, imin(__float_as_int(of_row<v>(abs_sv)), __float_as_int(a[mt][v] + 0x1p100f)));
+                }, std::make_integer_sequence<int, 16>{});
+            }
+            high = low = __builtin_amdgcn_logf(fmaxf(pair_max(__int_as_float(most)), LEAST_SCALE));
+        }
     }
     float bmax = -INFINITY;
 #pragma unroll
@@ -595,10 +612,10 @@ __device__ __forceinline__ void tile4_block(lds_ptr ks, lds_ptr vs, lds_ptr sk, 
 #pragma unroll
         for (int v = 0; v < 16; ++v) bmax = fmaxf(bmax, a[mt][v]);
     __builtin_amdgcn_sched_barrier(0);
-    const float top = __builtin_fmaf(pair_max(bmax), sq2, -below);
+    const float top = __builtin_fmaf(pair_max(bmax), sq2, high - TILE4_BELOW);
     const bool moves = top > st.m2 + SLACK4;                     // (st.m2 = -inf: whenever a key counts)
     if (__any(moves)) {
-        const float m_new = moves ? top : st.m2;
+        const float m_new = moves ? top - (high - low) : st.m2;
         const float alpha = moves ? __builtin_amdgcn_exp2f(st.m2 - m_new) : 1.0f;
         st.m2 = m_new;
         st.l *= alpha;
@@ -691,8 +708,8 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
         if (D == 128 || wave >= 2) unpack_v(D == 128 ? vraw : kraw, masks, v + 64 * ((pc >> 1) ^ vx), v + 64 * (((pc >> 1) + D / 64) ^ vx));
         if (wave < 2) *reinterpret_cast<LDS_AS float *>((wave == 0 ? skbuf : svbuf) + slot * 256 + 4 * lane) = sraw;
         if (wave == 1) {
-            const float bound = scale_bound(sraw);
-            if (lane == 0) sm.sv_log[slot] = bound;
+            const float most = wave_max(fabsf(sraw)), high = __builtin_amdgcn_logf(fmaxf(most, LEAST_SCALE));
+            if (lane == 0) sm.sv_size[slot] = float2{high, most * (1.0f / (1 << ALIKE4))};
         }
     };
     if (t0 < t1) fetch(t0);
@@ -730,7 +747,7 @@ __device__ __forceinline__ void tile4_of_a_unit(SmemTile4<D> &sm, const Call &c,
         const bool any = alive && hi1 >= v0 && (hi0 - window < v0 + KEYS4 - 1 || v0 < sink);
         const bool clear = hi0 >= v0 + KEYS4 - 1 && (hi1 - window < v0 || v0 + KEYS4 <= sink);
         const uint64_t seen = clear ? 0 : keys_seen(hi - v0, hi - window + 1 - v0, sink - v0);
-        if (any) tile4_block<D>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, svbuf + slot * 256, TILE4_BELOW - sm.sv_log[slot], lane, lo, qf, sq2, clear, seen, bias, st);
+        if (any) tile4_block<D>(kbuf + slot * KB, vbuf + slot * VB, skbuf + slot * 256, svbuf + slot * 256, sm.sv_size[slot], hi1 - v0, lane, lo, qf, sq2, clear, seen, bias, st);
         __syncthreads();
     }
 

@@ -33,3 +33,23 @@ def test_scales_below_the_smallest_that_counts(ifa, kind, turn):  # noqa: F811
     want, tol = exact.attention(s, lens, tiles=kind.startswith("tiles"))
     assert ((want.abs() > 4 * tol).double().mean() > 0.2) or turn == "the smallest"      # (the tolerance leaves something to see)
     check(int4(ifa, s, None, 0, lens, out_dtype=torch.float32), want, tol)
+
+
+# B, Hkv, G, Nq, Nk, d, window: tiles of 128 rows
+TILES = [(2, 40, 1, 512, 512, 64, None), (2, 40, 2, 300, 700, 128, None), (2, 40, 1, 500, 900, 64, 40), (2, 40, 2, 300, 700, 128, 40), (1, 48, 3, 170, 333, 128, 5)]
+
+
+@pytest.mark.parametrize("case", TILES, ids=[f"{i}" for i in range(len(TILES))])
+def test_hidden_keys_do_not_count(ifa, case):  # noqa: F811
+    """Keys with scales 2^39 of the others', some of them later than a query or in front of its window in the same tile of keys: its output is what it is without them."""
+    B, Hkv, G, Nq, Nk, d, w = case
+    s = ref.problem(9, B, Hkv, G, Nq, Nk, d)
+    lens = [Nk, Nk - 37][:B]
+    s["sv"] = (s["sv"] * 2.0 ** -20).float()
+    if w is None:
+        s["sv"][:, :, (Nk - Nq) // 64 * 64 + 63] = 2.0 ** 19             # the last key of the tile in which the queries begin
+    else:
+        s["sv"][:, :, 31::97] = 2.0 ** 19
+    want, tol = exact.attention(s, lens, w, tiles=True)
+    assert (want.abs() > 4 * tol).double().mean() > 0.2
+    check(int4(ifa, s, w, 0, lens, out_dtype=torch.float32), want, tol)
