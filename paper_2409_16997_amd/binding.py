@@ -607,6 +607,8 @@ def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=
     """A run of the cache (as append_keys has it) back as values: (K, V) [B, Hkv, count, d], fp16 unless out_dtype/out says otherwise.  Row i is the key at first + i, or with first=None at
     lens[b] - count + i; rows in front of key 0 or behind the last one are zeros.  count: None for all from `first` on.  hadamard=True rotates K back.
     out: optional tuple of the two tensors to write into."""
+    if first is not None and int(first) < 0:                         # (-1 is the C call's word for the last ones)
+        raise IntfaError(f"keys from {first} on: first is at least 0, or None for the last ones")
     first = -1 if first is None else int(first)
     if out is None and count is not None:
         r = (_native or _load_native()).read(K_c, s_K, V_c, s_V, lens, first, count, hadamard, out_dtype)
@@ -618,8 +620,8 @@ def read_keys(K_c, s_K, V_c, s_V=None, lens=None, first=0, count=None, hadamard=
     if first == -1 and count is None:
         count = Nk
     count = Nk - first if count is None else int(count)
-    if first < -1 or first > Nk or count < 1 or B * Hkv * count > 1 << 28:
-        raise IntfaError(f"{count} keys from {first} on of {Nk} (at least one, and at most 2^28 rows in all)")
+    if first > Nk or count < 1 or B * Hkv * count > 1 << 28:
+        raise IntfaError(f"{count} keys {'at the end' if first < 0 else f'from {first} on'} of {Nk} (at least one, and at most 2^28 rows in all)")
     shape = (B, Hkv, count, d)
     if out is None:
         out = tuple(torch.empty(shape, dtype=out_dtype or torch.float16, device=K_c.device) for _ in range(2))
