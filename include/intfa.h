@@ -49,7 +49,8 @@ int ifa_set_stream(void *hip_stream);
  *   X       [rows, d] real activations of dtype x_dtype (ifa_dtype), rows = B*H*N
  *   Xq      [rows, d] int8 out:  q = clamp(rint(x * (127 / a)), -127, 127), a = max_k |x[r,k]|
  *   scale   [rows] fp32 out:     a / 127  (fp32 divide); an all-zero row gets scale 1, q = 0
- * Arithmetic is fp32 with round-half-to-even and is bit-exact against that definition.
+ * Arithmetic is fp32 with round-half-to-even and is bit-exact against that definition.  Where 127 / a is infinite
+ * (a < 3.8e-37) that is q = 0 for x = 0 and +-127 for any other x.
  * d must be one of 32, 64, 128, 256, 512.  NaN/Inf inputs are outside the contract.
  */
 int quantize_tokenwise(const void *X, int x_dtype, long rows, int d,

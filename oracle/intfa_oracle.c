@@ -41,7 +41,7 @@ int orc_num_threads(void)
  * One scale per row of a [rows, cols] matrix: cols = d gives the token-level scheme of
  * Q and K; rows = heads, cols = N*d gives the tensor-level scheme of V.
  *   a = max|x|, s = a / 127, q = clamp(rint(x * (127 / a)), -127, 127); a == 0 -> s = 1, q = 0.
- * All in fp32, round-half-to-even. */
+ * All in fp32, round-half-to-even.  Where 127 / a is infinite (a < 3.8e-37) x = 0 still gives 0, any other x +-127. */
 void orc_quantize_rows(const float *X, int64_t rows, int64_t cols, int8_t *q, float *s)
 {
 #pragma omp parallel for schedule(static)
@@ -61,7 +61,7 @@ void orc_quantize_rows(const float *X, int64_t rows, int64_t cols, int8_t *q, fl
         s[r] = a / 127.0f;
         const float inv = 127.0f / a;
         for (int64_t k = 0; k < cols; ++k) {
-            float t = rintf(x[k] * inv);
+            float t = x[k] == 0.0f ? 0.0f : rintf(x[k] * inv);
             if (t > 127.0f) t = 127.0f;
             if (t < -127.0f) t = -127.0f;
             qr[k] = (int8_t)t;

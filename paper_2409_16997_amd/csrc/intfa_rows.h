@@ -71,14 +71,19 @@ __device__ __forceinline__ float absmax8(const float (&x)[8]) {
     return a;
 }
 
-// q = clamp(rint(x * inv), -127, 127) for 8 values, packed little-endian into two dwords.
+// The conversion as the hardware does it, which C++ leaves undefined: NaN becomes 0, what is too large the nearest integer.
+__device__ __forceinline__ int to_int(float t) {
+    int i;
+    asm("v_cvt_i32_f32 %0, %1" : "=v"(i) : "v"(t));
+    return i;
+}
+// q = clamp(rint(x * inv), -127, 127) for 8 values, packed little-endian into two dwords.  For rows below 127 / max fp32 inv is infinite: every number but 0 is +-127, and 0 times it, NaN, is 0.
 __device__ __forceinline__ uint2 quant8(const float (&x)[8], float inv) {
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float t = rintf(x[i] * inv);
-        t = fminf(fmaxf(t, -127.0f), 127.0f);
-        w[i >> 2] |= (static_cast<uint32_t>(static_cast<int>(t)) & 0xffu) << (8 * (i & 3));
+        const int t = to_int(rintf(x[i] * inv));
+        w[i >> 2] |= (static_cast<uint32_t>(t < -127 ? -127 : t > 127 ? 127 : t) & 0xffu) << (8 * (i & 3));
     }
     return make_uint2(w[0], w[1]);
 }
