@@ -348,6 +348,7 @@ typedef enum { IFA_CACHE_I8_F16 = 0, IFA_CACHE_I8 = 1, IFA_CACHE_I4 = 2 } ifa_ca
  *   V      rounded to fp16; or q = clamp(rint(x * (1 / s_V)), -127, 127) by the given scale (0: codes 0); or in 4 bits as K (never rotated).
  *   s_V    null; or [B, Hkv], read; or [B, Hkv, Nk], written.
  * Tokens at p < 0 (padding in front) are not written, nothing else of the cache is changed.  fp32 with round-half-to-even, bit-exact against that definition.  NaN/Inf are outside the contract.
+ * Scales of V in 4 bits of 2^20 and more (rows of 7 2^20 and more, which fp16 has none of) are written and read back, but int_flash_attn_fwd_int4 does not take them.
  * Supported: d in {64, 128}; B Hkv Nn <= 2^28.  The cache's arrays overlap neither the tokens, nor lens, nor each other (else IFA_ERR_UNSUPPORTED).
  */
 int append_keys(const void *K, const void *V, int x_dtype, long K_stride_b, long K_stride_h, long K_stride_n, long V_stride_b, long V_stride_h, long V_stride_n,

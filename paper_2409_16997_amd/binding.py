@@ -588,7 +588,8 @@ def _tokens(X, what, dtype, shape, dev):
 def append_keys(K, V, K_c, s_K, V_c, s_V=None, lens=None, hadamard=False):
     """New tokens K, V [B, Hkv, Nn, d] fp32/fp16/bf16 (any strides of b, h and n) quantized into a cache: int8 K_c [B, Hkv, Nk, d] with V_c fp16, or int8 by the
     given s_V [B, Hkv]; or uint8 K_c, V_c [B, Hkv, Nk, d / 2] in 4 bits with s_V [B, Hkv, Nk]; s_K [B, Hkv, Nk].  lens[b] keys (int32 [B]; None: Nk) count the new ones, which are the last
-    Nn: token i goes to lens[b] - Nn + i, and nowhere if that is below 0.  hadamard=True rotates K as quantize_tokenwise does.  The cache is changed in place."""
+    Nn: token i goes to lens[b] - Nn + i, and nowhere if that is below 0.  hadamard=True rotates K as quantize_tokenwise does.  The cache is changed in place.
+    (int_flash_attn_fwd_int4 takes scales of V below 2^20: rows of up to 7 2^20, any fp16 row.)"""
     if (_native or _load_native()).append(K, V, K_c, s_K, V_c, s_V, lens, hadamard):
         return
     import torch
