@@ -6,7 +6,8 @@
 
 namespace ifa {
 
-// n / d for n < 2^31 by a multiplication: the quotient's multiplier of 33 bits, the 33rd being the + n
+// n / d for n < 2^31 by a multiplication: the quotient's multiplier, 2^(32 + s) / d rounded up, has 33 bits, the 33rd being the + n (T. Granlund, P. L. Montgomery, "Division by Invariant Integers
+// using Multiplication", 1994; n < 2^31 spares their sum its second shift)
 struct Divisor {
     unsigned d, m, s;
     explicit Divisor(unsigned d_) : d(d_), s(0) {
