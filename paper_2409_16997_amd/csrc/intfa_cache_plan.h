@@ -86,15 +86,20 @@ struct Int4Plan {
 };
 // Tiles of 128 rows, which unpack a key once for all of them but start and end late, where these are at most two sevenths as many as tiles of 32 and those are more than fit the chip at once, two workgroups to a CU,
 // or have more than 900 K keys (us, 32 rows / 128, key heads x rows x keys, d = 128: 160 x 100 x 300 17.8 / 13.3, 128 x 100 x 300 11.6 / 12.8; 80 x 256 x 456 18.4 / 17.9, 64 x 256 x 456 13.3 / 17.0; window 256, 20 heads of 1000
-// queries 18.1 / 15.3, 16 heads 11.8 / 15.0; causal, 9 x 2048 46.1 / 31.1, 8 x 1500 19.4 / 25.5, 4 x 3500 53.6 / 35.4; 64 x 100 x 4000 36.8 / 32.4, 16 x 256 x 4000 24.8 / 29.5, x 16000 57.0 / 52.5; 64 x 40 x 16000 63.8 / 74.5.
+// queries 18.2 / 16.2, 16 heads 12.1 / 16.1; causal, 9 x 2048 46.1 / 31.1, 8 x 1500 19.4 / 25.5, 4 x 3500 53.6 / 35.4; 64 x 100 x 4000 36.8 / 32.4, 16 x 256 x 4000 24.8 / 29.5, x 16000 57.0 / 52.5; 64 x 40 x 16000 63.8 / 74.5.
 // d = 64: 136 x 100 x 300 13.1 / 10.3, 24 heads of 1000 causal 19.7 / 22.2, 64 x 256 x 1000 14.6 / 21.2).  In full turns also with fewer rows to a tile, on short keys, where a turn of 32-row workgroups is mostly its start and end
 // (400 x 40 x 300 20.2 / 16.2, x 512 21.1 / 21.3, 640 x 64 x 64 19.6 / 12.6, 600 x 80 x 500 40.4 / 36.1; 260 x 64 x 768 22.2 / 28.4, 300 x 96 x 2000 57.2 / 70.2; up to 32 rows: 600 x 32 x 64 11.7 / 10.7, x 300 19.0 / 23.0;
 // 16: 600 x 16 x 64 6.6 / 10.5).
 //   Otherwise 16 or 32 rows to a workgroup of four wavefronts that take 64 keys each in a round.  A round takes 1.2 us, parts and their join 2.9 us more than none: parts of as few rounds as there are places for two
 // workgroups on a CU, if that saves three rounds, and with many groups, whose rounds wait for memory, more (128 x 1500 whole 12.7, in four parts 13.5; 256 x 3000 25.5 both, in two; 64 x 1100 10.5 and, in three, 9.7;
-// 8 x 2200 14.9 and, in eight, 9.3).  Up to 64 parts, or 128 where that is one workgroup on a CU (1 x 200000 24.2 and 19.0, 2 x 131072 19.1 and 16.2, 1 x 40000 10.9 and 11.4; 4 x 94150 17.7 and 19.3).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 6.9, 8.5 in two parts, 7.5 whole; d = 64 5.8, 7.7, 6.6).
-//   With lens, parts by the lengths where that is more than three rounds a part (8 x 8 x up to 2048 10.1 us in as many each, 11.4 counted out), for as many places as registers leave: three workgroups of 16 rows on a
-// CU (16 x 8 x 8191 of 16384 34.3, in as many each 35.5), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 25.8, in as many each 31.1).
+// 8 x 2200 14.9 and, in eight, 9.3).  Up to 64 parts, or 128 where that is one workgroup on a CU (1 x 200000 24.2 and 19.0, 2 x 131072 19.1 and 16.2, 1 x 40000 10.9 and 11.4; 4 x 94150 17.7 and 19.3).  Up to 128 groups of somewhat more keys than one round: eight wavefronts, two tiles ahead each (8 x 700 6.9, 8.5 in two parts, 7.5 whole; d = 64 5.8, 7.7, 6.6).  At its lines, eight
+// wavefronts / four, d = 128: 8 x 256 5.1 / 4.7, x 300 6.0 / 6.1, x 340 6.1 / 6.2; 8 x 768 6.9 / 7.3, x 800 8.3 / 7.4, x 896 8.1 / 7.3, 64 x 860 8.5 / 8.1, 120 x 860 9.7 / 9.6; 8 groups of 32 rows x 768 9.5 / 10.5, x 896 11.3 / 9.4;
+// 120 x 700 7.7 / 8.2, 140 x 700 8.3 / 8.4, 200 x 700 9.4 / 8.9.  d = 64: 8 x 256 4.6 / 4.3, x 340 5.2 / 5.4; 8 x 1000 6.7 / 7.0, x 1200 6.9 / 7.5, 8 groups of 32 rows x 1024 8.7 / 8.2; 120 x 700 6.1 / 6.7, 200 x 700 6.5 / 7.1.  So at
+// d = 128 they are the slower side from 769 keys on, where a wavefront has a second tile, by up to 1 us (32 rows: 2).
+//   With lens, parts by the lengths where that is more than three rounds a part (8 x 8 x up to 2048 10.1 us in as many each, 11.4 counted out), for three workgroups of 16 rows on a
+// CU (16 x 8 x 8191 of 16384 34.3, in as many each 35.5), two of 32 (8 x 4 heads, 40 rows on up to 16391 keys 25.8, in as many each 31.1).  Registers leave room for three of 16 rows at d = 128 and four at d = 64.  For two / three / four, lengths
+// even from 0 to the largest unless stated: d = 128, 16 x 8 x 16384 34.1 / 34.7 / 35.3, one long and 15 of 100 12.3 / 13.6 / 13.4, 64 x 2 x 8192 21.4 / 21.9 / 21.9, 32 x 4 x 900 to 4000 16.7 / 16.8 / 16.9; d = 64 24.8 / 22.6 / 23.6, 10.2 / 11.2 / 11.1,
+// 16.2 / 15.7 / 15.9, 13.6 / 13.9 / 13.9.
 static inline Int4Plan int4_plan(int B, int Hkv, int G, int Nq, int Nk, int d, int window, int sinks, bool lens) {
     const long units = static_cast<long>(B) * Hkv, rows = static_cast<long>(G) * Nq;
     const long span = static_cast<long>(window) + (Nq < TILE_ROWS ? Nq : TILE_ROWS) + sinks, keys = Nk < span ? Nk : span;
